@@ -312,6 +312,83 @@ DSV_API dsv_status dsv_profile_sparsity(const dsv_problem *p, const void *Q, con
                                         int32_t n_rows, float mass, int32_t *counts, float *sparsity, float *ema,
                                         float alpha, void *workspace, size_t ws_bytes, void *hip_stream);
 
+/* ---- Full attention over packed sequences --------------------------------------------------------------
+ * Sec. "Various Self-Attention Paradigms": what every block runs until the predictors are good enough, and afterwards every block that
+ * the method's dispatcher does not find worth sparsifying; with other lengths on the key side, attention to a caption or to a
+ * cache of earlier tokens.  Sequences of any lengths (0 and 1 among them) lie one behind another:
+ *     sequence s: query tokens cu_q[s] .. cu_q[s+1] - 1, key tokens cu_k[s] .. cu_k[s+1] - 1  (nq, nk of them)
+ *     query i of it sees its keys j < nk, with causal set those with j <= i + nk - nq (the last query sees all);
+ *     head h of Q reads head h / (Hq / Hkv) of K and V.
+ * dsv_packed_attn_fwd: O and lse as for dsv_sparse_attn_fwd.  A query that sees no key: O = 0, lse = -inf, and no gradient comes from it.
+ * dsv_packed_attn_bwd: dQ, dK, dV; dK and dV are summed over the heads that share them; keys that no query sees get zeros.
+ *
+ *   - Q, O, dO, dQ: [total_q, Hq, d]; K, V, dK, dV: [total_k, Hkv, d]; every tensor with its own strides from token to token and head
+ *     to head, in elements, multiples of 16 bytes, the d channels side by side: [B, H, L, d] memory is one sequence of B * H heads
+ *     {d, L * d}, a slice of a fused projection's output {3 * H * d, d}.  The strides of inputs may be anything from 0, those of outputs
+ *     must keep its rows apart (one at least d, the other beyond all of those).
+ *   - lse: float [Hq, total_q].  cu_q, cu_k: DEVICE int32 [n_seq + 1], ascending from 0.  They are read by the kernels only: a call that
+ *     was captured into a graph replays on whatever lengths they hold then, within the descriptor's limits.  max_q, max_k (HOST) bound
+ *     the lengths; sequences longer than that, and entries that are not ascending or point behind the tensors, give undefined results
+ *     but no access outside the tensors.  Rows that belong to no sequence are left as they are, in every output, and may hold anything.
+ *   - O_tail (bf16; NULL: not wanted; must be NULL for F32): bf16 [total_q, Hq, d], contiguous, what rounding O took away.  Given to the
+ *     backward, it forms Delta from all 16 bits: gradients within 3e-3 of the exact ones (relative, in norm), where O alone leaves 3 to 6e-3.
+ *   - scale: finite and > 0.  The weights enter the second product as bf16 (bf16 tensors), everything else is held in 32 bits.  The same
+ *     results from run to run, bit for bit.
+ *   - Limits: Hkv divides Hq; total_q * Hq * (Hq / Hkv) < 2^32; total_q * Hq / 32 + n_seq * Hkv < 2^24, and so for total_k * Hkv;
+ *     anything larger: DSV_EUNSUPPORTED.  total_q, total_k of 0 are accepted, the tensors may then be NULL.
+ *   - Workspace: the forward's, of calls with few rows, for partial results of pieces of the key axis (else the query returns 0); the backward's
+ *     for two floats a row and partial sums. */
+typedef struct dsv_rows {
+    int64_t row, head;   /* elements from one token, from one head, to the next */
+} dsv_rows;
+typedef struct dsv_packed {
+    int32_t n_seq;             /* sequences, >= 1 */
+    int32_t total_q, total_k;  /* tokens in Q and in K, V (of the tensors, not of the sequences) */
+    int32_t max_q, max_k;      /* no sequence has more queries, more keys */
+    int32_t Hq, Hkv;           /* heads of Q, and of K and V */
+    int32_t d;                 /* head dimension */
+    int32_t dtype;             /* dsv_dtype of every tensor but lse */
+    int32_t causal;            /* 0 or 1 */
+    float scale;
+    uint32_t flags;            /* 0 */
+    dsv_rows q, k, v, o;       /* layouts; the forward reads these */
+    dsv_rows dO, dq, dk, dv;   /* and the backward all */
+} dsv_packed;
+DSV_API size_t dsv_packed_attn_fwd_workspace(const dsv_packed *p);
+DSV_API dsv_status dsv_packed_attn_fwd(const dsv_packed *p, const void *Q, const void *K, const void *V, const int32_t *cu_q,
+                                       const int32_t *cu_k, void *O, void *O_tail, float *lse, void *workspace, size_t ws_bytes,
+                                       void *hip_stream);
+DSV_API size_t dsv_packed_attn_bwd_workspace(const dsv_packed *p);
+DSV_API dsv_status dsv_packed_attn_bwd(const dsv_packed *p, const void *Q, const void *K, const void *V, const int32_t *cu_q,
+                                       const int32_t *cu_k, const void *O, const void *O_tail, const float *lse, const void *dO,
+                                       void *dQ, void *dK, void *dV, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/* ---- Layer norm -----------------------------------------------------------------------------------------
+ * Of the rows of Q and K before they are scored (n = d, one row a token and head), or of a block's activations (n = width, heads = 1):
+ *     mu = mean x;  r = 1 / sqrt(mean (x - mu)^2 + eps);  y = (x - mu) r gamma + beta;   mean, rstd keep mu and r
+ *     xh = (x - mu) r,  g = dy gamma:   dx = r (g - mean g - xh mean(g xh));   dgamma = sum dy xh, dbeta = sum dy over all rows
+ *   - X, Y, dY, dX: [tokens, heads, n], strides as above but of any size and alignment (rows that begin on 16 bytes and fill whole
+ *     ones are read 16 bytes at a time).  No output may overlap an input.
+ *   - gamma, beta: [n] in `dtype`, or NULL (1 and 0); dgamma, dbeta: float [n], or both NULL (not wanted; then no workspace either).
+ *     mean, rstd: float [tokens, heads].
+ *   - n <= 8192, tokens * heads < 2^31 (larger: DSV_EUNSUPPORTED); eps >= 0, finite; tokens = 0: nothing is written but zeros to dgamma, dbeta.
+ *   - Everything is summed in 32 bits, the sums over rows in a fixed order: the same results from run to run. */
+typedef struct dsv_norm {
+    int32_t tokens, heads;     /* rows = tokens * heads */
+    int32_t n;                 /* elements of a row */
+    int32_t dtype;             /* dsv_dtype of X, Y, dY, dX, gamma, beta */
+    float eps;
+    uint32_t flags;            /* 0 */
+    dsv_rows x, y;             /* layouts; the forward reads these */
+    dsv_rows dy, dx;           /* the backward x, dy and dx */
+} dsv_norm;
+DSV_API dsv_status dsv_layer_norm_fwd(const dsv_norm *p, const void *X, const void *gamma, const void *beta, void *Y, float *mean,
+                                      float *rstd, void *hip_stream);
+DSV_API size_t dsv_layer_norm_bwd_workspace(const dsv_norm *p);
+DSV_API dsv_status dsv_layer_norm_bwd(const dsv_norm *p, const void *X, const void *gamma, const float *mean, const float *rstd,
+                                      const void *dY, void *dX, float *dgamma, float *dbeta, void *workspace, size_t ws_bytes,
+                                      void *hip_stream);
+
 /* ---- Optional debug check of an index tensor ---------------------------------------------------
  * Checks every row of idx against the idx contract above: values in [0, L), distinct within a row,
  * and -- when dsv_problem.flags has DSV_FLAG_SORTED_INDEX -- strictly ascending (which is what the

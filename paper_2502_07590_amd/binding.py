@@ -36,6 +36,8 @@ EXPORTED_SYMBOLS = (
     "dsv_lowrank_topk_noalloc_max_bytes", "dsv_lowrank_topk_noalloc",
     "dsv_lowrank_project", "dsv_lowrank_scores_rows",
     "dsv_kernel_timing", "dsv_kernel_ms", "dsv_threshold_search", "dsv_threshold_sample_keys", "dsv_dense_min_k", "dsv_measure_gather_ceiling",
+    "dsv_packed_attn_fwd_workspace", "dsv_packed_attn_fwd", "dsv_packed_attn_bwd_workspace", "dsv_packed_attn_bwd",
+    "dsv_layer_norm_fwd", "dsv_layer_norm_bwd_workspace", "dsv_layer_norm_bwd",
 )
 
 
@@ -52,6 +54,20 @@ class _CProblem(ctypes.Structure):
 
 class _CGrouping(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("F", "Hh", "Ww", "gf", "gh", "gw")]
+
+
+class _CRows(ctypes.Structure):
+    _fields_ = [("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class _CPacked(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seq", "total_q", "total_k", "max_q", "max_k", "Hq", "Hkv", "d", "dtype", "causal")] + \
+               [("scale", ctypes.c_float), ("flags", ctypes.c_uint32)] + [(n, _CRows) for n in ("q", "k", "v", "o", "dO", "dq", "dk", "dv")]
+
+
+class _CNorm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "heads", "n", "dtype")] + [("eps", ctypes.c_float), ("flags", ctypes.c_uint32)] + \
+               [(n, _CRows) for n in ("x", "y", "dy", "dx")]
 
 
 class Grouping:
@@ -159,6 +175,18 @@ def load_library():
     lib.dsv_kernel_timing.argtypes = [i32]
     lib.dsv_kernel_ms.restype = ctypes.c_int
     lib.dsv_kernel_ms.argtypes = [i32, ctypes.POINTER(ctypes.c_float)]
+    PP, PN = ctypes.POINTER(_CPacked), ctypes.POINTER(_CNorm)
+    for name, descriptor in (("dsv_packed_attn_fwd_workspace", PP), ("dsv_packed_attn_bwd_workspace", PP), ("dsv_layer_norm_bwd_workspace", PN)):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [descriptor]
+    lib.dsv_packed_attn_fwd.restype = ctypes.c_int
+    lib.dsv_packed_attn_fwd.argtypes = [PP] + [vp] * 8 + [vp, sz, vp]
+    lib.dsv_packed_attn_bwd.restype = ctypes.c_int
+    lib.dsv_packed_attn_bwd.argtypes = [PP] + [vp] * 12 + [vp, sz, vp]
+    lib.dsv_layer_norm_fwd.restype = ctypes.c_int
+    lib.dsv_layer_norm_fwd.argtypes = [PN] + [vp] * 6 + [vp]
+    lib.dsv_layer_norm_bwd.restype = ctypes.c_int
+    lib.dsv_layer_norm_bwd.argtypes = [PN] + [vp] * 8 + [vp, sz, vp]
     lib.dsv_measure_gather_ceiling.restype = ctypes.c_int
     lib.dsv_measure_gather_ceiling.argtypes = [i32, i32, i32, i32, i32, vp, vp, vp, vp, i32, ctypes.POINTER(ctypes.c_float), vp]
     _lib = lib
@@ -474,6 +502,182 @@ def profile_sparsity(p: Problem, Q, K, rows, mass: float = 0.9, ema=None, alpha:
     _check(lib.dsv_profile_sparsity(p.c, _ptr(Q), _ptr(K), _ptr(rows), n, float(mass), _ptr(counts), _ptr(sparsity), _ptr(ema),
                                     float(alpha), _ptr(ws), nbytes, _stream(stream)), "dsv_profile_sparsity")
     return sparsity, counts
+
+
+# ---- full attention over packed sequences, layer norm -------------------------------------------------
+class Packed:
+    """Host-side descriptor of packed sequences (mirrors struct dsv_packed; the calls fill in the layouts of their tensors)."""
+
+    def __init__(self, n_seq: int, total_q: int, total_k: int, max_q: int, max_k: int, Hq: int, Hkv: int, d: int, dtype, scale: float,
+                 causal: bool = False):
+        if isinstance(dtype, str):
+            dtype = _DTYPE_NAME[dtype]
+        self.n_seq, self.total_q, self.total_k, self.max_q, self.max_k = int(n_seq), int(total_q), int(total_k), int(max_q), int(max_k)
+        self.Hq, self.Hkv, self.d, self.scale, self.causal = int(Hq), int(Hkv), int(d), float(scale), bool(causal)
+        self.torch_dtype = dtype
+        self._c = _CPacked(self.n_seq, self.total_q, self.total_k, self.max_q, self.max_k, self.Hq, self.Hkv, self.d, _DTYPE_CODE.get(dtype, -1),
+                           int(self.causal), self.scale, 0)
+        q, k = (self.Hq * self.d, self.d), (self.Hkv * self.d, self.d)
+        for name, rows in (("q", q), ("k", k), ("v", k), ("o", q), ("dO", q), ("dq", q), ("dk", k), ("dv", k)):
+            setattr(self._c, name, rows)
+
+    @property
+    def c(self):
+        return ctypes.byref(self._c)
+
+
+class Norm:
+    """Host-side descriptor of rows to be normed (mirrors struct dsv_norm; the calls fill in the layouts of their tensors)."""
+
+    def __init__(self, tokens: int, n: int, dtype, eps: float = 1e-5, heads: int = 1):
+        if isinstance(dtype, str):
+            dtype = _DTYPE_NAME[dtype]
+        self.tokens, self.n, self.eps, self.heads = int(tokens), int(n), float(eps), int(heads)
+        self.torch_dtype = dtype
+        self._c = _CNorm(self.tokens, self.heads, self.n, _DTYPE_CODE.get(dtype, -1), self.eps, 0)
+        for name in ("x", "y", "dy", "dx"):
+            setattr(self._c, name, (self.heads * self.n, self.n))
+
+    @property
+    def c(self):
+        return ctypes.byref(self._c)
+
+
+def _rows(c, name: str, t: torch.Tensor, shape, dtype, device):
+    """Pointer of a tensor of rows [tokens, heads, n]; its strides go into the descriptor `c`."""
+    if t.device != device:
+        raise DsvError(f"libdsv takes device tensors, all on one device: {t.device} beside {device}")
+    if tuple(t.shape) != shape or t.dtype != dtype:
+        raise DsvError(f"{name}: expected {dtype} of shape {shape}, got {t.dtype} of shape {tuple(t.shape)}")
+    row, head, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        raise DsvError(f"{name}: the elements of a row must lie side by side")
+    # the stride of an axis that is never stepped along says nothing
+    setattr(c, name, (row if shape[0] > 1 else shape[1] * shape[2], head if shape[1] > 1 else shape[2]))
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _flat(what: str, t, shape, dtype, device):
+    """Pointer of a contiguous tensor, None for None."""
+    if t is None:
+        return None
+    if t.device != device or tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+        raise DsvError(f"{what}: expected contiguous {dtype} of shape {shape} on {device}, got {t.dtype} of shape {tuple(t.shape)} on {t.device}")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+class _On:
+    """The call's device and stream made current, so that what the call allocates belongs to that stream; .ptr is the stream's handle."""
+
+    def __init__(self, t: torch.Tensor, stream):
+        if not t.is_cuda:
+            raise DsvError("libdsv takes device tensors")
+        if stream is not None and stream.device != t.device:
+            raise DsvError(f"tensors on {t.device}, stream on {stream.device}")
+        self._device, self._stream, self._ctx = t.device, stream, None
+
+    def __enter__(self):
+        if self._stream is not None:
+            self._ctx = torch.cuda.stream(self._stream)
+        elif self._device.index != torch.cuda.current_device():
+            self._ctx = torch.cuda.device(self._device)
+        if self._ctx is not None:
+            self._ctx.__enter__()
+        self.ptr = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        return self
+
+    def __exit__(self, *exc):
+        if self._ctx is not None:
+            self._ctx.__exit__(*exc)
+
+
+def _scratch(nbytes: int, device, workspace):
+    """(pointer, bytes) of the caller's workspace, or of one made here, in the current stream's memory."""
+    if workspace is None:
+        if nbytes == 0:
+            return None, 0, None
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    elif workspace.device != device:
+        raise DsvError(f"workspace on {workspace.device}, tensors on {device}")
+    return _ptr(workspace), workspace.numel() * workspace.element_size(), workspace
+
+
+def packed_attn_fwd_workspace(p: Packed) -> int:
+    return int(load_library().dsv_packed_attn_fwd_workspace(p.c))
+
+
+def packed_attn_fwd(p: Packed, Q, K, V, cu_q, cu_k, O=None, lse=None, O_tail=None, workspace=None, stream=None):
+    """(O, lse) of full attention over packed sequences.  Q [total_q, Hq, d], K, V [total_k, Hkv, d]: views with any strides between
+    tokens and heads; cu_q, cu_k int32 [n_seq + 1] on the device.  O is made like Q.  O_tail (bf16 [total_q, Hq, d]): filled for the backward."""
+    lib = load_library()
+    with _On(Q, stream) as on:
+        dev, td, c = Q.device, p.torch_dtype, _CPacked.from_buffer_copy(p._c)
+        q, k = (p.total_q, p.Hq, p.d), (p.total_k, p.Hkv, p.d)
+        O = torch.empty_like(Q) if O is None else O
+        lse = torch.empty((p.Hq, p.total_q), dtype=torch.float32, device=dev) if lse is None else lse
+        args = [_rows(c, "q", Q, q, td, dev), _rows(c, "k", K, k, td, dev), _rows(c, "v", V, k, td, dev),
+                _flat("cu_q", cu_q, (p.n_seq + 1,), torch.int32, dev), _flat("cu_k", cu_k, (p.n_seq + 1,), torch.int32, dev),
+                _rows(c, "o", O, q, td, dev), _flat("O_tail", O_tail, q, td, dev), _flat("lse", lse, (p.Hq, p.total_q), torch.float32, dev)]
+        ws, nbytes, held = _scratch(int(lib.dsv_packed_attn_fwd_workspace(c)), dev, workspace)
+        _check(lib.dsv_packed_attn_fwd(c, *args, ws, nbytes, on.ptr), "dsv_packed_attn_fwd")
+    return O, lse
+
+
+def packed_attn_bwd_workspace(p: Packed) -> int:
+    return int(load_library().dsv_packed_attn_bwd_workspace(p.c))
+
+
+def packed_attn_bwd(p: Packed, Q, K, V, cu_q, cu_k, O, lse, dO, dQ=None, dK=None, dV=None, O_tail=None, workspace=None, stream=None):
+    """(dQ, dK, dV) of packed_attn_fwd; the gradients are made like Q, K and V."""
+    lib = load_library()
+    with _On(Q, stream) as on:
+        dev, td, c = Q.device, p.torch_dtype, _CPacked.from_buffer_copy(p._c)
+        q, k = (p.total_q, p.Hq, p.d), (p.total_k, p.Hkv, p.d)
+        dQ = torch.empty_like(Q) if dQ is None else dQ
+        dK = torch.empty_like(K) if dK is None else dK
+        dV = torch.empty_like(V) if dV is None else dV
+        args = [_rows(c, "q", Q, q, td, dev), _rows(c, "k", K, k, td, dev), _rows(c, "v", V, k, td, dev),
+                _flat("cu_q", cu_q, (p.n_seq + 1,), torch.int32, dev), _flat("cu_k", cu_k, (p.n_seq + 1,), torch.int32, dev),
+                _rows(c, "o", O, q, td, dev), _flat("O_tail", O_tail, q, td, dev), _flat("lse", lse, (p.Hq, p.total_q), torch.float32, dev),
+                _rows(c, "dO", dO, q, td, dev), _rows(c, "dq", dQ, q, td, dev), _rows(c, "dk", dK, k, td, dev), _rows(c, "dv", dV, k, td, dev)]
+        ws, nbytes, held = _scratch(int(lib.dsv_packed_attn_bwd_workspace(c)), dev, workspace)
+        _check(lib.dsv_packed_attn_bwd(c, *args, ws, nbytes, on.ptr), "dsv_packed_attn_bwd")
+    return dQ, dK, dV
+
+
+def layer_norm_fwd(p: Norm, X, gamma=None, beta=None, Y=None, mean=None, rstd=None, stream=None):
+    """(Y, mean, rstd): X [tokens, heads, n], any strides between tokens and heads; gamma, beta [n] or None; mean, rstd float [tokens, heads]."""
+    lib = load_library()
+    with _On(X, stream) as on:
+        dev, td, c, shape = X.device, p.torch_dtype, _CNorm.from_buffer_copy(p._c), (p.tokens, p.heads, p.n)
+        Y = torch.empty_like(X) if Y is None else Y
+        mean = torch.empty(shape[:2], dtype=torch.float32, device=dev) if mean is None else mean
+        rstd = torch.empty(shape[:2], dtype=torch.float32, device=dev) if rstd is None else rstd
+        args = [_rows(c, "x", X, shape, td, dev), _flat("gamma", gamma, (p.n,), td, dev), _flat("beta", beta, (p.n,), td, dev), _rows(c, "y", Y, shape, td, dev),
+                _flat("mean", mean, shape[:2], torch.float32, dev), _flat("rstd", rstd, shape[:2], torch.float32, dev)]
+        _check(lib.dsv_layer_norm_fwd(c, *args, on.ptr), "dsv_layer_norm_fwd")
+    return Y, mean, rstd
+
+
+def layer_norm_bwd_workspace(p: Norm) -> int:
+    return int(load_library().dsv_layer_norm_bwd_workspace(p.c))
+
+
+def layer_norm_bwd(p: Norm, X, gamma, mean, rstd, dY, dX=None, dgamma=None, dbeta=None, workspace=None, stream=None):
+    """(dX, dgamma, dbeta): dX made like X, dgamma and dbeta float [n]; both None where gamma is None and neither was passed."""
+    lib = load_library()
+    with _On(X, stream) as on:
+        dev, td, c, shape = X.device, p.torch_dtype, _CNorm.from_buffer_copy(p._c), (p.tokens, p.heads, p.n)
+        dX = torch.empty_like(X) if dX is None else dX
+        if gamma is not None or dgamma is not None or dbeta is not None:
+            dgamma = torch.empty(p.n, dtype=torch.float32, device=dev) if dgamma is None else dgamma
+            dbeta = torch.empty(p.n, dtype=torch.float32, device=dev) if dbeta is None else dbeta
+        args = [_rows(c, "x", X, shape, td, dev), _flat("gamma", gamma, (p.n,), td, dev), _flat("mean", mean, shape[:2], torch.float32, dev),
+                _flat("rstd", rstd, shape[:2], torch.float32, dev), _rows(c, "dy", dY, shape, td, dev), _rows(c, "dx", dX, shape, td, dev),
+                _flat("dgamma", dgamma, (p.n,), torch.float32, dev), _flat("dbeta", dbeta, (p.n,), torch.float32, dev)]
+        ws, nbytes, held = _scratch(int(lib.dsv_layer_norm_bwd_workspace(c)) if dgamma is not None else 0, dev, workspace)
+        _check(lib.dsv_layer_norm_bwd(c, *args, ws, nbytes, on.ptr), "dsv_layer_norm_bwd")
+    return dX, dgamma, dbeta
 
 
 def idx_validate(p: Problem, idx, workspace=None, stream=None):

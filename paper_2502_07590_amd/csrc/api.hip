@@ -2,30 +2,17 @@
 // before anything is enqueued; the library never allocates device memory.
 #include <algorithm>
 #include <cmath>
-#include <initializer_list>
 #include <mutex>
 #include <optional>
 #include <vector>
 
-#include "common.h"
+#include "checks.h"
 
 namespace dsv {
 KernelTimer g_kernel_timer;
 namespace {
 
-bool supported_d(int d) { return d == 64 || d == 128; }
 bool supported_r(int r) { return r == 16 || r == 32 || r == 64; }
-bool supported_dtype(int t) { return t == DSV_F32 || t == DSV_BF16; }
-size_t esize(int dtype) { return dtype == DSV_BF16 ? 2 : 4; }
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// true when every pointer is non-null and 16-byte aligned
-bool ok_ptrs(std::initializer_list<const void *> ps)
-{
-    for (const void *p : ps)
-        if (!p || !aligned16(p)) return false;
-    return true;
-}
 
 dsv_status check_problem(const dsv_problem *p, bool need_r)
 {
@@ -72,13 +59,6 @@ size_t total_pairs(const dsv_problem &p)
     size_t nnz = 0;
     for (int bh = 0; bh < p.B * p.H; ++bh) nnz += (size_t)p.L * p.k_per_head[bh % p.H];
     return nnz;
-}
-
-dsv_status check_workspace(const void *ws, size_t have, size_t need)
-{
-    if (need == 0) return DSV_OK;
-    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || have < need) return DSV_EWORKSPACE;
-    return DSV_OK;
 }
 
 // ---- workspace layouts (byte offsets, every block aligned to 256) ------------------------------

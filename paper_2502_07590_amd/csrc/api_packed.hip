@@ -1,0 +1,248 @@
+// C ABI of attention over packed sequences and of layer norm: argument checks, forms and workspace layout, as in api.hip.
+#include <algorithm>
+#include <cmath>
+
+#include "checks.h"
+#include "norm.h"
+#include "packed_attn.h"
+
+namespace dsv {
+namespace {
+
+// Strides of an input: whole 16 bytes.  Of an output: also no two of its rows on the same memory.
+bool ok_strides(const dsv_rows &s, size_t es)
+{
+    const int64_t unit = 16 / (int64_t)es, most = (int64_t)1 << 40;
+    return s.row >= 0 && s.head >= 0 && s.row < most && s.head < most && s.row % unit == 0 && s.head % unit == 0;
+}
+bool rows_apart(const dsv_rows &s, int64_t rows, int64_t heads, int64_t n)
+{
+    if (rows <= 1 && heads <= 1) return true;
+    if (rows <= 1) return s.head >= n;
+    if (heads <= 1) return s.row >= n;
+    return (s.head >= n && s.row >= (heads - 1) * s.head + n) || (s.row >= n && s.head >= (rows - 1) * s.row + n);
+}
+
+dsv_status check_packed(const dsv_packed *p, bool grad)
+{
+    if (!p) return DSV_EINVAL;
+    if (p->n_seq < 1 || p->total_q < 0 || p->total_k < 0 || p->max_q < 0 || p->max_k < 0) return DSV_EINVAL;
+    if (p->Hq < 1 || p->Hkv < 1 || p->Hq % p->Hkv) return DSV_EINVAL;
+    if (p->causal != 0 && p->causal != 1) return DSV_EINVAL;
+    if (p->flags || !std::isfinite(p->scale) || !(p->scale > 0.f)) return DSV_EINVAL;
+    if (!supported_dtype(p->dtype) || !supported_d(p->d)) return DSV_EUNSUPPORTED;
+    const size_t es = esize(p->dtype);
+    for (const dsv_rows *s : {&p->q, &p->k, &p->v, &p->o})
+        if (!ok_strides(*s, es)) return DSV_EINVAL;
+    if (!grad && !rows_apart(p->o, p->total_q, p->Hq, p->d)) return DSV_EINVAL;
+    if (grad) {
+        for (const dsv_rows *s : {&p->dO, &p->dq, &p->dk, &p->dv})
+            if (!ok_strides(*s, es)) return DSV_EINVAL;
+        if (!rows_apart(p->dq, p->total_q, p->Hq, p->d) || !rows_apart(p->dk, p->total_k, p->Hkv, p->d) || !rows_apart(p->dv, p->total_k, p->Hkv, p->d))
+            return DSV_EINVAL;
+    }
+    // row / group by a 32-bit reciprocal, and the blocks of a launch
+    if ((int64_t)p->total_q * p->Hq >= 1ll << 31 || (int64_t)p->total_q * p->Hq * (p->Hq / p->Hkv) >= 1ll << 32) return DSV_EUNSUPPORTED;
+    if ((int64_t)p->total_q * p->Hq / 32 + (int64_t)p->n_seq * p->Hkv >= 1 << 24) return DSV_EUNSUPPORTED;
+    if ((int64_t)p->total_k * p->Hkv / 32 + (int64_t)p->n_seq * p->Hkv >= 1 << 24) return DSV_EUNSUPPORTED;
+    return DSV_OK;
+}
+
+PackedArgs packed_args(const dsv_packed &p, const int32_t *cu_q, const int32_t *cu_k)
+{
+    const int64_t es = (int64_t)esize(p.dtype);
+    PackedArgs a{};
+    a.cu_q = cu_q;
+    a.cu_k = cu_k;
+    a.n_seq = p.n_seq;
+    a.total_q = p.total_q;
+    a.total_k = p.total_k;
+    a.max_q = p.max_q;
+    a.max_k = p.max_k;
+    a.Hq = p.Hq;
+    a.Hkv = p.Hkv;
+    a.group = p.Hq / p.Hkv;
+    a.magic = a.group > 1 ? (uint32_t)((1ull << 32) / (uint64_t)a.group) + 1u : 0u;
+    a.causal = p.causal;
+    a.scale = p.scale;
+    a.q_row = p.q.row * es, a.q_head = p.q.head * es;
+    a.k_row = p.k.row * es, a.k_head = p.k.head * es;
+    a.v_row = p.v.row * es, a.v_head = p.v.head * es;
+    a.o_row = p.o.row * es, a.o_head = p.o.head * es;
+    a.do_row = p.dO.row * es, a.do_head = p.dO.head * es;
+    a.dq_row = p.dq.row * es, a.dq_head = p.dq.head * es;
+    a.dk_row = p.dk.row * es, a.dk_head = p.dk.head * es;
+    a.dv_row = p.dv.row * es, a.dv_head = p.dv.head * es;
+    a.splits = 1;
+    return a;
+}
+
+// How a step walks: own rows (queries times the heads that share, or keys) in tiles of 128, or of 32 where those would not fill the chip or the
+// sequences are short; and the other axis in pieces where even the small tiles are few.
+struct Walk {
+    bool few;
+    int splits, chunk;
+};
+Walk plan_walk(int64_t own, int64_t heads, int64_t n_seq, int64_t other, int64_t max_other)
+{
+    constexpr int64_t kFew = 256, kWork = 512, kUnit = 128, kMinChunk = 256, kMaxSplits = 64;
+    Walk w{};
+    w.few = (own / 128 + 1) * heads < kFew || own / n_seq <= 64;
+    w.splits = 1;
+    if (!w.few) return w;
+    const int64_t tiles = own / 32 + n_seq, blocks = tiles * heads;
+    if (blocks >= 2 * kWork) return w;
+    // pieces so long that all blocks together walk about kWork of them
+    const int64_t work = (int64_t)((double)tiles / (double)n_seq * (double)other * (double)heads) / kWork;
+    const int64_t chunk = (std::max({work, kMinChunk, (max_other + kMaxSplits - 1) / kMaxSplits}) + kUnit - 1) / kUnit * kUnit;
+    if (chunk >= max_other) return w;
+    w.chunk = (int)chunk;
+    w.splits = (int)((max_other + chunk - 1) / chunk);
+    return w;
+}
+Walk walk_q(const dsv_packed &p) { return plan_walk((int64_t)p.total_q * (p.Hq / p.Hkv), p.Hkv, p.n_seq, p.total_k, std::min(p.max_k, p.total_k)); }
+Walk walk_k(const dsv_packed &p)
+{
+    const int64_t g = p.Hq / p.Hkv;
+    return plan_walk(p.total_k, p.Hkv, p.n_seq, (int64_t)p.total_q * g, std::min(p.max_q, p.total_q) * g);
+}
+
+size_t fwd_bytes(const dsv_packed &p)
+{
+    const Walk w = walk_q(p);
+    return w.splits > 1 ? packed_fwd_acc_bytes(p.total_q, p.Hq, p.d, w.splits) + align_up((size_t)p.total_q * p.Hq * w.splits * 8, 256) : 0;
+}
+size_t bwd_bytes(const dsv_packed &p)
+{
+    return packed_stat_bytes(p.total_q, p.Hq) +
+           std::max(packed_dq_bytes(p.total_q, p.Hq, p.d, walk_q(p).splits), packed_dkdv_bytes(p.total_k, p.Hkv, p.d, walk_k(p).splits));
+}
+
+dsv_status check_norm(const dsv_norm *p, bool grad)
+{
+    if (!p) return DSV_EINVAL;
+    if (p->tokens < 0 || p->heads < 1 || p->n < 1 || p->flags || !std::isfinite(p->eps) || !(p->eps >= 0.f)) return DSV_EINVAL;
+    if (!supported_dtype(p->dtype) || p->n > kMaxNormWidth || (int64_t)p->tokens * p->heads >= 1ll << 31) return DSV_EUNSUPPORTED;
+    const int64_t most = (int64_t)1 << 40;
+    for (const dsv_rows *s : {&p->x, grad ? &p->dy : &p->y, grad ? &p->dx : &p->y})
+        if (s->row < 0 || s->head < 0 || s->row >= most || s->head >= most) return DSV_EINVAL;
+    if (!rows_apart(grad ? p->dx : p->y, p->tokens, p->heads, p->n)) return DSV_EINVAL;
+    return DSV_OK;
+}
+NormArgs norm_args(const dsv_norm &p)
+{
+    return NormArgs{p.tokens, p.heads, p.n, p.eps, p.x.row, p.x.head, p.y.row, p.y.head, p.dy.row, p.dy.head, p.dx.row, p.dx.head};
+}
+// every pointer on an element
+bool on_elements(std::initializer_list<const void *> ps, size_t es)
+{
+    for (const void *q : ps)
+        if (reinterpret_cast<uintptr_t>(q) % es) return false;
+    return true;
+}
+bool wide_rows(const dsv_norm &p, std::initializer_list<const void *> ps, std::initializer_list<dsv_rows> strides)
+{
+    const int64_t unit = 16 / (int64_t)esize(p.dtype);
+    if (p.n % unit) return false;
+    for (const void *q : ps)
+        if (!aligned16(q)) return false;
+    for (const dsv_rows &s : strides)
+        if (s.row % unit || s.head % unit) return false;
+    return true;
+}
+}  // namespace
+}  // namespace dsv
+
+using namespace dsv;
+
+extern "C" {
+
+size_t dsv_packed_attn_fwd_workspace(const dsv_packed *p)
+{
+    if (check_packed(p, false) != DSV_OK) return 0;
+    return fwd_bytes(*p);
+}
+
+dsv_status dsv_packed_attn_fwd(const dsv_packed *p, const void *Q, const void *K, const void *V, const int32_t *cu_q, const int32_t *cu_k, void *O,
+                               void *O_tail, float *lse, void *workspace, size_t ws_bytes, void *hip_stream)
+{
+    dsv_status st = check_packed(p, false);
+    if (st != DSV_OK) return st;
+    if (!cu_q || !cu_k || !on_elements({cu_q, cu_k, lse}, 4)) return DSV_EINVAL;
+    if (p->total_q > 0 && (!ok_ptrs({Q, O}) || !lse)) return DSV_EINVAL;
+    if (p->total_k > 0 && !ok_ptrs({K, V})) return DSV_EINVAL;
+    if (O_tail && (p->dtype != DSV_BF16 || !aligned16(O_tail))) return DSV_EINVAL;
+    st = check_workspace(workspace, ws_bytes, fwd_bytes(*p));
+    if (st != DSV_OK) return st;
+    if (p->total_q == 0) return DSV_OK;
+    const Walk w = walk_q(*p);
+    PackedArgs a = packed_args(*p, cu_q, cu_k);
+    a.splits = w.splits;
+    a.chunk = w.chunk;
+    return launch_packed_fwd(a, p->dtype, p->d, w.few, Q, K, V, O, O_tail, lse, static_cast<char *>(workspace), static_cast<hipStream_t>(hip_stream));
+}
+
+size_t dsv_packed_attn_bwd_workspace(const dsv_packed *p)
+{
+    if (check_packed(p, true) != DSV_OK) return 0;
+    return bwd_bytes(*p);
+}
+
+dsv_status dsv_packed_attn_bwd(const dsv_packed *p, const void *Q, const void *K, const void *V, const int32_t *cu_q, const int32_t *cu_k, const void *O,
+                               const void *O_tail, const float *lse, const void *dO, void *dQ, void *dK, void *dV, void *workspace, size_t ws_bytes,
+                               void *hip_stream)
+{
+    dsv_status st = check_packed(p, true);
+    if (st != DSV_OK) return st;
+    if (!cu_q || !cu_k || !on_elements({cu_q, cu_k, lse}, 4)) return DSV_EINVAL;
+    if (p->total_q > 0 && (!ok_ptrs({Q, O, dO, dQ}) || !lse)) return DSV_EINVAL;
+    if (p->total_k > 0 && !ok_ptrs({K, V, dK, dV})) return DSV_EINVAL;
+    if (O_tail && (p->dtype != DSV_BF16 || !aligned16(O_tail))) return DSV_EINVAL;
+    st = check_workspace(workspace, ws_bytes, bwd_bytes(*p));
+    if (st != DSV_OK) return st;
+    const Walk q = walk_q(*p), k = walk_k(*p);
+    const PackedBwdPlan plan{q.few, k.few, q.splits, q.chunk, k.splits, k.chunk};
+    return launch_packed_bwd(packed_args(*p, cu_q, cu_k), plan, p->dtype, p->d, Q, K, V, O, O_tail, lse, dO, dQ, dK, dV, static_cast<char *>(workspace),
+                             static_cast<hipStream_t>(hip_stream));
+}
+
+dsv_status dsv_layer_norm_fwd(const dsv_norm *p, const void *X, const void *gamma, const void *beta, void *Y, float *mean, float *rstd, void *hip_stream)
+{
+    dsv_status st = check_norm(p, false);
+    if (st != DSV_OK) return st;
+    if (p->tokens > 0 && (!X || !Y || !mean || !rstd)) return DSV_EINVAL;
+    if (!on_elements({X, gamma, beta, Y}, esize(p->dtype)) || !on_elements({mean, rstd}, 4)) return DSV_EINVAL;
+    if (p->tokens == 0) return DSV_OK;
+    const bool wide = wide_rows(*p, {X, gamma, beta, Y}, {p->x, p->y});
+    return launch_norm_fwd(norm_args(*p), p->dtype, wide, X, gamma, beta, Y, mean, rstd, static_cast<hipStream_t>(hip_stream));
+}
+
+// the pointers do not enter: as many blocks as rows of either alignment may take
+static size_t norm_bwd_bytes(const dsv_norm &p)
+{
+    const NormArgs a = norm_args(p);
+    return align_up((size_t)std::max(norm_bwd_blocks(a, p.dtype, false), norm_bwd_blocks(a, p.dtype, true)) * 2 * p.n * 4, 256);
+}
+
+size_t dsv_layer_norm_bwd_workspace(const dsv_norm *p)
+{
+    if (check_norm(p, true) != DSV_OK) return 0;
+    return norm_bwd_bytes(*p);
+}
+
+dsv_status dsv_layer_norm_bwd(const dsv_norm *p, const void *X, const void *gamma, const float *mean, const float *rstd, const void *dY, void *dX,
+                              float *dgamma, float *dbeta, void *workspace, size_t ws_bytes, void *hip_stream)
+{
+    dsv_status st = check_norm(p, true);
+    if (st != DSV_OK) return st;
+    if (p->tokens > 0 && (!X || !mean || !rstd || !dY || !dX)) return DSV_EINVAL;
+    if (!dgamma != !dbeta) return DSV_EINVAL;
+    if (!on_elements({X, gamma, dY, dX}, esize(p->dtype)) || !on_elements({mean, rstd, dgamma, dbeta}, 4)) return DSV_EINVAL;
+    st = check_workspace(workspace, ws_bytes, dgamma ? norm_bwd_bytes(*p) : 0);
+    if (st != DSV_OK) return st;
+    const bool wide = wide_rows(*p, {X, gamma, dY, dX}, {p->x, p->dy, p->dx});
+    return launch_norm_bwd(norm_args(*p), p->dtype, wide, X, gamma, mean, rstd, dY, dX, dgamma, dbeta, dgamma ? static_cast<float *>(workspace) : nullptr,
+                           static_cast<hipStream_t>(hip_stream));
+}
+
+}  // extern "C"

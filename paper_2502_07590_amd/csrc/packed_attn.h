@@ -1,0 +1,228 @@
+// Attention over packed sequences: what its kernels share (packed_fwd.hip, packed_bwd.hip).
+//
+// Sequence i holds query tokens cu_q[i] .. cu_q[i+1] - 1 and key tokens cu_k[i] .. cu_k[i+1] - 1.  The `group` query heads that read one
+// K/V head are rows of the same tile: row = query * group + head of the group.  A single query of a decoding step then still gives a tile
+// `group` rows, and the key-major sums of the backward run over the shared heads by themselves.
+#pragma once
+
+#include "stage2_core.h"
+
+namespace dsv {
+
+constexpr float kNegInf = -__builtin_inff();
+
+// A descriptor as the kernels read it; strides in bytes.
+struct PackedArgs {
+    const int32_t *cu_q, *cu_k;
+    int32_t n_seq, total_q, total_k, max_q, max_k, Hq, Hkv, group;
+    uint32_t magic;   // row / group = umulhi(row, magic) for group > 1: magic = floor(2^32 / group) + 1, rows below 2^32 / group
+    int32_t causal;
+    float scale;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
+    int64_t do_row, do_head, dq_row, dq_head, dk_row, dk_head, dv_row, dv_head;
+    int32_t splits, chunk;  // the long axis in `splits` pieces of `chunk` rows (0: in one)
+};
+
+__device__ __forceinline__ int row_token(const PackedArgs &a, int row) { return a.group == 1 ? row : (int)__umulhi((uint32_t)row, a.magic); }
+
+// One sequence, its ends forced into the tensors: nothing an entry of cu_q or cu_k can say leads out of them.
+struct Sequence {
+    int q0, k0, nq, nk;
+};
+__device__ __forceinline__ Sequence read_sequence(const PackedArgs &a, int i)
+{
+    Sequence s;
+    s.q0 = min(max(a.cu_q[i], 0), a.total_q);
+    s.k0 = min(max(a.cu_k[i], 0), a.total_k);
+    s.nq = min(min(max(a.cu_q[i + 1], s.q0), a.total_q) - s.q0, a.max_q);
+    s.nk = min(min(max(a.cu_k[i + 1], s.k0), a.total_k) - s.k0, a.max_k);
+    return s;
+}
+
+// Tiles of ROWS rows are numbered without a sum over the sequences before: sequence i's begin at floor(cu[i] * mul / ROWS) + i, which leaves
+// ceil(length / ROWS) places at least.  The owner of a place is the last sequence that begins at or before it; 64 candidates a step.
+// ROWS = 0: the tokens themselves, no place left empty (the owner of a token).
+__device__ __forceinline__ int first_slot(int cu, int total, int mul, int rows, int i)
+{
+    const int at = min(max(cu, 0), total) * mul;
+    return rows ? (int)((uint32_t)at / (uint32_t)rows) + i : at;
+}
+__device__ __forceinline__ int find_sequence(const int32_t *__restrict__ cu, int n_seq, int total, int mul, int rows, int slot)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = n_seq;  // lo begins at or before the slot, hi after it
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) >> 6, at = lo + (lane + 1) * step;
+        const bool before = at < hi && first_slot(cu[at], total, mul, rows, at) <= slot;
+        lo += __popcll(__ballot(before)) * step;
+        hi = min(hi, lo + step);
+    }
+    return lo;
+}
+__host__ __device__ __forceinline__ int64_t tile_slots(int64_t total, int mul, int rows, int n_seq) { return total * mul / rows + n_seq; }
+
+// A tile of rows in LDS, row after row.  Piece p (16 bytes) of row r lies at place p ^ turn(r) of the row: eight consecutive rows have
+// their p-th pieces, and four consecutive rows their p-th pairs of pieces, in different banks -- the two ways matrix operands are read,
+// 16 bytes of 32 rows or transposing from four rows at a time.
+template <typename T, int D> struct RowTile {
+    static constexpr int RB = D * (int)sizeof(T), PIECES = RB / 16;
+    __device__ __forceinline__ static int turn(int r) { return (((r & 3) << 1) | ((r >> 2) & 1) | (r & 8)) & (PIECES - 1); }
+    __device__ __forceinline__ static int at(int r, int p) { return r * RB + ((p ^ turn(r)) << 4); }
+
+    // ROWS rows into LDS by direct loads, a kilobyte an instruction, shared among WAVES waves; row(r) is the address of row r.
+    template <int ROWS, int WAVES, typename F> __device__ __forceinline__ static void load(unsigned char *lds, int wave, F row)
+    {
+        constexpr int N = ROWS * RB / 1024, RPC = 1024 / RB;
+        static_assert(N % WAVES == 0, "every kilobyte has its wave");
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < N / WAVES; ++i) {
+            const int c = i * WAVES + wave, r = c * RPC + lane / PIECES;
+            const unsigned char *src = row(r) + (((lane % PIECES) ^ turn(r)) << 4);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
+                                             (__attribute__((address_space(3))) void *)(lds + c * 1024), 16, 0, 0);
+        }
+    }
+};
+
+// Operands of the products.  Every product is one of 32 x 32 with the tile's rows (or channels) as A and the wave's own 32 rows as B; a
+// lane holds column lane % 32 and, of each eight rows, the four of its half: rows 8 (i / 4) + 4 (lane / 32) + i % 4.
+template <typename T> struct Frag;
+template <> struct Frag<bf16_t> { bf16x8_t v; };
+template <> struct Frag<float> { floatx4_t v; };
+
+__device__ __forceinline__ floatx16_t product(const Frag<bf16_t> &a, const Frag<bf16_t> &b, const floatx16_t &c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+// 16 bytes are four channels: half 0 brings channels 0 .. 3 of eight, half 1 channels 4 .. 7; step i contracts over channels i and 4 + i
+__device__ __forceinline__ floatx16_t product(const Frag<float> &a, const Frag<float> &b, floatx16_t c)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[i], b.v[i], c, 0, 0, 0);
+    return c;
+}
+
+__device__ __forceinline__ floatx16_t zero16()
+{
+    floatx16_t z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    return z;
+}
+
+// Pieces 2 m + half of row r, m = 0 .. NM - 1
+template <typename T, int D> __device__ __forceinline__ Frag<T> row_frag(const unsigned char *tile, int r, int m, int half)
+{
+    return *reinterpret_cast<const Frag<T> *>(tile + RowTile<T, D>::at(r, 2 * m + half));
+}
+
+// acc[nb] (channels 32 nb .. + 31 by own rows) += sum over the 32 tile rows of row[channel] * w; w: a result of a product with the tile rows
+// as A.  bf16: 16 rows a step, weights rounded to bf16 (half a step of 2^-8 each, of one sign as often as the other; the sums are in 32 bits).
+template <int D> __device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const floatx16_t &w, floatx16_t (&acc)[D / 32], const bf16_t *)
+{
+    typedef RowTile<bf16_t, D> RT;
+    const int lane = threadIdx.x & 63, half = lane >> 5, e = (lane >> 2) & 3, q = lane & 3, b4 = (lane >> 4) & 1;
+    const int r = r0 + 4 * half + e;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        Frag<bf16_t> b;
+        b.v = __builtin_bit_cast(bf16x8_t, make_uint4(pack_bf16x2(w[8 * s], w[8 * s + 1]), pack_bf16x2(w[8 * s + 2], w[8 * s + 3]),
+                                                      pack_bf16x2(w[8 * s + 4], w[8 * s + 5]), pack_bf16x2(w[8 * s + 6], w[8 * s + 7])));
+#pragma unroll
+        for (int nb = 0; nb < D / 32; ++nb) {
+            const int p = 4 * nb + 2 * b4 + (q >> 1), sub = (q & 1) * 8;
+            Frag<bf16_t> a;
+            a.v = tr_frag(tile + RT::at(r + 16 * s, p) + sub, tile + RT::at(r + 16 * s + 8, p) + sub);
+            acc[nb] = product(a, b, acc[nb]);
+        }
+    }
+}
+template <int D> __device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const floatx16_t &w, floatx16_t (&acc)[D / 32], const float *)
+{
+    typedef RowTile<float, D> RT;
+    const int lane = threadIdx.x & 63, half = lane >> 5, n = lane & 31;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int r = r0 + 8 * (i >> 2) + 4 * half + (i & 3);
+#pragma unroll
+        for (int nb = 0; nb < D / 32; ++nb) {
+            const float v = *reinterpret_cast<const float *>(tile + RT::at(r, 8 * nb + (n >> 2)) + (n & 3) * 4);
+            acc[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w[i], acc[nb], 0, 0, 0);
+        }
+    }
+}
+
+// Value of the other half's lane with the same column, combined by max or sum.
+__device__ __forceinline__ float halves_max(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// four channels of a row
+__device__ __forceinline__ void store4(bf16_t *p, float a, float b, float c, float d)
+{
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
+}
+__device__ __forceinline__ void store4(float *p, float a, float b, float c, float d) { *reinterpret_cast<float4 *>(p) = make_float4(a, b, c, d); }
+
+// O rounded to its type, and what the rounding took (the backward's Delta = dO . O wants more than 8 bits of O: with O alone, queries that see
+// few keys get gradients 5e-3 off, with the tail 2.5e-3, the rounding of weights and results).
+__device__ __forceinline__ void store_out(bf16_t *p, bf16_t *tail, float a, float b, float c, float d)
+{
+    const uint32_t w0 = pack_bf16x2(a, b), w1 = pack_bf16x2(c, d);
+    *reinterpret_cast<uint2 *>(p) = make_uint2(w0, w1);
+    if (tail)
+        *reinterpret_cast<uint2 *>(tail) = make_uint2(pack_bf16x2(a - __uint_as_float(w0 << 16), b - __uint_as_float(w0 & 0xFFFF0000u)),
+                                                      pack_bf16x2(c - __uint_as_float(w1 << 16), d - __uint_as_float(w1 & 0xFFFF0000u)));
+}
+__device__ __forceinline__ void store_out(float *p, bf16_t *, float a, float b, float c, float d) { store4(p, a, b, c, d); }
+
+// Kernels that join pieces: a wave takes 64 / LPR heads of one token, LPR lanes each.  False behind the last token (whole waves); heads past the
+// last one are the caller's to leave out.
+template <int LPR> __device__ __forceinline__ bool merge_row(int total, int heads, int &tok, int &head)
+{
+    constexpr int HPW = 64 / LPR;
+    const int per = (heads + HPW - 1) / HPW;
+    const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    tok = (int)(w / per);
+    head = (int)(w - (int64_t)tok * per) * HPW + (threadIdx.x & 63) / LPR;
+    return tok < total;
+}
+template <int LPR> __host__ __forceinline__ unsigned merge_blocks(int64_t total, int heads)
+{
+    constexpr int HPW = 64 / LPR;
+    return (unsigned)((total * ((heads + HPW - 1) / HPW) + 3) / 4);
+}
+
+__device__ __forceinline__ void wait_loads_and_sync()
+{
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): a barrier alone does not wait for loads into LDS
+    __syncthreads();
+}
+
+// Bytes of the unnormalised sums of a forward in pieces; behind them, two floats a row and piece.
+inline size_t packed_fwd_acc_bytes(int64_t total_q, int Hq, int d, int splits) { return splits > 1 ? align_up((size_t)total_q * Hq * splits * d * 4, 256) : 0; }
+// few: tiles of 32 rows whose four waves share the long axis, else 128 rows, 32 a wave
+dsv_status launch_packed_fwd(const PackedArgs &a, int dtype, int d, bool few, const void *Q, const void *K, const void *V, void *O, void *O_tail,
+                             float *lse, char *ws, hipStream_t st);
+
+// The backward's scratch: statistics of every row, and the pieces of dQ or of dK and dV.
+struct PackedBwdPlan {
+    bool few_q, few_k;        // tiles of 32 rows in the dq step, of 32 keys in the dkdv step
+    int splits_q, chunk_q;    // keys of the dq step in pieces
+    int splits_k, chunk_k;    // rows of the dkdv step in pieces
+};
+inline size_t packed_stat_bytes(int64_t total_q, int Hq) { return align_up((size_t)total_q * Hq * 8, 256); }
+inline size_t packed_dq_bytes(int64_t total_q, int Hq, int d, int splits) { return splits > 1 ? align_up((size_t)total_q * Hq * splits * d * 4, 256) : 0; }
+inline size_t packed_dkdv_bytes(int64_t total_k, int Hkv, int d, int splits) { return splits > 1 ? 2 * align_up((size_t)total_k * Hkv * splits * d * 4, 256) : 0; }
+dsv_status launch_packed_bwd(const PackedArgs &a, const PackedBwdPlan &plan, int dtype, int d, const void *Q, const void *K, const void *V, const void *O,
+                             const void *O_tail, const float *lse, const void *dO, void *dQ, void *dK, void *dV, char *ws, hipStream_t st);
+
+}  // namespace dsv

@@ -1,0 +1,408 @@
+// Softmax attention over packed sequences, backward.
+//
+//   p_ij = exp(s_ij - lse_i);  Delta_i = dO_i . O_i;  dS_ij = p_ij (dO_i . v_j - Delta_i)
+//   dQ_i = scale sum_j dS_ij k_j;   dK_j = scale sum_i dS_ij q_i;   dV_j = sum_i p_ij dO_i   (i over the queries of every head that reads j's)
+//
+// Three kernels: the rows' statistics; dQ with a wave's 32 rows as columns against tiles of keys, as in the forward; dK and dV with a wave's 32
+// keys as columns against tiles of rows.  Scores and dP are formed in both, seven products where five would do, so that every sum has
+// one owner: no atomics, the same bits from run to run.
+#include "packed_attn.h"
+
+namespace dsv {
+namespace {
+
+template <typename T, int D> __device__ __forceinline__ float dot16(const T *a, const T *b)  // 16 bytes of each
+{
+    constexpr int CH = 16 / sizeof(T);
+    return dot_chunk<T, CH>(load_chunk<T, CH>(a), load_chunk<T, CH>(b));
+}
+
+// stat[hk][token * group + head of the group] = {lse * log2(e), Delta}; rows that saw no key: {inf, 0}, weights of zero
+template <typename T, int D>
+__global__ __launch_bounds__(256) void packed_stat_kernel(const T *__restrict__ O, const T *__restrict__ tail, const T *__restrict__ dO, const float *__restrict__ lse,
+                                                          float2 *__restrict__ stat, PackedArgs a)
+{
+    constexpr int LPR = D * (int)sizeof(T) / 16, CH = 16 / (int)sizeof(T);
+    int tok, head;
+    if (!merge_row<LPR>(a.total_q, a.Hq, tok, head)) return;
+    const int lane = threadIdx.x % LPR;
+    const int hc = min(head, a.Hq - 1);
+    const T *go = reinterpret_cast<const T *>(reinterpret_cast<const unsigned char *>(dO) + (int64_t)tok * a.do_row + (int64_t)hc * a.do_head) + lane * CH;
+    const T *o = reinterpret_cast<const T *>(reinterpret_cast<const unsigned char *>(O) + (int64_t)tok * a.o_row + (int64_t)hc * a.o_head) + lane * CH;
+    float x = dot16<T, D>(go, o);
+    if (tail) x += dot16<T, D>(go, tail + ((int64_t)tok * a.Hq + hc) * D + lane * CH);
+#pragma unroll
+    for (int s = LPR / 2; s > 0; s >>= 1) x += __shfl_xor(x, s);
+    if (lane || head >= a.Hq) return;
+    const float l = lse[(int64_t)head * a.total_q + tok];
+    const int hk = head / a.group;
+    stat[(int64_t)hk * a.total_q * a.group + (int64_t)tok * a.group + (head - hk * a.group)] =
+        l == kNegInf ? make_float2(-kNegInf, 0.f) : make_float2(l * kLog2e, x);
+}
+
+template <typename T, int D, int WK> struct BwdShape {
+    static constexpr int OWN = WK == 1 ? 128 : 32, ROWS = WK == 1 ? 64 : 128, RT = ROWS / 32 / WK;  // own rows, rows of a tile, 32s of them a wave
+    static constexpr int TILE = ROWS * D * (int)sizeof(T);
+    static constexpr int NBUF = 2 * 2 * TILE <= 128 * 1024 ? 2 : 1;
+    static constexpr int LDS = NBUF * 2 * TILE;
+};
+
+// The four waves' sums of the same 32 rows, joined in LDS: thread t's share is channels 4 g .. 4 g + 3 of row t % 32 for g = t / 32, + 8, ...
+template <int D, typename F> __device__ __forceinline__ void join_waves(float *sa, const floatx16_t (&acc)[D / 32], int wave, F put)
+{
+    const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
+    __syncthreads();
+#pragma unroll
+    for (int nb = 0; nb < D / 32; ++nb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<float4 *>(sa + ((wave * (D / 4) + nb * 8 + 2 * g + half) * 32 + n) * 4) =
+                make_float4(acc[nb][4 * g], acc[nb][4 * g + 1], acc[nb][4 * g + 2], acc[nb][4 * g + 3]);
+    __syncthreads();
+    for (int g = wave * 2 + half; g < D / 4; g += 8) {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float4 x = *reinterpret_cast<const float4 *>(sa + ((w * (D / 4) + g) * 32 + n) * 4);
+            v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+        }
+        put(4 * g, v[0], v[1], v[2], v[3]);
+    }
+}
+
+template <typename T, int D, int WK>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed_dq_kernel(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V,
+                                                                                       const T *__restrict__ dO, const float2 *__restrict__ stat,
+                                                                                       T *__restrict__ dQ, float *__restrict__ part, PackedArgs a)
+{
+    typedef RowTile<T, D> RT;
+    typedef BwdShape<T, D, WK> Sh;
+    constexpr int NM = RT::RB / 32, NB = D / 32;
+    __shared__ __align__(1024) unsigned char lds[Sh::LDS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, half = lane >> 5;
+    const int hk = blockIdx.x % a.Hkv, place = blockIdx.x / a.Hkv, split = blockIdx.y;
+    const int slot = a.causal ? (int)(gridDim.x / a.Hkv) - 1 - place : place;
+    const int si = __builtin_amdgcn_readfirstlane(find_sequence(a.cu_q, a.n_seq, a.total_q, a.group, Sh::OWN, slot));
+    const Sequence sq = read_sequence(a, si);
+    const int rows = sq.nq * a.group;
+    const int row0 = (slot - first_slot(a.cu_q[si], a.total_q, a.group, Sh::OWN, si)) * Sh::OWN;
+    if (row0 < 0 || row0 >= rows) return;
+    const int row = row0 + (WK == 1 ? wave * 32 : 0) + n;
+    const int rc = min(row, rows - 1), tok = row_token(a, rc), head = hk * a.group + (rc - tok * a.group);
+    const int kbeg = split * a.chunk, kcut = a.chunk ? min(sq.nk, kbeg + a.chunk) : sq.nk;
+    const int past = sq.nk - sq.nq, seen = a.causal ? min(sq.nk, tok + past + 1) : sq.nk;
+    int kend = kcut;
+    if (a.causal) kend = min(kend, row_token(a, min(row0 + Sh::OWN, rows) - 1) + past + 1);
+    if (a.chunk && kbeg >= sq.nk && split > 0) return;  // no such piece of this sequence
+
+    Frag<T> qf[NM], gf[NM];
+    {
+        const unsigned char *qp = reinterpret_cast<const unsigned char *>(Q) + (int64_t)(sq.q0 + tok) * a.q_row + (int64_t)head * a.q_head;
+        const unsigned char *gp = reinterpret_cast<const unsigned char *>(dO) + (int64_t)(sq.q0 + tok) * a.do_row + (int64_t)head * a.do_head;
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+            qf[m] = *reinterpret_cast<const Frag<T> *>(qp + (2 * m + half) * 16);
+            gf[m] = *reinterpret_cast<const Frag<T> *>(gp + (2 * m + half) * 16);
+        }
+    }
+    const float2 rs = stat[(int64_t)hk * a.total_q * a.group + (int64_t)sq.q0 * a.group + rc];
+    const unsigned char *kp = reinterpret_cast<const unsigned char *>(K) + (int64_t)sq.k0 * a.k_row + (int64_t)hk * a.k_head;
+    const unsigned char *vp = reinterpret_cast<const unsigned char *>(V) + (int64_t)sq.k0 * a.v_row + (int64_t)hk * a.v_head;
+    auto request = [&](int k0, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
+        RT::template load<Sh::ROWS, 4>(kt, wave, [&](int r) { return kp + (int64_t)min(k0 + r, sq.nk - 1) * a.k_row; });
+        RT::template load<Sh::ROWS, 4>(vt, wave, [&](int r) { return vp + (int64_t)min(k0 + r, sq.nk - 1) * a.v_row; });
+    };
+    const float c = a.scale * kLog2e;
+    floatx16_t acc[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) acc[nb] = zero16();
+    auto tile = [&](int k0, const unsigned char *kt, const unsigned char *vt) __attribute__((always_inline)) {
+        const bool edge = k0 + Sh::ROWS > kcut || (a.causal && k0 + Sh::ROWS > row_token(a, row0) + past + 1);
+#pragma unroll
+        for (int t = 0; t < Sh::RT; ++t) {
+            const int sub = (WK == 1 ? 0 : wave * 32) + 32 * t;
+            floatx16_t s = zero16(), dp = zero16();
+#pragma unroll
+            for (int m = 0; m < NM; ++m) {
+                s = product(row_frag<T, D>(kt, sub + n, m, half), qf[m], s);
+                dp = product(row_frag<T, D>(vt, sub + n, m, half), gf[m], dp);
+            }
+            if (edge) {
+                const int lim = min(seen, kcut) - k0 - sub - 4 * half;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) < lim ? s[i] : kNegInf;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = fast_exp2(fmaf(s[i], c, -rs.x)) * (dp[i] - rs.y);
+            weighted_rows<D>(kt, sub, s, acc, (const T *)nullptr);
+        }
+    };
+    if (kbeg < kend) {
+        if constexpr (Sh::NBUF == 2) {
+            unsigned char *const ka = lds, *const va = lds + Sh::TILE, *const kb = lds + 2 * Sh::TILE, *const vb = lds + 3 * Sh::TILE;
+            request(kbeg, ka, va);
+            for (int k0 = kbeg; k0 < kend; k0 += 2 * Sh::ROWS) {
+                wait_loads_and_sync();
+                if (k0 + Sh::ROWS < kend) request(k0 + Sh::ROWS, kb, vb);
+                tile(k0, ka, va);
+                if (k0 + Sh::ROWS >= kend) break;
+                wait_loads_and_sync();
+                if (k0 + 2 * Sh::ROWS < kend) request(k0 + 2 * Sh::ROWS, ka, va);
+                tile(k0 + Sh::ROWS, kb, vb);
+            }
+        } else {
+            for (int k0 = kbeg; k0 < kend; k0 += Sh::ROWS) {
+                __syncthreads();
+                request(k0, lds, lds + Sh::TILE);
+                wait_loads_and_sync();
+                tile(k0, lds, lds + Sh::TILE);
+            }
+        }
+    }
+    T *const op = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(dQ) + (int64_t)(sq.q0 + tok) * a.dq_row + (int64_t)head * a.dq_head);
+    float *const pp = part + (((int64_t)(sq.q0 + tok) * a.Hq + head) * a.splits + split) * D;
+    auto put = [&](int ch, float x, float y, float z, float w) __attribute__((always_inline)) {
+        if (row >= rows) return;
+        if (a.splits > 1) store4(pp + ch, x * a.scale, y * a.scale, z * a.scale, w * a.scale);
+        else store4(op + ch, x * a.scale, y * a.scale, z * a.scale, w * a.scale);
+    };
+    if constexpr (WK > 1) {
+        join_waves<D>(reinterpret_cast<float *>(lds), acc, wave, put);
+    } else {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) put(32 * nb + 8 * g + 4 * half, acc[nb][4 * g], acc[nb][4 * g + 1], acc[nb][4 * g + 2], acc[nb][4 * g + 3]);
+    }
+}
+
+template <typename T, int D, int WK>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 && D == 64 ? 2 : 1) void packed_dkdv_kernel(
+    const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V, const T *__restrict__ dO, const float2 *__restrict__ stat, T *__restrict__ dK,
+    T *__restrict__ dV, float *__restrict__ part_k, float *__restrict__ part_v, PackedArgs a)
+{
+    typedef RowTile<T, D> RT;
+    typedef BwdShape<T, D, WK> Sh;
+    constexpr int NM = RT::RB / 32, NB = D / 32;
+    __shared__ __align__(1024) unsigned char lds[Sh::LDS];
+    __shared__ __align__(16) float st[Sh::NBUF][2][Sh::ROWS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, half = lane >> 5;
+    const int hk = blockIdx.x % a.Hkv, slot = blockIdx.x / a.Hkv, split = blockIdx.y;
+    const int si = __builtin_amdgcn_readfirstlane(find_sequence(a.cu_k, a.n_seq, a.total_k, 1, Sh::OWN, slot));
+    const Sequence sq = read_sequence(a, si);
+    const int key0 = (slot - first_slot(a.cu_k[si], a.total_k, 1, Sh::OWN, si)) * Sh::OWN;
+    if (key0 < 0 || key0 >= sq.nk) return;
+    const int rows = sq.nq * a.group, past = sq.nk - sq.nq;
+    const int key = key0 + (WK == 1 ? wave * 32 : 0) + n, kc = min(key, sq.nk - 1);
+    int rbeg = split * a.chunk;
+    const int rend = a.chunk ? min(rows, rbeg + a.chunk) : rows;
+    if (a.chunk && rbeg >= rows && split > 0) return;  // no such piece of this sequence
+    if (a.causal) rbeg = max(rbeg, max(0, key0 - past) * a.group / Sh::ROWS * Sh::ROWS);  // rows before see none of these keys
+
+    Frag<T> kf[NM], vf[NM];
+    {
+        const unsigned char *kp = reinterpret_cast<const unsigned char *>(K) + (int64_t)(sq.k0 + kc) * a.k_row + (int64_t)hk * a.k_head;
+        const unsigned char *vp = reinterpret_cast<const unsigned char *>(V) + (int64_t)(sq.k0 + kc) * a.v_row + (int64_t)hk * a.v_head;
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+            kf[m] = *reinterpret_cast<const Frag<T> *>(kp + (2 * m + half) * 16);
+            vf[m] = *reinterpret_cast<const Frag<T> *>(vp + (2 * m + half) * 16);
+        }
+    }
+    const unsigned char *qp = reinterpret_cast<const unsigned char *>(Q) + (int64_t)sq.q0 * a.q_row + (int64_t)hk * a.group * a.q_head;
+    const unsigned char *gp = reinterpret_cast<const unsigned char *>(dO) + (int64_t)sq.q0 * a.do_row + (int64_t)hk * a.group * a.do_head;
+    const float2 *const sp = stat + (int64_t)hk * a.total_q * a.group + (int64_t)sq.q0 * a.group;
+    float2 sn = make_float2(-kNegInf, 0.f);
+    auto request = [&](int r0, unsigned char *qt, unsigned char *gt) __attribute__((always_inline)) {
+        auto place = [&](int r, int64_t row_b, int64_t head_b) {
+            const int rho = min(r0 + r, rows - 1), tok = row_token(a, rho);
+            return (int64_t)tok * row_b + (int64_t)(rho - tok * a.group) * head_b;
+        };
+        RT::template load<Sh::ROWS, 4>(qt, wave, [&](int r) { return qp + place(r, a.q_row, a.q_head); });
+        RT::template load<Sh::ROWS, 4>(gt, wave, [&](int r) { return gp + place(r, a.do_row, a.do_head); });
+        if ((int)threadIdx.x < Sh::ROWS) sn = r0 + (int)threadIdx.x < rend ? sp[r0 + threadIdx.x] : make_float2(-kNegInf, 0.f);  // rows past the end: weights of zero
+    };
+    auto park = [&](int b) __attribute__((always_inline)) {
+        if ((int)threadIdx.x < Sh::ROWS) {
+            st[b][0][threadIdx.x] = sn.x;
+            st[b][1][threadIdx.x] = sn.y;
+        }
+    };
+    const float c = a.scale * kLog2e;
+    floatx16_t dk[NB], dv[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) dk[nb] = dv[nb] = zero16();
+    auto tile = [&](int r0, const unsigned char *qt, const unsigned char *gt, int b) __attribute__((always_inline)) {
+        const bool edge = a.causal && key0 + Sh::OWN > row_token(a, r0) + past + 1;
+#pragma unroll
+        for (int t = 0; t < Sh::RT; ++t) {
+            const int sub = (WK == 1 ? 0 : wave * 32) + 32 * t;
+            floatx16_t s = zero16(), dp = zero16();
+#pragma unroll
+            for (int m = 0; m < NM; ++m) {
+                s = product(row_frag<T, D>(qt, sub + n, m, half), kf[m], s);
+                dp = product(row_frag<T, D>(gt, sub + n, m, half), vf[m], dp);
+            }
+            if (edge) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = key <= row_token(a, r0 + sub + 8 * (i >> 2) + 4 * half + (i & 3)) + past ? s[i] : kNegInf;
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 l2 = *reinterpret_cast<const float4 *>(&st[b][0][sub + 8 * g + 4 * half]);
+                const float4 dl = *reinterpret_cast<const float4 *>(&st[b][1][sub + 8 * g + 4 * half]);
+                const float l[4] = {l2.x, l2.y, l2.z, l2.w}, d[4] = {dl.x, dl.y, dl.z, dl.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[4 * g + i] = fast_exp2(fmaf(s[4 * g + i], c, -l[i]));
+                    dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - d[i]);
+                }
+            }
+            weighted_rows<D>(gt, sub, s, dv, (const T *)nullptr);
+            weighted_rows<D>(qt, sub, dp, dk, (const T *)nullptr);
+        }
+    };
+    if (rbeg < rend) {
+        if constexpr (Sh::NBUF == 2) {
+            unsigned char *const qa = lds, *const ga = lds + Sh::TILE, *const qb = lds + 2 * Sh::TILE, *const gb = lds + 3 * Sh::TILE;
+            request(rbeg, qa, ga);
+            park(0);
+            for (int r0 = rbeg; r0 < rend; r0 += 2 * Sh::ROWS) {
+                wait_loads_and_sync();
+                if (r0 + Sh::ROWS < rend) request(r0 + Sh::ROWS, qb, gb);
+                tile(r0, qa, ga, 0);
+                if (r0 + Sh::ROWS >= rend) break;
+                park(1);
+                wait_loads_and_sync();
+                if (r0 + 2 * Sh::ROWS < rend) request(r0 + 2 * Sh::ROWS, qa, ga);
+                tile(r0 + Sh::ROWS, qb, gb, 1);
+                if (r0 + 2 * Sh::ROWS < rend) park(0);
+            }
+        } else {
+            for (int r0 = rbeg; r0 < rend; r0 += Sh::ROWS) {
+                __syncthreads();
+                request(r0, lds, lds + Sh::TILE);
+                park(0);
+                wait_loads_and_sync();
+                tile(r0, lds, lds + Sh::TILE, 0);
+            }
+        }
+    }
+    T *const kop = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(dK) + (int64_t)(sq.k0 + kc) * a.dk_row + (int64_t)hk * a.dk_head);
+    T *const vop = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(dV) + (int64_t)(sq.k0 + kc) * a.dv_row + (int64_t)hk * a.dv_head);
+    const int64_t pid = (((int64_t)(sq.k0 + kc) * a.Hkv + hk) * a.splits + split) * D;
+    auto put_k = [&](int ch, float x, float y, float z, float w) __attribute__((always_inline)) {
+        if (key >= sq.nk) return;
+        if (a.splits > 1) store4(part_k + pid + ch, x * a.scale, y * a.scale, z * a.scale, w * a.scale);
+        else store4(kop + ch, x * a.scale, y * a.scale, z * a.scale, w * a.scale);
+    };
+    auto put_v = [&](int ch, float x, float y, float z, float w) __attribute__((always_inline)) {
+        if (key >= sq.nk) return;
+        if (a.splits > 1) store4(part_v + pid + ch, x, y, z, w);
+        else store4(vop + ch, x, y, z, w);
+    };
+    if constexpr (WK > 1) {
+        join_waves<D>(reinterpret_cast<float *>(lds), dk, wave, put_k);
+        join_waves<D>(reinterpret_cast<float *>(lds), dv, wave, put_v);
+    } else {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int ch = 32 * nb + 8 * g + 4 * half;
+                put_k(ch, dk[nb][4 * g], dk[nb][4 * g + 1], dk[nb][4 * g + 2], dk[nb][4 * g + 3]);
+                put_v(ch, dv[nb][4 * g], dv[nb][4 * g + 1], dv[nb][4 * g + 2], dv[nb][4 * g + 3]);
+            }
+    }
+}
+
+// Sums of the pieces.  KEYS: of dK and dV (blockIdx.y), pieces of the rows; else of dQ, pieces of the keys.
+template <typename T, int D, bool KEYS>
+__global__ __launch_bounds__(256) void packed_sum_kernel(const float *__restrict__ p0, const float *__restrict__ p1, T *__restrict__ out0, T *__restrict__ out1, PackedArgs a)
+{
+    constexpr int LPR = D / 4;
+    const int heads = KEYS ? a.Hkv : a.Hq;
+    int tok, head;
+    if (!merge_row<LPR>(KEYS ? a.total_k : a.total_q, heads, tok, head)) return;
+    const int lane = threadIdx.x % LPR;
+    const Sequence sq = read_sequence(a, __builtin_amdgcn_readfirstlane(find_sequence(KEYS ? a.cu_k : a.cu_q, a.n_seq, KEYS ? a.total_k : a.total_q, 1, 0, tok)));
+    const int t0 = KEYS ? sq.k0 : sq.q0, nt = KEYS ? sq.nk : sq.nq;
+    if (tok < t0 || tok >= t0 + nt || head >= heads) return;
+    const int pieces = max(1, ((KEYS ? sq.nq * a.group : sq.nk) + a.chunk - 1) / a.chunk);
+    const bool second = KEYS && blockIdx.y;
+    const float *p = (second ? p1 : p0) + ((int64_t)tok * heads + head) * a.splits * D + 4 * lane;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < pieces; ++s) {
+        const float4 x = *reinterpret_cast<const float4 *>(p + s * D);
+        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+    }
+    const int64_t rb = KEYS ? (second ? a.dv_row : a.dk_row) : a.dq_row, hb = KEYS ? (second ? a.dv_head : a.dk_head) : a.dq_head;
+    T *op = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(second ? out1 : out0) + (int64_t)tok * rb + (int64_t)head * hb);
+    store4(op + 4 * lane, v[0], v[1], v[2], v[3]);
+}
+
+template <typename T, int D, int WK>
+dsv_status launch_dq(const PackedArgs &a, const T *Q, const T *K, const T *V, const T *dO, const float2 *stat, T *dQ, float *part, hipStream_t st)
+{
+    const int64_t slots = tile_slots(a.total_q, a.group, BwdShape<T, D, WK>::OWN, a.n_seq);
+    packed_dq_kernel<T, D, WK><<<dim3((unsigned)(slots * a.Hkv), a.splits), 256, 0, st>>>(Q, K, V, dO, stat, dQ, part, a);
+    DSV_LAUNCH_CHECK();
+    if (a.splits > 1) {
+        packed_sum_kernel<T, D, false><<<merge_blocks<D / 4>(a.total_q, a.Hq), 256, 0, st>>>(part, nullptr, dQ, nullptr, a);
+        DSV_LAUNCH_CHECK();
+    }
+    return DSV_OK;
+}
+
+template <typename T, int D, int WK>
+dsv_status launch_dkdv(const PackedArgs &a, const T *Q, const T *K, const T *V, const T *dO, const float2 *stat, T *dK, T *dV, float *part, hipStream_t st)
+{
+    const int64_t slots = tile_slots(a.total_k, 1, BwdShape<T, D, WK>::OWN, a.n_seq);
+    float *const part_v = part + packed_dkdv_bytes(a.total_k, a.Hkv, D, a.splits) / 8;
+    packed_dkdv_kernel<T, D, WK><<<dim3((unsigned)(slots * a.Hkv), a.splits), 256, 0, st>>>(Q, K, V, dO, stat, dK, dV, part, part_v, a);
+    DSV_LAUNCH_CHECK();
+    if (a.splits > 1) {
+        packed_sum_kernel<T, D, true><<<dim3(merge_blocks<D / 4>(a.total_k, a.Hkv), 2), 256, 0, st>>>(part, part_v, dK, dV, a);
+        DSV_LAUNCH_CHECK();
+    }
+    return DSV_OK;
+}
+
+template <typename T, int D>
+dsv_status launch_t(PackedArgs a, const PackedBwdPlan &pl, const void *Qv, const void *Kv, const void *Vv, const void *Ov, const void *tail, const float *lse,
+                    const void *dOv, void *dQv, void *dKv, void *dVv, char *ws, hipStream_t st)
+{
+    const T *Q = static_cast<const T *>(Qv), *K = static_cast<const T *>(Kv), *V = static_cast<const T *>(Vv), *dO = static_cast<const T *>(dOv);
+    T *dQ = static_cast<T *>(dQv), *dK = static_cast<T *>(dKv), *dV = static_cast<T *>(dVv);
+    float2 *const stat = reinterpret_cast<float2 *>(ws);
+    float *const part = reinterpret_cast<float *>(ws + packed_stat_bytes(a.total_q, a.Hq));  // of dQ, then, when that is done, of dK and dV
+    dsv_status s = DSV_OK;
+    if (a.total_q > 0) {
+        packed_stat_kernel<T, D><<<merge_blocks<D *(int)sizeof(T) / 16>(a.total_q, a.Hq), 256, 0, st>>>(static_cast<const T *>(Ov), static_cast<const T *>(tail), dO, lse, stat, a);
+        DSV_LAUNCH_CHECK();
+        a.splits = pl.splits_q;
+        a.chunk = pl.chunk_q;
+        s = pl.few_q ? launch_dq<T, D, 4>(a, Q, K, V, dO, stat, dQ, part, st) : launch_dq<T, D, 1>(a, Q, K, V, dO, stat, dQ, part, st);
+        if (s != DSV_OK) return s;
+    }
+    if (a.total_k > 0) {
+        a.splits = pl.splits_k;
+        a.chunk = pl.chunk_k;
+        s = pl.few_k ? launch_dkdv<T, D, 4>(a, Q, K, V, dO, stat, dK, dV, part, st) : launch_dkdv<T, D, 1>(a, Q, K, V, dO, stat, dK, dV, part, st);
+    }
+    return s;
+}
+}  // namespace
+
+dsv_status launch_packed_bwd(const PackedArgs &a, const PackedBwdPlan &plan, int dtype, int d, const void *Q, const void *K, const void *V, const void *O,
+                             const void *O_tail, const float *lse, const void *dO, void *dQ, void *dK, void *dV, char *ws, hipStream_t st)
+{
+    if (dtype == DSV_BF16)
+        return d == 128 ? launch_t<bf16_t, 128>(a, plan, Q, K, V, O, O_tail, lse, dO, dQ, dK, dV, ws, st) : launch_t<bf16_t, 64>(a, plan, Q, K, V, O, O_tail, lse, dO, dQ, dK, dV, ws, st);
+    return d == 128 ? launch_t<float, 128>(a, plan, Q, K, V, O, nullptr, lse, dO, dQ, dK, dV, ws, st) : launch_t<float, 64>(a, plan, Q, K, V, O, nullptr, lse, dO, dQ, dK, dV, ws, st);
+}
+
+}  // namespace dsv

@@ -1,0 +1,270 @@
+// Softmax attention over packed sequences, forward.
+//
+//   s_ij = scale q_i . k_j over the keys j of i's sequence (causal: j <= i + nk - nq);  O_i = sum_j p_ij v_j,  lse_i = log sum_j exp s_ij
+//
+// One pass over the keys with the running maximum and sum.  A wave owns 32 rows as the columns of its products, S^T = K Q^T and
+// O^T = V^T P^T: a lane then holds one row's scores, the maximum and the sum are its own but for one exchange between the halves, and
+// the scores are where the second product wants them.
+#include "packed_attn.h"
+
+namespace dsv {
+namespace {
+
+// WK = 1: the four waves own 32 rows each and share tiles of 64 keys.  WK = 4: they own the same 32 rows and take 32 keys each of a tile of
+// 128; for calls of few rows.  NBUF: tiles in LDS in turn.
+template <typename T, int D, int WK> struct FwdShape {
+    static constexpr int ROWS = WK == 1 ? 128 : 32, KEYS = WK == 1 ? 64 : 128, KT = KEYS / 32 / WK;
+    static constexpr int TILE = KEYS * D * (int)sizeof(T);
+    static constexpr int NBUF = 2 * 2 * TILE <= 128 * 1024 ? 2 : 1;
+    static constexpr int LDS = NBUF * 2 * TILE;
+};
+
+template <typename T, int D, int WK>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed_fwd_kernel(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V,
+                                                                                        T *__restrict__ O, bf16_t *__restrict__ O_tail, float *__restrict__ lse,
+                                                                                        float2 *__restrict__ pml, float *__restrict__ pacc, PackedArgs a)
+{
+    typedef RowTile<T, D> RT;
+    typedef FwdShape<T, D, WK> Sh;
+    constexpr int NM = RT::RB / 32, NB = D / 32, KT = Sh::KT;
+    __shared__ __align__(1024) unsigned char lds[Sh::LDS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, half = lane >> 5;
+    // heads side by side: with as many heads as XCDs, or a multiple or a divisor of that, a head's keys stay in the L2 of one or a few of them;
+    // causal tiles of most keys first
+    const int hk = blockIdx.x % a.Hkv, place = blockIdx.x / a.Hkv, split = blockIdx.y;
+    const int slot = a.causal ? (int)(gridDim.x / a.Hkv) - 1 - place : place;
+    const int si = __builtin_amdgcn_readfirstlane(find_sequence(a.cu_q, a.n_seq, a.total_q, a.group, Sh::ROWS, slot));
+    const Sequence sq = read_sequence(a, si);
+    const int rows = sq.nq * a.group;
+    const int row0 = (slot - first_slot(a.cu_q[si], a.total_q, a.group, Sh::ROWS, si)) * Sh::ROWS;
+    if (row0 < 0 || row0 >= rows) return;
+    const int row = row0 + (WK == 1 ? wave * 32 : 0) + n;
+    const int rc = min(row, rows - 1), tok = row_token(a, rc), head = hk * a.group + (rc - tok * a.group);
+    // keys this block walks, and the first key that this lane's row does not see
+    const int kbeg = split * a.chunk, kcut = a.chunk ? min(sq.nk, kbeg + a.chunk) : sq.nk;
+    const int past = sq.nk - sq.nq, seen = a.causal ? min(sq.nk, tok + past + 1) : sq.nk;
+    int kend = kcut;
+    if (a.causal) kend = min(kend, row_token(a, min(row0 + Sh::ROWS, rows) - 1) + past + 1);
+    if (a.chunk && kbeg >= sq.nk && split > 0) return;  // no such piece of this sequence: the merge does not look for it
+
+    Frag<T> qf[NM];
+    {
+        const unsigned char *qp = reinterpret_cast<const unsigned char *>(Q) + (int64_t)(sq.q0 + tok) * a.q_row + (int64_t)head * a.q_head;
+#pragma unroll
+        for (int m = 0; m < NM; ++m) qf[m] = *reinterpret_cast<const Frag<T> *>(qp + (2 * m + half) * 16);
+    }
+    const unsigned char *kp = reinterpret_cast<const unsigned char *>(K) + (int64_t)sq.k0 * a.k_row + (int64_t)hk * a.k_head;
+    const unsigned char *vp = reinterpret_cast<const unsigned char *>(V) + (int64_t)sq.k0 * a.v_row + (int64_t)hk * a.v_head;
+    auto request = [&](int k0, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {  // rows past the end repeat the last one
+        RT::template load<Sh::KEYS, 4>(kt, wave, [&](int r) { return kp + (int64_t)min(k0 + r, sq.nk - 1) * a.k_row; });
+        RT::template load<Sh::KEYS, 4>(vt, wave, [&](int r) { return vp + (int64_t)min(k0 + r, sq.nk - 1) * a.v_row; });
+    };
+
+    const float c = a.scale * kLog2e;
+    floatx16_t acc[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) acc[nb] = zero16();
+    float mrun = kNegInf, l = 0.f;
+    auto tile = [&](int k0, const unsigned char *kt, const unsigned char *vt) __attribute__((always_inline)) {
+        const int sub = WK == 1 ? 0 : wave * 32;
+        floatx16_t s[KT];
+#pragma unroll
+        for (int t = 0; t < KT; ++t) s[t] = zero16();
+#pragma unroll
+        for (int m = 0; m < NM; ++m)
+#pragma unroll
+            for (int t = 0; t < KT; ++t) s[t] = product(row_frag<T, D>(kt, sub + 32 * t + n, m, half), qf[m], s[t]);
+        // the tile's last key is behind the end, or not seen by the wave's first row
+        const bool edge = k0 + Sh::KEYS > kcut || (a.causal && k0 + Sh::KEYS > row_token(a, row0) + past + 1);
+        if (edge) {
+            const int lim = min(seen, kcut) - k0 - sub - 4 * half;
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[t][i] = 32 * t + 8 * (i >> 2) + (i & 3) < lim ? s[t][i] : kNegInf;
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][i]);
+        mx = halves_max(mx) * c;
+        // The sums are held against a maximum that may be up to 2^8 too low: they are rescaled only when a row's has grown by more.
+        if (__any(mx > mrun + 8.f)) {
+            const float m2 = fmaxf(mrun, mx), f = m2 == kNegInf ? 1.f : fast_exp2(mrun - m2);
+            l *= f;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[nb][i] *= f;
+            mrun = m2;
+        }
+        const float mref = mrun == kNegInf ? 0.f : mrun;
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[t][i] = fast_exp2(fmaf(s[t][i], c, -mref));
+                l += s[t][i];
+            }
+            weighted_rows<D>(vt, sub + 32 * t, s[t], acc, (const T *)nullptr);
+        }
+    };
+    if (kbeg < kend) {
+        if constexpr (Sh::NBUF == 2) {
+            unsigned char *const ka = lds, *const va = lds + Sh::TILE, *const kb = lds + 2 * Sh::TILE, *const vb = lds + 3 * Sh::TILE;
+            request(kbeg, ka, va);
+            for (int k0 = kbeg; k0 < kend; k0 += 2 * Sh::KEYS) {
+                wait_loads_and_sync();
+                if (k0 + Sh::KEYS < kend) request(k0 + Sh::KEYS, kb, vb);
+                tile(k0, ka, va);
+                if (k0 + Sh::KEYS >= kend) break;
+                wait_loads_and_sync();
+                if (k0 + 2 * Sh::KEYS < kend) request(k0 + 2 * Sh::KEYS, ka, va);
+                tile(k0 + Sh::KEYS, kb, vb);
+            }
+        } else {
+            for (int k0 = kbeg; k0 < kend; k0 += Sh::KEYS) {
+                __syncthreads();
+                request(k0, lds, lds + Sh::TILE);
+                wait_loads_and_sync();
+                tile(k0, lds, lds + Sh::TILE);
+            }
+        }
+    }
+    l = halves_sum(l);
+    if constexpr (WK > 1) {  // the waves' sums over their keys, joined in LDS: wave w then holds channels 32 w / 4 .. of every row
+        __syncthreads();
+        float *const sm = reinterpret_cast<float *>(lds), *const sl = sm + 128, *const sa = sm + 256;
+        if (half == 0) {
+            sm[wave * 32 + n] = mrun;
+            sl[wave * 32 + n] = l;
+        }
+        __syncthreads();
+        float m2 = kNegInf;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m2 = fmaxf(m2, sm[w * 32 + n]);
+        const float mref = m2 == kNegInf ? 0.f : m2;
+        l = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) l += sl[w * 32 + n] * fast_exp2(sm[w * 32 + n] - mref);
+        const float f = fast_exp2(mrun - mref);
+        // channel by row, [wave][channel / 4][row][4]
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<float4 *>(sa + ((wave * (D / 4) + nb * 8 + 2 * g + half) * 32 + n) * 4) =
+                    make_float4(acc[nb][4 * g] * f, acc[nb][4 * g + 1] * f, acc[nb][4 * g + 2] * f, acc[nb][4 * g + 3] * f);
+        mrun = m2;
+        __syncthreads();
+        if (row >= rows) return;
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const int64_t rid = (int64_t)(sq.q0 + tok) * a.Hq + head;
+        for (int g = wave * 2 + half; g < D / 4; g += 8) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float4 x = *reinterpret_cast<const float4 *>(sa + ((w * (D / 4) + g) * 32 + n) * 4);
+                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+            }
+            if (a.splits > 1) {
+                store4(pacc + (rid * a.splits + split) * D + 4 * g, v[0], v[1], v[2], v[3]);
+            } else {
+                T *op = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(O) + (int64_t)(sq.q0 + tok) * a.o_row + (int64_t)head * a.o_head);
+                store_out(op + 4 * g, O_tail ? O_tail + rid * D + 4 * g : nullptr, v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+            }
+        }
+        if (wave == 0 && half == 0) {
+            if (a.splits > 1) pml[rid * a.splits + split] = make_float2(mrun, l);
+            else lse[(int64_t)head * a.total_q + sq.q0 + tok] = l > 0.f ? (mrun + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+        }
+    } else {
+        if (row >= rows) return;
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const int64_t rid = (int64_t)(sq.q0 + tok) * a.Hq + head;
+        if (a.splits > 1) {
+            float *const pa = pacc + (rid * a.splits + split) * D;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    store4(pa + 32 * nb + 8 * g + 4 * half, acc[nb][4 * g], acc[nb][4 * g + 1], acc[nb][4 * g + 2], acc[nb][4 * g + 3]);
+            if (half == 0) pml[rid * a.splits + split] = make_float2(mrun, l);
+        } else {
+            T *op = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(O) + (int64_t)(sq.q0 + tok) * a.o_row + (int64_t)head * a.o_head);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int ch = 32 * nb + 8 * g + 4 * half;
+                    store_out(op + ch, O_tail ? O_tail + rid * D + ch : nullptr, acc[nb][4 * g] * inv, acc[nb][4 * g + 1] * inv,
+                              acc[nb][4 * g + 2] * inv, acc[nb][4 * g + 3] * inv);
+                }
+            if (half == 0) lse[(int64_t)head * a.total_q + sq.q0 + tok] = l > 0.f ? (mrun + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+        }
+    }
+}
+
+// The pieces of a row joined: weights 2^(m_s - max).  A wave takes 64 / (D / 4) heads of one query, D / 4 lanes each.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void packed_fwd_merge_kernel(const float2 *__restrict__ pml, const float *__restrict__ pacc, T *__restrict__ O,
+                                                               bf16_t *__restrict__ O_tail, float *__restrict__ lse, PackedArgs a)
+{
+    constexpr int LPR = D / 4;
+    int tok, head;
+    if (!merge_row<LPR>(a.total_q, a.Hq, tok, head)) return;
+    const int lane = threadIdx.x % LPR;
+    const Sequence sq = read_sequence(a, __builtin_amdgcn_readfirstlane(find_sequence(a.cu_q, a.n_seq, a.total_q, 1, 0, tok)));
+    if (tok < sq.q0 || tok >= sq.q0 + sq.nq || head >= a.Hq) return;
+    const int64_t rid = (int64_t)tok * a.Hq + head;
+    const int pieces = max(1, (sq.nk + a.chunk - 1) / a.chunk);
+    const float2 *const ml = pml + rid * a.splits;
+    const float *const pa = pacc + rid * a.splits * D + 4 * lane;
+    float m = kNegInf, l = 0.f;
+    for (int s = 0; s < pieces; ++s) m = fmaxf(m, ml[s].x);
+    const float mref = m == kNegInf ? 0.f : m;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < pieces; ++s) {
+        const float f = fast_exp2(ml[s].x - mref);
+        l = fmaf(ml[s].y, f, l);
+        const float4 x = *reinterpret_cast<const float4 *>(pa + s * D);
+        v[0] = fmaf(x.x, f, v[0]); v[1] = fmaf(x.y, f, v[1]); v[2] = fmaf(x.z, f, v[2]); v[3] = fmaf(x.w, f, v[3]);
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    T *op = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(O) + (int64_t)tok * a.o_row + (int64_t)head * a.o_head);
+    store_out(op + 4 * lane, O_tail ? O_tail + rid * D + 4 * lane : nullptr, v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+    if (lane == 0) lse[(int64_t)head * a.total_q + tok] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+}
+
+template <typename T, int D, int WK>
+dsv_status launch_t(const PackedArgs &a, const void *Q, const void *K, const void *V, void *O, void *O_tail, float *lse, char *ws, hipStream_t st)
+{
+    const int64_t slots = tile_slots(a.total_q, a.group, FwdShape<T, D, WK>::ROWS, a.n_seq);
+    float *const pacc = reinterpret_cast<float *>(ws);
+    float2 *const pml = reinterpret_cast<float2 *>(ws + packed_fwd_acc_bytes(a.total_q, a.Hq, D, a.splits));
+    packed_fwd_kernel<T, D, WK><<<dim3((unsigned)(slots * a.Hkv), a.splits), 256, 0, st>>>(
+        static_cast<const T *>(Q), static_cast<const T *>(K), static_cast<const T *>(V), static_cast<T *>(O), static_cast<bf16_t *>(O_tail), lse, pml, pacc, a);
+    DSV_LAUNCH_CHECK();
+    if (a.splits > 1) {
+        packed_fwd_merge_kernel<T, D><<<merge_blocks<D / 4>(a.total_q, a.Hq), 256, 0, st>>>(pml, pacc, static_cast<T *>(O), static_cast<bf16_t *>(O_tail), lse, a);
+        DSV_LAUNCH_CHECK();
+    }
+    return DSV_OK;
+}
+}  // namespace
+
+dsv_status launch_packed_fwd(const PackedArgs &a, int dtype, int d, bool few, const void *Q, const void *K, const void *V, void *O, void *O_tail,
+                             float *lse, char *ws, hipStream_t st)
+{
+    if (dtype == DSV_BF16) {
+        if (d == 128) return few ? launch_t<bf16_t, 128, 4>(a, Q, K, V, O, O_tail, lse, ws, st) : launch_t<bf16_t, 128, 1>(a, Q, K, V, O, O_tail, lse, ws, st);
+        return few ? launch_t<bf16_t, 64, 4>(a, Q, K, V, O, O_tail, lse, ws, st) : launch_t<bf16_t, 64, 1>(a, Q, K, V, O, O_tail, lse, ws, st);
+    }
+    if (d == 128) return few ? launch_t<float, 128, 4>(a, Q, K, V, O, nullptr, lse, ws, st) : launch_t<float, 128, 1>(a, Q, K, V, O, nullptr, lse, ws, st);
+    return few ? launch_t<float, 64, 4>(a, Q, K, V, O, nullptr, lse, ws, st) : launch_t<float, 64, 1>(a, Q, K, V, O, nullptr, lse, ws, st);
+}
+
+}  // namespace dsv
