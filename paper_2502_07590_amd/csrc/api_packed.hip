@@ -41,6 +41,12 @@ dsv_status check_packed(const dsv_packed *p, bool grad)
         if (!rows_apart(p->dq, p->total_q, p->Hq, p->d) || !rows_apart(p->dk, p->total_k, p->Hkv, p->d) || !rows_apart(p->dv, p->total_k, p->Hkv, p->d))
             return DSV_EINVAL;
     }
+    // the kernels place the rows of a tile by 32-bit offsets from its first
+    const int64_t most = 1ll << 32, group = p->Hq / p->Hkv;
+    for (const dsv_rows *s : {&p->q, &p->k, &p->v, &p->dO})
+        if (128 * s->row * (int64_t)es >= most) return DSV_EUNSUPPORTED;
+    for (const dsv_rows *s : {&p->q, &p->dO})
+        if (grad && 128 * s->row * (int64_t)es + (group - 1) * s->head * (int64_t)es >= most) return DSV_EUNSUPPORTED;
     // row / group by a 32-bit reciprocal, and the blocks of a launch
     if ((int64_t)p->total_q * p->Hq >= 1ll << 31 || (int64_t)p->total_q * p->Hq * (p->Hq / p->Hkv) >= 1ll << 32) return DSV_EUNSUPPORTED;
     if ((int64_t)p->total_q * p->Hq / 32 + (int64_t)p->n_seq * p->Hkv >= 1 << 24) return DSV_EUNSUPPORTED;

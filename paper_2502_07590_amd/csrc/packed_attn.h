@@ -9,6 +9,9 @@
 
 namespace dsv {
 
+#ifndef DSV_PIN
+#define DSV_PIN 0x406
+#endif
 constexpr float kNegInf = -__builtin_inff();
 
 // A descriptor as the kernels read it; strides in bytes.
@@ -61,27 +64,82 @@ __device__ __forceinline__ int find_sequence(const int32_t *__restrict__ cu, int
 }
 __host__ __device__ __forceinline__ int64_t tile_slots(int64_t total, int mul, int rows, int n_seq) { return total * mul / rows + n_seq; }
 
-// A tile of rows in LDS, row after row.  Piece p (16 bytes) of row r lies at place p ^ turn(r) of the row: eight consecutive rows have
-// their p-th pieces, and four consecutive rows their p-th pairs of pieces, in different banks -- the two ways matrix operands are read,
-// 16 bytes of 32 rows or transposing from four rows at a time.
+// A tile of rows in LDS, row after row.  Piece p (16 bytes) of row r lies at place p ^ turn(r) of the row, so that what one cycle of the 64
+// banks serves lies in different ones: 16 bytes of 16 consecutive rows; for the transposing reads 64 bytes of four rows (bf16); 128 bytes of two rows
+// four apart (fp32, element by element).  (With bits of turn that let the halves of a transposing read meet, those took twice as long: a third
+// of all LDS cycles of the forward.)
 template <typename T, int D> struct RowTile {
     static constexpr int RB = D * (int)sizeof(T), PIECES = RB / 16;
-    __device__ __forceinline__ static int turn(int r) { return (((r & 3) << 1) | ((r >> 2) & 1) | (r & 8)) & (PIECES - 1); }
-    __device__ __forceinline__ static int at(int r, int p) { return r * RB + ((p ^ turn(r)) << 4); }
-
-    // ROWS rows into LDS by direct loads, a kilobyte an instruction, shared among WAVES waves; row(r) is the address of row r.
-    template <int ROWS, int WAVES, typename F> __device__ __forceinline__ static void load(unsigned char *lds, int wave, F row)
+    __device__ __forceinline__ static int turn(int r)
     {
-        constexpr int N = ROWS * RB / 1024, RPC = 1024 / RB;
-        static_assert(N % WAVES == 0, "every kilobyte has its wave");
-        const int lane = threadIdx.x & 63;
+        if constexpr (sizeof(T) == 4) return (((r >> 2) & 1) << 3) | ((r & 3) << 1) | ((r >> 3) & 1);
+        else if constexpr (D == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
+        else return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);  // two rows to 256 bytes
+    }
+    __device__ __forceinline__ static int at(int r, int p) { return r * RB + ((p ^ turn(r)) << 4); }
+};
+
+// The loads of one wave for tiles of ROWS rows that WAVES waves bring together, directly into LDS, a kilobyte an instruction.  A lane's
+// place in a tile is one offset plus what all lanes add; rows past the end repeat the last one.
+template <typename T, int D, int ROWS, int WAVES> struct RowLoads {
+    typedef RowTile<T, D> RT;
+    static constexpr int N = ROWS * RT::RB / 1024 / WAVES, RPC = 1024 / RT::RB, STEP = WAVES * RPC;  // rows from a load to the next
+    static constexpr int NV = STEP % 16 ? 2 : 1;  // turn() has a period of 16 rows
+    static_assert(N * WAVES * 1024 == ROWS * RT::RB && (NV == 1 || STEP == 8), "every kilobyte has its wave");
+    uint32_t off[NV], piece[NV];
+    int wave;
+    __device__ __forceinline__ int row(int i) const { return i * STEP + wave * RPC + (int)(threadIdx.x & 63) / RT::PIECES; }
+    __device__ __forceinline__ void set(int wave_, int64_t row_b)
+    {
+        wave = wave_;
 #pragma unroll
-        for (int i = 0; i < N / WAVES; ++i) {
-            const int c = i * WAVES + wave, r = c * RPC + lane / PIECES;
-            const unsigned char *src = row(r) + (((lane % PIECES) ^ turn(r)) << 4);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
-                                             (__attribute__((address_space(3))) void *)(lds + c * 1024), 16, 0, 0);
+        for (int v = 0; v < NV; ++v) {
+            piece[v] = (uint32_t)(((int)(threadIdx.x & 63) % RT::PIECES) ^ RT::turn(row(v))) << 4;
+            off[v] = (uint32_t)row(0) * (uint32_t)row_b + piece[v];
         }
+    }
+    __device__ __forceinline__ void send(const unsigned char *base, const uint32_t (&at)[N], unsigned char *lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + at[i]),
+                                             (__attribute__((address_space(3))) void *)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
+    }
+    __device__ __forceinline__ void plain(int64_t row_b, int left, uint32_t (&at)[N]) const  // rows row_b apart, `left` of them to the end
+    {
+        const uint32_t last = (uint32_t)(min(left, ROWS) - 1) * (uint32_t)row_b;
+        uint32_t o[NV], p[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {  // hidden from the compiler, which would keep all N places in registers that the products need
+            o[v] = off[v];
+            p[v] = piece[v];
+            asm volatile("" : "+v"(o[v]), "+v"(p[v]));
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) at[i] = min(o[i % NV] + (uint32_t)(i * STEP) * (uint32_t)row_b, last + p[i % NV]);
+    }
+    // rows k0 .. of n that lie row_b apart
+    __device__ __forceinline__ void keys(const unsigned char *first, int64_t row_b, int k0, int n, unsigned char *lds) const
+    {
+        uint32_t at[N];
+        plain(row_b, n - k0, at);
+        send(first + (int64_t)k0 * row_b, at, lds);
+    }
+    // rows r0 .. of n, row = token * group + head
+    __device__ __forceinline__ void rows(const PackedArgs &a, const unsigned char *first, int64_t row_b, int64_t head_b, int r0, int n, unsigned char *lds) const
+    {
+        uint32_t at[N];
+        const int tok0 = row_token(a, r0);
+        if (a.group == 1) {
+            plain(row_b, n - r0, at);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int rho = min(r0 + row(i), n - 1), tok = row_token(a, rho);
+                at[i] = (uint32_t)(tok - tok0) * (uint32_t)row_b + (uint32_t)(rho - tok * a.group) * (uint32_t)head_b + piece[i % NV];
+            }
+        }
+        send(first + (int64_t)tok0 * row_b, at, lds);
     }
 };
 
@@ -117,28 +175,129 @@ template <typename T, int D> __device__ __forceinline__ Frag<T> row_frag(const u
     return *reinterpret_cast<const Frag<T> *>(tile + RowTile<T, D>::at(r, 2 * m + half));
 }
 
-// acc[nb] (channels 32 nb .. + 31 by own rows) += sum over the 32 tile rows of row[channel] * w; w: a result of a product with the tile rows
-// as A.  bf16: 16 rows a step, weights rounded to bf16 (half a step of 2^-8 each, of one sign as often as the other; the sums are in 32 bits).
-template <int D> __device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const floatx16_t &w, floatx16_t (&acc)[D / 32], const bf16_t *)
+// Fragments are read two steps before the products that need them.  The order of reads and products is pinned -- left alone a read sinks to its
+// use, or all of them rise and spill -- while vector arithmetic may move between them.
+__device__ __forceinline__ void pin_order() { __builtin_amdgcn_sched_barrier(DSV_PIN); }
+
+// s[t] = rows r + 32 t of a tile by the own rows
+template <typename T, int D, int KT>
+__device__ __forceinline__ void tile_scores(const unsigned char *tile, int r, const Frag<T> (&own)[D * sizeof(T) / 32], floatx16_t (&s)[KT])
 {
-    typedef RowTile<bf16_t, D> RT;
-    const int lane = threadIdx.x & 63, half = lane >> 5, e = (lane >> 2) & 3, q = lane & 3, b4 = (lane >> 4) & 1;
-    const int r = r0 + 4 * half + e;
+    constexpr int NM = D * (int)sizeof(T) / 32;
+    const int half = (threadIdx.x & 63) >> 5;
+    Frag<T> f[2][KT];
+    auto fetch = [&](int m) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        Frag<bf16_t> b;
-        b.v = __builtin_bit_cast(bf16x8_t, make_uint4(pack_bf16x2(w[8 * s], w[8 * s + 1]), pack_bf16x2(w[8 * s + 2], w[8 * s + 3]),
-                                                      pack_bf16x2(w[8 * s + 4], w[8 * s + 5]), pack_bf16x2(w[8 * s + 6], w[8 * s + 7])));
+        for (int t = 0; t < KT; ++t) f[m & 1][t] = row_frag<T, D>(tile, r + 32 * t, m, half);
+    };
 #pragma unroll
-        for (int nb = 0; nb < D / 32; ++nb) {
-            const int p = 4 * nb + 2 * b4 + (q >> 1), sub = (q & 1) * 8;
-            Frag<bf16_t> a;
-            a.v = tr_frag(tile + RT::at(r + 16 * s, p) + sub, tile + RT::at(r + 16 * s + 8, p) + sub);
-            acc[nb] = product(a, b, acc[nb]);
-        }
+    for (int t = 0; t < KT; ++t) s[t] = zero16();
+    fetch(0);
+    fetch(1);
+    pin_order();
+#pragma unroll
+    for (int m = 0; m < NM; ++m) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t) s[t] = product(f[m & 1][t], own[m], s[t]);
+        if (m + 2 < NM) fetch(m + 2);
+        pin_order();
     }
 }
-template <int D> __device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const floatx16_t &w, floatx16_t (&acc)[D / 32], const float *)
+// The same of row r of two tiles, each by own rows of its own.
+template <typename T, int D>
+__device__ __forceinline__ void tile_scores2(const unsigned char *t1, const unsigned char *t2, int r, const Frag<T> (&own1)[D * sizeof(T) / 32],
+                                             const Frag<T> (&own2)[D * sizeof(T) / 32], floatx16_t &s1, floatx16_t &s2)
+{
+    constexpr int NM = D * (int)sizeof(T) / 32;
+    const int half = (threadIdx.x & 63) >> 5;
+    Frag<T> f[2][2];
+    auto fetch = [&](int m) __attribute__((always_inline)) {
+        f[m & 1][0] = row_frag<T, D>(t1, r, m, half);
+        f[m & 1][1] = row_frag<T, D>(t2, r, m, half);
+    };
+    s1 = zero16();
+    s2 = zero16();
+    fetch(0);
+    fetch(1);
+    pin_order();
+#pragma unroll
+    for (int m = 0; m < NM; ++m) {
+        s1 = product(f[m & 1][0], own1[m], s1);
+        s2 = product(f[m & 1][1], own2[m], s2);
+        if (m + 2 < NM) fetch(m + 2);
+        pin_order();
+    }
+}
+
+// Weights as the products take them: of 32 tile rows by the own column, results of a product with the tile rows as A.
+// bf16: rounded (half a step of 2^-8 each, of one sign as often as the other; the sums are in 32 bits), 16 rows a step.
+template <typename T> struct Weights;
+template <> struct Weights<bf16_t> {
+    bf16x8_t v[2];
+    static constexpr int PIECES = 2;
+    __device__ __forceinline__ void set(const floatx16_t &w)
+    {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            v[s] = __builtin_bit_cast(bf16x8_t, make_uint4(pack_bf16x2(w[8 * s], w[8 * s + 1]), pack_bf16x2(w[8 * s + 2], w[8 * s + 3]),
+                                                           pack_bf16x2(w[8 * s + 4], w[8 * s + 5]), pack_bf16x2(w[8 * s + 6], w[8 * s + 7])));
+    }
+    // what the rounding of w to *this left
+    __device__ __forceinline__ void set_tail(const floatx16_t &w, const Weights &head)
+    {
+        floatx16_t t;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const uint4 h = __builtin_bit_cast(uint4, head.v[s]);
+            const uint32_t x[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                t[8 * s + 2 * i] = w[8 * s + 2 * i] - __uint_as_float(x[i] << 16);
+                t[8 * s + 2 * i + 1] = w[8 * s + 2 * i + 1] - __uint_as_float(x[i] & 0xFFFF0000u);
+            }
+        }
+        set(t);
+    }
+    __device__ __forceinline__ uint4 piece(int i) const { return __builtin_bit_cast(uint4, v[i]); }
+    __device__ __forceinline__ void set_piece(int i, uint4 x) { v[i] = __builtin_bit_cast(bf16x8_t, x); }
+};
+template <> struct Weights<float> {
+    floatx16_t v;
+    static constexpr int PIECES = 4;
+    __device__ __forceinline__ void set(const floatx16_t &w) { v = w; }
+    __device__ __forceinline__ uint4 piece(int i) const
+    {
+        return make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+    }
+    __device__ __forceinline__ void set_piece(int i, uint4 x)
+    {
+        v[4 * i] = __uint_as_float(x.x); v[4 * i + 1] = __uint_as_float(x.y); v[4 * i + 2] = __uint_as_float(x.z); v[4 * i + 3] = __uint_as_float(x.w);
+    }
+};
+
+// acc[nb] (channels 32 nb .. + 31 by own rows) += sum over tile rows r0 .. r0 + 31 of row[channel] * w
+template <int D> __device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const Weights<bf16_t> &w, floatx16_t (&acc)[D / 32])
+{
+    typedef RowTile<bf16_t, D> RT;
+    constexpr int NB = D / 32;
+    const int lane = threadIdx.x & 63, half = lane >> 5, e = (lane >> 2) & 3, q = lane & 3, b4 = (lane >> 4) & 1;
+    const int r = r0 + 4 * half + e;
+    bf16x8_t f[2];
+    auto fetch = [&](int i) __attribute__((always_inline)) {
+        const int s = i / NB, p = 4 * (i % NB) + 2 * b4 + (q >> 1), sub = (q & 1) * 8;
+        f[i & 1] = tr_frag(tile + RT::at(r + 16 * s, p) + sub, tile + RT::at(r + 16 * s + 8, p) + sub);
+    };
+    fetch(0);
+    fetch(1);
+    pin_order();
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i) {
+        acc[i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i & 1], w.v[i / NB], acc[i % NB], 0, 0, 0);
+        if (i + 2 < 2 * NB) fetch(i + 2);
+        pin_order();
+    }
+}
+template <int D> __device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const Weights<float> &w, floatx16_t (&acc)[D / 32])
 {
     typedef RowTile<float, D> RT;
     const int lane = threadIdx.x & 63, half = lane >> 5, n = lane & 31;
@@ -148,9 +307,15 @@ template <int D> __device__ __forceinline__ void weighted_rows(const unsigned ch
 #pragma unroll
         for (int nb = 0; nb < D / 32; ++nb) {
             const float v = *reinterpret_cast<const float *>(tile + RT::at(r, 8 * nb + (n >> 2)) + (n & 3) * 4);
-            acc[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w[i], acc[nb], 0, 0, 0);
+            acc[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w.v[i], acc[nb], 0, 0, 0);
         }
     }
+}
+template <typename T, int D> __device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const floatx16_t &w, floatx16_t (&acc)[D / 32])
+{
+    Weights<T> x;
+    x.set(w);
+    weighted_rows<D>(tile, r0, x, acc);
 }
 
 // Value of the other half's lane with the same column, combined by max or sum.

@@ -44,11 +44,17 @@ template <typename T, int D, int WK> struct BwdShape {
     static constexpr int OWN = WK == 1 ? 128 : 32, ROWS = WK == 1 ? 64 : 128, RT = ROWS / 32 / WK;  // own rows, rows of a tile, 32s of them a wave
     static constexpr int TILE = ROWS * D * (int)sizeof(T);
     static constexpr int NBUF = 2 * 2 * TILE <= 128 * 1024 ? 2 : 1;
-    static constexpr int LDS = NBUF * 2 * TILE;
+    static_assert(TILE / (NBUF == 2 ? 1 : 2) >= 32 * D * 4, "a wave's sums fit its part of the tiles");
+};
+
+constexpr int kPairKeys = 64;
+template <typename T, int D> struct PairShape {
+    static constexpr int ROWS = 64, NBUF = 2 * 2 * ROWS * D * (int)sizeof(T) <= 128 * 1024 ? 2 : 1;
 };
 
 // The four waves' sums of the same 32 rows, joined in LDS: thread t's share is channels 4 g .. 4 g + 3 of row t % 32 for g = t / 32, + 8, ...
-template <int D, typename F> __device__ __forceinline__ void join_waves(float *sa, const floatx16_t (&acc)[D / 32], int wave, F put)
+// area(w): where wave w's 32 rows of D sums go.
+template <int D, typename A, typename F> __device__ __forceinline__ void join_waves(A area, const floatx16_t (&acc)[D / 32], int wave, F put)
 {
     const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
     __syncthreads();
@@ -56,14 +62,14 @@ template <int D, typename F> __device__ __forceinline__ void join_waves(float *s
     for (int nb = 0; nb < D / 32; ++nb)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<float4 *>(sa + ((wave * (D / 4) + nb * 8 + 2 * g + half) * 32 + n) * 4) =
+            *reinterpret_cast<float4 *>(area(wave) + ((nb * 8 + 2 * g + half) * 32 + n) * 4) =
                 make_float4(acc[nb][4 * g], acc[nb][4 * g + 1], acc[nb][4 * g + 2], acc[nb][4 * g + 3]);
     __syncthreads();
     for (int g = wave * 2 + half; g < D / 4; g += 8) {
         float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const float4 x = *reinterpret_cast<const float4 *>(sa + ((w * (D / 4) + g) * 32 + n) * 4);
+            const float4 x = *reinterpret_cast<const float4 *>(area(w) + (g * 32 + n) * 4);
             v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
         }
         put(4 * g, v[0], v[1], v[2], v[3]);
@@ -78,7 +84,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
     typedef RowTile<T, D> RT;
     typedef BwdShape<T, D, WK> Sh;
     constexpr int NM = RT::RB / 32, NB = D / 32;
-    __shared__ __align__(1024) unsigned char lds[Sh::LDS];
+    // every tile an array of its own: reads of one then need not wait for the loads into another
+    __shared__ __align__(1024) unsigned char ka[Sh::TILE], va[Sh::TILE], kb[Sh::NBUF == 2 ? Sh::TILE : 16], vb[Sh::NBUF == 2 ? Sh::TILE : 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, half = lane >> 5;
     const int hk = blockIdx.x % a.Hkv, place = blockIdx.x / a.Hkv, split = blockIdx.y;
@@ -109,9 +116,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
     const float2 rs = stat[(int64_t)hk * a.total_q * a.group + (int64_t)sq.q0 * a.group + rc];
     const unsigned char *kp = reinterpret_cast<const unsigned char *>(K) + (int64_t)sq.k0 * a.k_row + (int64_t)hk * a.k_head;
     const unsigned char *vp = reinterpret_cast<const unsigned char *>(V) + (int64_t)sq.k0 * a.v_row + (int64_t)hk * a.v_head;
+    RowLoads<T, D, Sh::ROWS, 4> kl, vl;
+    kl.set(wave, a.k_row);
+    vl.set(wave, a.v_row);
     auto request = [&](int k0, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
-        RT::template load<Sh::ROWS, 4>(kt, wave, [&](int r) { return kp + (int64_t)min(k0 + r, sq.nk - 1) * a.k_row; });
-        RT::template load<Sh::ROWS, 4>(vt, wave, [&](int r) { return vp + (int64_t)min(k0 + r, sq.nk - 1) * a.v_row; });
+        kl.keys(kp, a.k_row, k0, sq.nk, kt);
+        vl.keys(vp, a.v_row, k0, sq.nk, vt);
     };
     const float c = a.scale * kLog2e;
     floatx16_t acc[NB];
@@ -122,12 +132,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
 #pragma unroll
         for (int t = 0; t < Sh::RT; ++t) {
             const int sub = (WK == 1 ? 0 : wave * 32) + 32 * t;
-            floatx16_t s = zero16(), dp = zero16();
-#pragma unroll
-            for (int m = 0; m < NM; ++m) {
-                s = product(row_frag<T, D>(kt, sub + n, m, half), qf[m], s);
-                dp = product(row_frag<T, D>(vt, sub + n, m, half), gf[m], dp);
-            }
+            floatx16_t s, dp;
+            tile_scores2<T, D>(kt, vt, sub + n, qf, gf, s, dp);
             if (edge) {
                 const int lim = min(seen, kcut) - k0 - sub - 4 * half;
 #pragma unroll
@@ -135,28 +141,28 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = fast_exp2(fmaf(s[i], c, -rs.x)) * (dp[i] - rs.y);
-            weighted_rows<D>(kt, sub, s, acc, (const T *)nullptr);
+            weighted_rows<T, D>(kt, sub, s, acc);
         }
     };
     if (kbeg < kend) {
         if constexpr (Sh::NBUF == 2) {
-            unsigned char *const ka = lds, *const va = lds + Sh::TILE, *const kb = lds + 2 * Sh::TILE, *const vb = lds + 3 * Sh::TILE;
             request(kbeg, ka, va);
             for (int k0 = kbeg; k0 < kend; k0 += 2 * Sh::ROWS) {
                 wait_loads_and_sync();
                 if (k0 + Sh::ROWS < kend) request(k0 + Sh::ROWS, kb, vb);
                 tile(k0, ka, va);
-                if (k0 + Sh::ROWS >= kend) break;
-                wait_loads_and_sync();
-                if (k0 + 2 * Sh::ROWS < kend) request(k0 + 2 * Sh::ROWS, ka, va);
-                tile(k0 + Sh::ROWS, kb, vb);
+                if (k0 + Sh::ROWS < kend) {  // (a break here makes the compiler move all sums to other registers and back)
+                    wait_loads_and_sync();
+                    if (k0 + 2 * Sh::ROWS < kend) request(k0 + 2 * Sh::ROWS, ka, va);
+                    tile(k0 + Sh::ROWS, kb, vb);
+                }
             }
         } else {
             for (int k0 = kbeg; k0 < kend; k0 += Sh::ROWS) {
                 __syncthreads();
-                request(k0, lds, lds + Sh::TILE);
+                request(k0, ka, va);
                 wait_loads_and_sync();
-                tile(k0, lds, lds + Sh::TILE);
+                tile(k0, ka, va);
             }
         }
     }
@@ -168,7 +174,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
         else store4(op + ch, x * a.scale, y * a.scale, z * a.scale, w * a.scale);
     };
     if constexpr (WK > 1) {
-        join_waves<D>(reinterpret_cast<float *>(lds), acc, wave, put);
+        auto area = [&](int w) __attribute__((always_inline)) {
+            return reinterpret_cast<float *>(Sh::NBUF == 2 ? (w == 0 ? ka : w == 1 ? va : w == 2 ? kb : vb) : (w < 2 ? ka : va) + (w & 1) * (Sh::TILE / 2));
+        };
+        join_waves<D>(area, acc, wave, put);
     } else {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
@@ -185,7 +194,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 && D == 64 ? 2 : 1) 
     typedef RowTile<T, D> RT;
     typedef BwdShape<T, D, WK> Sh;
     constexpr int NM = RT::RB / 32, NB = D / 32;
-    __shared__ __align__(1024) unsigned char lds[Sh::LDS];
+    // every tile an array of its own: reads of one then need not wait for the loads into another
+    __shared__ __align__(1024) unsigned char qa[Sh::TILE], ga[Sh::TILE], qb[Sh::NBUF == 2 ? Sh::TILE : 16], gb[Sh::NBUF == 2 ? Sh::TILE : 16];
     __shared__ __align__(16) float st[Sh::NBUF][2][Sh::ROWS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, half = lane >> 5;
@@ -215,13 +225,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 && D == 64 ? 2 : 1) 
     const unsigned char *gp = reinterpret_cast<const unsigned char *>(dO) + (int64_t)sq.q0 * a.do_row + (int64_t)hk * a.group * a.do_head;
     const float2 *const sp = stat + (int64_t)hk * a.total_q * a.group + (int64_t)sq.q0 * a.group;
     float2 sn = make_float2(-kNegInf, 0.f);
+    RowLoads<T, D, Sh::ROWS, 4> ql, gl;
+    ql.set(wave, a.q_row);
+    gl.set(wave, a.do_row);
     auto request = [&](int r0, unsigned char *qt, unsigned char *gt) __attribute__((always_inline)) {
-        auto place = [&](int r, int64_t row_b, int64_t head_b) {
-            const int rho = min(r0 + r, rows - 1), tok = row_token(a, rho);
-            return (int64_t)tok * row_b + (int64_t)(rho - tok * a.group) * head_b;
-        };
-        RT::template load<Sh::ROWS, 4>(qt, wave, [&](int r) { return qp + place(r, a.q_row, a.q_head); });
-        RT::template load<Sh::ROWS, 4>(gt, wave, [&](int r) { return gp + place(r, a.do_row, a.do_head); });
+        ql.rows(a, qp, a.q_row, a.q_head, r0, rows, qt);
+        gl.rows(a, gp, a.do_row, a.do_head, r0, rows, gt);
         if ((int)threadIdx.x < Sh::ROWS) sn = r0 + (int)threadIdx.x < rend ? sp[r0 + threadIdx.x] : make_float2(-kNegInf, 0.f);  // rows past the end: weights of zero
     };
     auto park = [&](int b) __attribute__((always_inline)) {
@@ -239,12 +248,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 && D == 64 ? 2 : 1) 
 #pragma unroll
         for (int t = 0; t < Sh::RT; ++t) {
             const int sub = (WK == 1 ? 0 : wave * 32) + 32 * t;
-            floatx16_t s = zero16(), dp = zero16();
-#pragma unroll
-            for (int m = 0; m < NM; ++m) {
-                s = product(row_frag<T, D>(qt, sub + n, m, half), kf[m], s);
-                dp = product(row_frag<T, D>(gt, sub + n, m, half), vf[m], dp);
-            }
+            floatx16_t s, dp;
+            tile_scores2<T, D>(qt, gt, sub + n, kf, vf, s, dp);
             if (edge) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = key <= row_token(a, r0 + sub + 8 * (i >> 2) + 4 * half + (i & 3)) + past ? s[i] : kNegInf;
@@ -260,33 +265,33 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 && D == 64 ? 2 : 1) 
                     dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - d[i]);
                 }
             }
-            weighted_rows<D>(gt, sub, s, dv, (const T *)nullptr);
-            weighted_rows<D>(qt, sub, dp, dk, (const T *)nullptr);
+            weighted_rows<T, D>(gt, sub, s, dv);
+            weighted_rows<T, D>(qt, sub, dp, dk);
         }
     };
     if (rbeg < rend) {
         if constexpr (Sh::NBUF == 2) {
-            unsigned char *const qa = lds, *const ga = lds + Sh::TILE, *const qb = lds + 2 * Sh::TILE, *const gb = lds + 3 * Sh::TILE;
             request(rbeg, qa, ga);
             park(0);
             for (int r0 = rbeg; r0 < rend; r0 += 2 * Sh::ROWS) {
                 wait_loads_and_sync();
                 if (r0 + Sh::ROWS < rend) request(r0 + Sh::ROWS, qb, gb);
                 tile(r0, qa, ga, 0);
-                if (r0 + Sh::ROWS >= rend) break;
-                park(1);
-                wait_loads_and_sync();
-                if (r0 + 2 * Sh::ROWS < rend) request(r0 + 2 * Sh::ROWS, qa, ga);
-                tile(r0 + Sh::ROWS, qb, gb, 1);
-                if (r0 + 2 * Sh::ROWS < rend) park(0);
+                if (r0 + Sh::ROWS < rend) {
+                    park(1);
+                    wait_loads_and_sync();
+                    if (r0 + 2 * Sh::ROWS < rend) request(r0 + 2 * Sh::ROWS, qa, ga);
+                    tile(r0 + Sh::ROWS, qb, gb, 1);
+                    if (r0 + 2 * Sh::ROWS < rend) park(0);
+                }
             }
         } else {
             for (int r0 = rbeg; r0 < rend; r0 += Sh::ROWS) {
                 __syncthreads();
-                request(r0, lds, lds + Sh::TILE);
+                request(r0, qa, ga);
                 park(0);
                 wait_loads_and_sync();
-                tile(r0, lds, lds + Sh::TILE, 0);
+                tile(r0, qa, ga, 0);
             }
         }
     }
@@ -304,8 +309,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 && D == 64 ? 2 : 1) 
         else store4(vop + ch, x, y, z, w);
     };
     if constexpr (WK > 1) {
-        join_waves<D>(reinterpret_cast<float *>(lds), dk, wave, put_k);
-        join_waves<D>(reinterpret_cast<float *>(lds), dv, wave, put_v);
+        auto area = [&](int w) __attribute__((always_inline)) {
+            return reinterpret_cast<float *>(Sh::NBUF == 2 ? (w == 0 ? qa : w == 1 ? ga : w == 2 ? qb : gb) : (w < 2 ? qa : ga) + (w & 1) * (Sh::TILE / 2));
+        };
+        join_waves<D>(area, dk, wave, put_k);
+        join_waves<D>(area, dv, wave, put_v);
     } else {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
@@ -316,6 +324,142 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 && D == 64 ? 2 : 1) 
                 put_v(ch, dv[nb][4 * g], dv[nb][4 * g + 1], dv[nb][4 * g + 2], dv[nb][4 * g + 3]);
             }
     }
+}
+
+// The same with half the registers a wave: two waves own the same 32 keys, form S and dP of 32 of a tile's 64 rows each, hand each other the
+// weights the other one sums -- a lane's weights go to the same lane of the other wave -- and the first sums dV, the second dK.
+template <typename T, int D>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void packed_dkdv_pair_kernel(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V, const T *__restrict__ dO,
+                                                                  const float2 *__restrict__ stat, T *__restrict__ dK, T *__restrict__ dV,
+                                                                  float *__restrict__ part_k, float *__restrict__ part_v, PackedArgs a)
+{
+    typedef RowTile<T, D> RT;
+    constexpr int NM = RT::RB / 32, NB = D / 32, OWN = kPairKeys, ROWS = PairShape<T, D>::ROWS, TILE = ROWS * RT::RB, WP = Weights<T>::PIECES;
+    static_assert(ROWS == 64, "32 rows of a tile for either wave of a pair");
+    // every tile an array of its own: reads of one then need not wait for the loads into another
+    __shared__ __align__(1024) unsigned char qa[TILE], ga[TILE], qb[PairShape<T, D>::NBUF == 2 ? TILE : 16], gb[PairShape<T, D>::NBUF == 2 ? TILE : 16];
+    __shared__ __align__(16) uint4 hand[4][WP][64];
+    __shared__ __align__(16) float st[PairShape<T, D>::NBUF][2][ROWS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), role = wave & 1;
+    const int n = lane & 31, half = lane >> 5;
+    const int hk = blockIdx.x % a.Hkv, slot = blockIdx.x / a.Hkv, split = blockIdx.y;
+    const int si = __builtin_amdgcn_readfirstlane(find_sequence(a.cu_k, a.n_seq, a.total_k, 1, OWN, slot));
+    const Sequence sq = read_sequence(a, si);
+    const int key0 = (slot - first_slot(a.cu_k[si], a.total_k, 1, OWN, si)) * OWN;
+    if (key0 < 0 || key0 >= sq.nk) return;
+    const int rows = sq.nq * a.group, past = sq.nk - sq.nq;
+    const int key = key0 + (wave >> 1) * 32 + n, kc = min(key, sq.nk - 1);
+    int rbeg = split * a.chunk;
+    const int rend = a.chunk ? min(rows, rbeg + a.chunk) : rows;
+    if (a.chunk && rbeg >= rows && split > 0) return;  // no such piece of this sequence
+    if (a.causal) rbeg = max(rbeg, max(0, key0 - past) * a.group / ROWS * ROWS);  // rows before see none of these keys
+
+    Frag<T> kf[NM], vf[NM];
+    {
+        const unsigned char *kp = reinterpret_cast<const unsigned char *>(K) + (int64_t)(sq.k0 + kc) * a.k_row + (int64_t)hk * a.k_head;
+        const unsigned char *vp = reinterpret_cast<const unsigned char *>(V) + (int64_t)(sq.k0 + kc) * a.v_row + (int64_t)hk * a.v_head;
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+            kf[m] = *reinterpret_cast<const Frag<T> *>(kp + (2 * m + half) * 16);
+            vf[m] = *reinterpret_cast<const Frag<T> *>(vp + (2 * m + half) * 16);
+        }
+    }
+    const unsigned char *qp = reinterpret_cast<const unsigned char *>(Q) + (int64_t)sq.q0 * a.q_row + (int64_t)hk * a.group * a.q_head;
+    const unsigned char *gp = reinterpret_cast<const unsigned char *>(dO) + (int64_t)sq.q0 * a.do_row + (int64_t)hk * a.group * a.do_head;
+    const float2 *const sp = stat + (int64_t)hk * a.total_q * a.group + (int64_t)sq.q0 * a.group;
+    float2 sn = make_float2(-kNegInf, 0.f);
+    RowLoads<T, D, ROWS, 4> ql, gl;
+    ql.set(wave, a.q_row);
+    gl.set(wave, a.do_row);
+    auto request = [&](int r0, unsigned char *qt, unsigned char *gt) __attribute__((always_inline)) {
+        ql.rows(a, qp, a.q_row, a.q_head, r0, rows, qt);
+        gl.rows(a, gp, a.do_row, a.do_head, r0, rows, gt);
+        if ((int)threadIdx.x < ROWS) sn = r0 + (int)threadIdx.x < rend ? sp[r0 + threadIdx.x] : make_float2(-kNegInf, 0.f);  // rows past the end: weights of zero
+    };
+    auto park = [&](int b) __attribute__((always_inline)) {
+        if ((int)threadIdx.x < ROWS) {
+            st[b][0][threadIdx.x] = sn.x;
+            st[b][1][threadIdx.x] = sn.y;
+        }
+    };
+    const float c = a.scale * kLog2e;
+    floatx16_t acc[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) acc[nb] = zero16();
+    auto tile = [&](int r0, const unsigned char *qt, const unsigned char *gt, int b) __attribute__((always_inline)) {
+        const int sub = role * 32;
+        floatx16_t s, dp;
+        tile_scores2<T, D>(qt, gt, sub + n, kf, vf, s, dp);
+        if (a.causal && key0 + OWN > row_token(a, r0) + past + 1) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = key <= row_token(a, r0 + sub + 8 * (i >> 2) + 4 * half + (i & 3)) + past ? s[i] : kNegInf;
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float4 l2 = *reinterpret_cast<const float4 *>(&st[b][0][sub + 8 * g + 4 * half]);
+            const float4 dl = *reinterpret_cast<const float4 *>(&st[b][1][sub + 8 * g + 4 * half]);
+            const float l[4] = {l2.x, l2.y, l2.z, l2.w}, d[4] = {dl.x, dl.y, dl.z, dl.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[4 * g + i] = fast_exp2(fmaf(s[4 * g + i], c, -l[i]));
+                dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - d[i]);
+            }
+        }
+        Weights<T> p, ds, mine, other;
+        p.set(s);
+        ds.set(dp);
+#pragma unroll
+        for (int i = 0; i < WP; ++i) {
+            const uint4 x = p.piece(i), y = ds.piece(i);
+            hand[wave][i][lane] = role ? x : y;
+            mine.set_piece(i, role ? y : x);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < WP; ++i) other.set_piece(i, hand[wave ^ 1][i][lane]);
+        const unsigned char *const rt = role ? qt : gt;
+        weighted_rows<D>(rt, sub, mine, acc);
+        weighted_rows<D>(rt, 32 - sub, other, acc);
+    };
+    if (rbeg < rend) {
+        if constexpr (PairShape<T, D>::NBUF == 2) {
+            request(rbeg, qa, ga);
+            park(0);
+            for (int r0 = rbeg; r0 < rend; r0 += 2 * ROWS) {
+                wait_loads_and_sync();
+                if (r0 + ROWS < rend) request(r0 + ROWS, qb, gb);
+                tile(r0, qa, ga, 0);
+                if (r0 + ROWS < rend) {
+                    park(1);
+                    wait_loads_and_sync();
+                    if (r0 + 2 * ROWS < rend) request(r0 + 2 * ROWS, qa, ga);
+                    tile(r0 + ROWS, qb, gb, 1);
+                    if (r0 + 2 * ROWS < rend) park(0);
+                }
+            }
+        } else {
+            for (int r0 = rbeg; r0 < rend; r0 += ROWS) {
+                __syncthreads();
+                request(r0, qa, ga);
+                park(0);
+                wait_loads_and_sync();
+                tile(r0, qa, ga, 0);
+            }
+        }
+    }
+    if (key >= sq.nk) return;
+    const float f = role ? a.scale : 1.f;
+    float *const pp = (role ? part_k : part_v) + (((int64_t)(sq.k0 + key) * a.Hkv + hk) * a.splits + split) * D;
+    T *const op = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(role ? dK : dV) + (int64_t)(sq.k0 + key) * (role ? a.dk_row : a.dv_row) +
+                                        (int64_t)hk * (role ? a.dk_head : a.dv_head));
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int ch = 32 * nb + 8 * g + 4 * half;
+            if (a.splits > 1) store4(pp + ch, acc[nb][4 * g] * f, acc[nb][4 * g + 1] * f, acc[nb][4 * g + 2] * f, acc[nb][4 * g + 3] * f);
+            else store4(op + ch, acc[nb][4 * g] * f, acc[nb][4 * g + 1] * f, acc[nb][4 * g + 2] * f, acc[nb][4 * g + 3] * f);
+        }
 }
 
 // Sums of the pieces.  KEYS: of dK and dV (blockIdx.y), pieces of the rows; else of dQ, pieces of the keys.
@@ -360,9 +504,11 @@ dsv_status launch_dq(const PackedArgs &a, const T *Q, const T *K, const T *V, co
 template <typename T, int D, int WK>
 dsv_status launch_dkdv(const PackedArgs &a, const T *Q, const T *K, const T *V, const T *dO, const float2 *stat, T *dK, T *dV, float *part, hipStream_t st)
 {
-    const int64_t slots = tile_slots(a.total_k, 1, BwdShape<T, D, WK>::OWN, a.n_seq);
+    const int64_t slots = tile_slots(a.total_k, 1, WK == 1 ? kPairKeys : BwdShape<T, D, WK>::OWN, a.n_seq);
+    const dim3 grid((unsigned)(slots * a.Hkv), a.splits);
     float *const part_v = part + packed_dkdv_bytes(a.total_k, a.Hkv, D, a.splits) / 8;
-    packed_dkdv_kernel<T, D, WK><<<dim3((unsigned)(slots * a.Hkv), a.splits), 256, 0, st>>>(Q, K, V, dO, stat, dK, dV, part, part_v, a);
+    if constexpr (WK == 1) packed_dkdv_pair_kernel<T, D><<<grid, 256, 0, st>>>(Q, K, V, dO, stat, dK, dV, part, part_v, a);
+    else packed_dkdv_kernel<T, D, WK><<<grid, 256, 0, st>>>(Q, K, V, dO, stat, dK, dV, part, part_v, a);
     DSV_LAUNCH_CHECK();
     if (a.splits > 1) {
         packed_sum_kernel<T, D, true><<<dim3(merge_blocks<D / 4>(a.total_k, a.Hkv), 2), 256, 0, st>>>(part, part_v, dK, dV, a);

@@ -16,7 +16,6 @@ template <typename T, int D, int WK> struct FwdShape {
     static constexpr int ROWS = WK == 1 ? 128 : 32, KEYS = WK == 1 ? 64 : 128, KT = KEYS / 32 / WK;
     static constexpr int TILE = KEYS * D * (int)sizeof(T);
     static constexpr int NBUF = 2 * 2 * TILE <= 128 * 1024 ? 2 : 1;
-    static constexpr int LDS = NBUF * 2 * TILE;
 };
 
 template <typename T, int D, int WK>
@@ -27,7 +26,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
     typedef RowTile<T, D> RT;
     typedef FwdShape<T, D, WK> Sh;
     constexpr int NM = RT::RB / 32, NB = D / 32, KT = Sh::KT;
-    __shared__ __align__(1024) unsigned char lds[Sh::LDS];
+    // every tile an array of its own: reads of one then need not wait for the loads into another
+    __shared__ __align__(1024) unsigned char ka[Sh::TILE], va[Sh::TILE], kb[Sh::NBUF == 2 ? Sh::TILE : 16], vb[Sh::NBUF == 2 ? Sh::TILE : 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, half = lane >> 5;
     // heads side by side: with as many heads as XCDs, or a multiple or a divisor of that, a head's keys stay in the L2 of one or a few of them;
@@ -56,9 +56,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
     }
     const unsigned char *kp = reinterpret_cast<const unsigned char *>(K) + (int64_t)sq.k0 * a.k_row + (int64_t)hk * a.k_head;
     const unsigned char *vp = reinterpret_cast<const unsigned char *>(V) + (int64_t)sq.k0 * a.v_row + (int64_t)hk * a.v_head;
-    auto request = [&](int k0, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {  // rows past the end repeat the last one
-        RT::template load<Sh::KEYS, 4>(kt, wave, [&](int r) { return kp + (int64_t)min(k0 + r, sq.nk - 1) * a.k_row; });
-        RT::template load<Sh::KEYS, 4>(vt, wave, [&](int r) { return vp + (int64_t)min(k0 + r, sq.nk - 1) * a.v_row; });
+    RowLoads<T, D, Sh::KEYS, 4> kl, vl;
+    kl.set(wave, a.k_row);
+    vl.set(wave, a.v_row);
+    auto request = [&](int k0, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
+        kl.keys(kp, a.k_row, k0, sq.nk, kt);
+        vl.keys(vp, a.v_row, k0, sq.nk, vt);
     };
 
     const float c = a.scale * kLog2e;
@@ -69,12 +72,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
     auto tile = [&](int k0, const unsigned char *kt, const unsigned char *vt) __attribute__((always_inline)) {
         const int sub = WK == 1 ? 0 : wave * 32;
         floatx16_t s[KT];
-#pragma unroll
-        for (int t = 0; t < KT; ++t) s[t] = zero16();
-#pragma unroll
-        for (int m = 0; m < NM; ++m)
-#pragma unroll
-            for (int t = 0; t < KT; ++t) s[t] = product(row_frag<T, D>(kt, sub + 32 * t + n, m, half), qf[m], s[t]);
+        tile_scores<T, D, KT>(kt, sub + n, qf, s);
         // the tile's last key is behind the end, or not seen by the wave's first row
         const bool edge = k0 + Sh::KEYS > kcut || (a.causal && k0 + Sh::KEYS > row_token(a, row0) + past + 1);
         if (edge) {
@@ -108,35 +106,39 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
                 s[t][i] = fast_exp2(fmaf(s[t][i], c, -mref));
                 l += s[t][i];
             }
-            weighted_rows<D>(vt, sub + 32 * t, s[t], acc, (const T *)nullptr);
+            weighted_rows<T, D>(vt, sub + 32 * t, s[t], acc);
         }
     };
     if (kbeg < kend) {
         if constexpr (Sh::NBUF == 2) {
-            unsigned char *const ka = lds, *const va = lds + Sh::TILE, *const kb = lds + 2 * Sh::TILE, *const vb = lds + 3 * Sh::TILE;
             request(kbeg, ka, va);
             for (int k0 = kbeg; k0 < kend; k0 += 2 * Sh::KEYS) {
                 wait_loads_and_sync();
                 if (k0 + Sh::KEYS < kend) request(k0 + Sh::KEYS, kb, vb);
                 tile(k0, ka, va);
-                if (k0 + Sh::KEYS >= kend) break;
-                wait_loads_and_sync();
-                if (k0 + 2 * Sh::KEYS < kend) request(k0 + 2 * Sh::KEYS, ka, va);
-                tile(k0 + Sh::KEYS, kb, vb);
+                if (k0 + Sh::KEYS < kend) {  // (a break here makes the compiler move all sums to other registers and back)
+                    wait_loads_and_sync();
+                    if (k0 + 2 * Sh::KEYS < kend) request(k0 + 2 * Sh::KEYS, ka, va);
+                    tile(k0 + Sh::KEYS, kb, vb);
+                }
             }
         } else {
             for (int k0 = kbeg; k0 < kend; k0 += Sh::KEYS) {
                 __syncthreads();
-                request(k0, lds, lds + Sh::TILE);
+                request(k0, ka, va);
                 wait_loads_and_sync();
-                tile(k0, lds, lds + Sh::TILE);
+                tile(k0, ka, va);
             }
         }
     }
     l = halves_sum(l);
     if constexpr (WK > 1) {  // the waves' sums over their keys, joined in LDS: wave w then holds channels 32 w / 4 .. of every row
+        __shared__ float sm[128], sl[128];
+        auto area = [&](int w) __attribute__((always_inline)) {  // 32 rows of D sums
+            return reinterpret_cast<float *>(Sh::NBUF == 2 ? (w == 0 ? ka : w == 1 ? va : w == 2 ? kb : vb) : (w < 2 ? ka : va) + (w & 1) * (Sh::TILE / 2));
+        };
+        static_assert(Sh::TILE / (Sh::NBUF == 2 ? 1 : 2) >= 32 * D * 4, "a wave's sums fit its part of the tiles");
         __syncthreads();
-        float *const sm = reinterpret_cast<float *>(lds), *const sl = sm + 128, *const sa = sm + 256;
         if (half == 0) {
             sm[wave * 32 + n] = mrun;
             sl[wave * 32 + n] = l;
@@ -150,12 +152,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
 #pragma unroll
         for (int w = 0; w < 4; ++w) l += sl[w * 32 + n] * fast_exp2(sm[w * 32 + n] - mref);
         const float f = fast_exp2(mrun - mref);
-        // channel by row, [wave][channel / 4][row][4]
+        // channel by row, [channel / 4][row][4]
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<float4 *>(sa + ((wave * (D / 4) + nb * 8 + 2 * g + half) * 32 + n) * 4) =
+                *reinterpret_cast<float4 *>(area(wave) + ((nb * 8 + 2 * g + half) * 32 + n) * 4) =
                     make_float4(acc[nb][4 * g] * f, acc[nb][4 * g + 1] * f, acc[nb][4 * g + 2] * f, acc[nb][4 * g + 3] * f);
         mrun = m2;
         __syncthreads();
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
             float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const float4 x = *reinterpret_cast<const float4 *>(sa + ((w * (D / 4) + g) * 32 + n) * 4);
+                const float4 x = *reinterpret_cast<const float4 *>(area(w) + (g * 32 + n) * 4);
                 v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
             }
             if (a.splits > 1) {
