@@ -332,7 +332,7 @@ DSV_API dsv_status dsv_profile_sparsity(const dsv_problem *p, const void *Q, con
  *     but no access outside the tensors.  Rows that belong to no sequence are left as they are, in every output, and may hold anything.
  *   - O_tail (bf16; NULL: not wanted; must be NULL for F32): bf16 [total_q, Hq, d], contiguous, what rounding O took away.  Given to the
  *     backward, it forms Delta from all 16 bits: gradients within 3e-3 of the exact ones (relative, in norm), where O alone leaves 3 to 6e-3.
- *   - scale: finite and > 0.  The weights enter the second product as bf16 (bf16 tensors), everything else is held in 32 bits.  The same
+ *   - scale: 1e-30 to 1e30.  The weights enter the second product as bf16 (bf16 tensors), everything else is held in 32 bits.  The same
  *     results from run to run, bit for bit.
  *   - Limits: Hkv divides Hq; total_q * Hq * (Hq / Hkv) < 2^32; total_q * Hq / 32 + n_seq * Hkv < 2^24, and so for total_k * Hkv;
  *     anything larger: DSV_EUNSUPPORTED.  total_q, total_k of 0 are accepted, the tensors may then be NULL.

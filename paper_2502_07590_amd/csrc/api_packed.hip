@@ -29,7 +29,7 @@ dsv_status check_packed(const dsv_packed *p, bool grad)
     if (p->n_seq < 1 || p->total_q < 0 || p->total_k < 0 || p->max_q < 0 || p->max_k < 0) return DSV_EINVAL;
     if (p->Hq < 1 || p->Hkv < 1 || p->Hq % p->Hkv) return DSV_EINVAL;
     if (p->causal != 0 && p->causal != 1) return DSV_EINVAL;
-    if (p->flags || !std::isfinite(p->scale) || !(p->scale > 0.f)) return DSV_EINVAL;
+    if (p->flags || !(p->scale >= 1e-30f && p->scale <= 1e30f)) return DSV_EINVAL;  // lse / scale and scale * log2(e) are finite
     if (!supported_dtype(p->dtype) || !supported_d(p->d)) return DSV_EUNSUPPORTED;
     const size_t es = esize(p->dtype);
     for (const dsv_rows *s : {&p->q, &p->k, &p->v, &p->o})
@@ -110,6 +110,7 @@ Walk walk_q(const dsv_packed &p) { return plan_walk((int64_t)p.total_q * (p.Hq /
 Walk walk_k(const dsv_packed &p)
 {
     const int64_t g = p.Hq / p.Hkv;
+    // (fp32 always takes the small tiles)
     return plan_walk(p.total_k, p.Hkv, p.n_seq, (int64_t)p.total_q * g, std::min(p.max_q, p.total_q) * g);
 }
 

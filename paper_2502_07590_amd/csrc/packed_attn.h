@@ -5,13 +5,13 @@
 // `group` rows, and the key-major sums of the backward run over the shared heads by themselves.
 #pragma once
 
+#include <type_traits>
+#include <utility>
+
 #include "stage2_core.h"
 
 namespace dsv {
 
-#ifndef DSV_PIN
-#define DSV_PIN 0x406
-#endif
 constexpr float kNegInf = -__builtin_inff();
 
 // A descriptor as the kernels read it; strides in bytes.
@@ -100,10 +100,12 @@ template <typename T, int D, int ROWS, int WAVES> struct RowLoads {
     }
     __device__ __forceinline__ void send(const unsigned char *base, const uint32_t (&at)[N], unsigned char *lds) const
     {
+        // by a buffer of all 32-bit offsets: as global loads, which the compiler takes for ones that may read LDS too, they would make every wait for
+        // an LDS read one for all of them
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(base), 0, -1, 0x00027000);
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + at[i]),
-                                             (__attribute__((address_space(3))) void *)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (i * WAVES + wave) * 1024), 16, (int)at[i], 0, 0, 0);
     }
     __device__ __forceinline__ void plain(int64_t row_b, int left, uint32_t (&at)[N]) const  // rows row_b apart, `left` of them to the end
     {
@@ -175,9 +177,13 @@ template <typename T, int D> __device__ __forceinline__ Frag<T> row_frag(const u
     return *reinterpret_cast<const Frag<T> *>(tile + RowTile<T, D>::at(r, 2 * m + half));
 }
 
-// Fragments are read two steps before the products that need them.  The order of reads and products is pinned -- left alone a read sinks to its
-// use, or all of them rise and spill -- while vector arithmetic may move between them.
-__device__ __forceinline__ void pin_order() { __builtin_amdgcn_sched_barrier(DSV_PIN); }
+// Operands are read some steps before the products that need them, and the order is pinned: left alone a read sinks to its use, or all of them
+// rise and spill.
+constexpr int kAhead = 3;  // steps of tile_scores; 2 and 4 are as fast
+constexpr int kRing = 6;   // operands of the dkdv kernel; 4 and 8 are as fast
+template <typename F, int... K> __device__ __forceinline__ void static_for_(F f, std::integer_sequence<int, K...>) { (f(std::integral_constant<int, K>{}), ...); }
+template <int N, typename F> __device__ __forceinline__ void static_for(F f) { static_for_(f, std::make_integer_sequence<int, N>{}); }  // f(0) .. f(N - 1), as constants
+__device__ __forceinline__ void pin_order() { __builtin_amdgcn_sched_barrier(0); }
 
 // s[t] = rows r + 32 t of a tile by the own rows
 template <typename T, int D, int KT>
@@ -185,46 +191,47 @@ __device__ __forceinline__ void tile_scores(const unsigned char *tile, int r, co
 {
     constexpr int NM = D * (int)sizeof(T) / 32;
     const int half = (threadIdx.x & 63) >> 5;
-    Frag<T> f[2][KT];
+    Frag<T> f[kAhead][KT];
     auto fetch = [&](int m) __attribute__((always_inline)) {
 #pragma unroll
-        for (int t = 0; t < KT; ++t) f[m & 1][t] = row_frag<T, D>(tile, r + 32 * t, m, half);
+        for (int t = 0; t < KT; ++t) f[m % kAhead][t] = row_frag<T, D>(tile, r + 32 * t, m, half);
     };
 #pragma unroll
     for (int t = 0; t < KT; ++t) s[t] = zero16();
-    fetch(0);
-    fetch(1);
+#pragma unroll
+    for (int m = 0; m < kAhead; ++m) fetch(m);
     pin_order();
 #pragma unroll
     for (int m = 0; m < NM; ++m) {
 #pragma unroll
-        for (int t = 0; t < KT; ++t) s[t] = product(f[m & 1][t], own[m], s[t]);
-        if (m + 2 < NM) fetch(m + 2);
+        for (int t = 0; t < KT; ++t) s[t] = product(f[m % kAhead][t], own[m], s[t]);
+        if (m + kAhead < NM) fetch(m + kAhead);
         pin_order();
     }
 }
-// The same of row r of two tiles, each by own rows of its own.
-template <typename T, int D>
+// The same of row r of two tiles, each by own rows of its own; between(m) is done between the products, m = 0 .. NM - 1.
+template <typename T, int D, typename F>
 __device__ __forceinline__ void tile_scores2(const unsigned char *t1, const unsigned char *t2, int r, const Frag<T> (&own1)[D * sizeof(T) / 32],
-                                             const Frag<T> (&own2)[D * sizeof(T) / 32], floatx16_t &s1, floatx16_t &s2)
+                                             const Frag<T> (&own2)[D * sizeof(T) / 32], floatx16_t &s1, floatx16_t &s2, F between)
 {
     constexpr int NM = D * (int)sizeof(T) / 32;
     const int half = (threadIdx.x & 63) >> 5;
-    Frag<T> f[2][2];
+    Frag<T> f[kAhead][2];
     auto fetch = [&](int m) __attribute__((always_inline)) {
-        f[m & 1][0] = row_frag<T, D>(t1, r, m, half);
-        f[m & 1][1] = row_frag<T, D>(t2, r, m, half);
+        f[m % kAhead][0] = row_frag<T, D>(t1, r, m, half);
+        f[m % kAhead][1] = row_frag<T, D>(t2, r, m, half);
     };
     s1 = zero16();
     s2 = zero16();
-    fetch(0);
-    fetch(1);
+#pragma unroll
+    for (int m = 0; m < kAhead; ++m) fetch(m);
     pin_order();
 #pragma unroll
     for (int m = 0; m < NM; ++m) {
-        s1 = product(f[m & 1][0], own1[m], s1);
-        s2 = product(f[m & 1][1], own2[m], s2);
-        if (m + 2 < NM) fetch(m + 2);
+        s1 = product(f[m % kAhead][0], own1[m], s1);
+        s2 = product(f[m % kAhead][1], own2[m], s2);
+        if (m + kAhead < NM) fetch(m + kAhead);
+        between(m);
         pin_order();
     }
 }
@@ -234,13 +241,25 @@ __device__ __forceinline__ void tile_scores2(const unsigned char *t1, const unsi
 template <typename T> struct Weights;
 template <> struct Weights<bf16_t> {
     bf16x8_t v[2];
-    static constexpr int PIECES = 2;
     __device__ __forceinline__ void set(const floatx16_t &w)
     {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
             v[s] = __builtin_bit_cast(bf16x8_t, make_uint4(pack_bf16x2(w[8 * s], w[8 * s + 1]), pack_bf16x2(w[8 * s + 2], w[8 * s + 3]),
                                                            pack_bf16x2(w[8 * s + 4], w[8 * s + 5]), pack_bf16x2(w[8 * s + 6], w[8 * s + 7])));
+    }
+    __device__ __forceinline__ float sum(float x) const  // x + all of them, as they were rounded
+    {
+        const bf16x2_t one = __builtin_bit_cast(bf16x2_t, 0x3F803F80u);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const uint4 h = __builtin_bit_cast(uint4, v[s]);
+            x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, h.x), one, x, false);
+            x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, h.y), one, x, false);
+            x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, h.z), one, x, false);
+            x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, h.w), one, x, false);
+        }
+        return x;
     }
     // what the rounding of w to *this left
     __device__ __forceinline__ void set_tail(const floatx16_t &w, const Weights &head)
@@ -258,64 +277,118 @@ template <> struct Weights<bf16_t> {
         }
         set(t);
     }
-    __device__ __forceinline__ uint4 piece(int i) const { return __builtin_bit_cast(uint4, v[i]); }
-    __device__ __forceinline__ void set_piece(int i, uint4 x) { v[i] = __builtin_bit_cast(bf16x8_t, x); }
+    __device__ __forceinline__ void set_pair(int i, float a, float b)  // weights i, i + 1
+    {
+        uint4 x = __builtin_bit_cast(uint4, v[i >> 3]);
+        const uint32_t p = pack_bf16x2(a, b);
+        if ((i & 6) == 0) x.x = p;
+        else if ((i & 6) == 2) x.y = p;
+        else if ((i & 6) == 4) x.z = p;
+        else x.w = p;
+        v[i >> 3] = __builtin_bit_cast(bf16x8_t, x);
+    }
 };
 template <> struct Weights<float> {
     floatx16_t v;
-    static constexpr int PIECES = 4;
     __device__ __forceinline__ void set(const floatx16_t &w) { v = w; }
-    __device__ __forceinline__ uint4 piece(int i) const
+    __device__ __forceinline__ void set_pair(int i, float a, float b)
     {
-        return make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
-    }
-    __device__ __forceinline__ void set_piece(int i, uint4 x)
-    {
-        v[4 * i] = __uint_as_float(x.x); v[4 * i + 1] = __uint_as_float(x.y); v[4 * i + 2] = __uint_as_float(x.z); v[4 * i + 3] = __uint_as_float(x.w);
+        v[i] = a;
+        v[i + 1] = b;
     }
 };
 
-// acc[nb] (channels 32 nb .. + 31 by own rows) += sum over tile rows r0 .. r0 + 31 of row[channel] * w
-template <int D> __device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const Weights<bf16_t> &w, floatx16_t (&acc)[D / 32])
-{
+// acc[nb] (channels 32 nb .. + 31 by own rows) += sum over tile rows r0 .. r0 + 31 of row[channel] * w, in STEPS steps: operands of step i are read
+// by fetch(i), at least AHEAD steps before step(i).
+template <typename T, int D> struct RowSum;
+template <int D> struct RowSum<bf16_t, D> {
     typedef RowTile<bf16_t, D> RT;
-    constexpr int NB = D / 32;
-    const int lane = threadIdx.x & 63, half = lane >> 5, e = (lane >> 2) & 3, q = lane & 3, b4 = (lane >> 4) & 1;
-    const int r = r0 + 4 * half + e;
-    bf16x8_t f[2];
-    auto fetch = [&](int i) __attribute__((always_inline)) {
-        const int s = i / NB, p = 4 * (i % NB) + 2 * b4 + (q >> 1), sub = (q & 1) * 8;
-        f[i & 1] = tr_frag(tile + RT::at(r + 16 * s, p) + sub, tile + RT::at(r + 16 * s + 8, p) + sub);
+    static constexpr int NB = D / 32, STEPS = 2 * NB, AHEAD = 4;
+    typedef bf16x8_t Operand;
+    __device__ __forceinline__ static Operand fetch(const unsigned char *tile, int r0, int i)
+    {
+        const int lane = threadIdx.x & 63, half = lane >> 5, e = (lane >> 2) & 3, q = lane & 3, b4 = (lane >> 4) & 1;
+        const int r = r0 + 4 * half + e + 16 * (i / NB), p = 4 * (i % NB) + 2 * b4 + (q >> 1), sub = (q & 1) * 8;
+        return tr_frag(tile + RT::at(r, p) + sub, tile + RT::at(r + 8, p) + sub);
+    }
+    __device__ __forceinline__ static void step(int i, const Operand &f, const Weights<bf16_t> &w, floatx16_t (&acc)[NB])
+    {
+        acc[i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, w.v[i / NB], acc[i % NB], 0, 0, 0);
+    }
+};
+template <int D> struct RowSum<float, D> {
+    typedef RowTile<float, D> RT;
+    static constexpr int NB = D / 32, STEPS = 16, AHEAD = 2;
+    struct Operand {
+        float v[NB];
     };
-    fetch(0);
-    fetch(1);
+    __device__ __forceinline__ static Operand fetch(const unsigned char *tile, int r0, int i)
+    {
+        const int lane = threadIdx.x & 63, half = lane >> 5, n = lane & 31, r = r0 + 8 * (i >> 2) + 4 * half + (i & 3);
+        Operand f;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) f.v[nb] = *reinterpret_cast<const float *>(tile + RT::at(r, 8 * nb + (n >> 2)) + (n & 3) * 4);
+        return f;
+    }
+    __device__ __forceinline__ static void step(int i, const Operand &f, const Weights<float> &w, floatx16_t (&acc)[NB])
+    {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) acc[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(f.v[nb], w.v[i], acc[nb], 0, 0, 0);
+    }
+};
+// KT times 32 rows from r0; between(i) is done between the products, i = 0 .. KT STEPS - 1.
+template <typename T, int D, int KT, typename F>
+__device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const Weights<T> (&w)[KT], floatx16_t (&acc)[D / 32], F between)
+{
+    typedef RowSum<T, D> RS;
+    constexpr int N = KT * RS::STEPS, A = RS::AHEAD;
+    typename RS::Operand f[A];
+    auto fetch = [&](int i) __attribute__((always_inline)) { f[i % A] = RS::fetch(tile, r0 + 32 * (i / RS::STEPS), i % RS::STEPS); };
+#pragma unroll
+    for (int i = 0; i < A; ++i) fetch(i);
     pin_order();
 #pragma unroll
-    for (int i = 0; i < 2 * NB; ++i) {
-        acc[i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i & 1], w.v[i / NB], acc[i % NB], 0, 0, 0);
-        if (i + 2 < 2 * NB) fetch(i + 2);
+    for (int i = 0; i < N; ++i) {
+        RS::step(i % RS::STEPS, f[i % A], w[i / RS::STEPS], acc);
+        if (i + A < N) fetch(i + A);
+        between(i);
         pin_order();
     }
 }
-template <int D> __device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const Weights<float> &w, floatx16_t (&acc)[D / 32])
+template <typename T, int D> __device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const Weights<T> &w, floatx16_t (&acc)[D / 32])
 {
-    typedef RowTile<float, D> RT;
-    const int lane = threadIdx.x & 63, half = lane >> 5, n = lane & 31;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int r = r0 + 8 * (i >> 2) + 4 * half + (i & 3);
-#pragma unroll
-        for (int nb = 0; nb < D / 32; ++nb) {
-            const float v = *reinterpret_cast<const float *>(tile + RT::at(r, 8 * nb + (n >> 2)) + (n & 3) * 4);
-            acc[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w.v[i], acc[nb], 0, 0, 0);
-        }
-    }
+    const Weights<T> one[1] = {w};
+    weighted_rows<T, D, 1>(tile, r0, one, acc, [](int) {});
 }
 template <typename T, int D> __device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const floatx16_t &w, floatx16_t (&acc)[D / 32])
 {
     Weights<T> x;
     x.set(w);
-    weighted_rows<D>(tile, r0, x, acc);
+    weighted_rows<T, D>(tile, r0, x, acc);
+}
+
+// Weights as two bf16 words, 16 significant bits; the operands are read once for both.
+template <typename T, int D> __device__ __forceinline__ void precise_weighted_rows(const unsigned char *tile, int r0, const floatx16_t &w, floatx16_t (&acc)[D / 32])
+{
+    if constexpr (sizeof(T) == 4) {
+        weighted_rows<T, D>(tile, r0, w, acc);
+    } else {
+        typedef RowSum<T, D> RS;
+        Weights<T> head, tail;
+        head.set(w);
+        tail.set_tail(w, head);
+        typename RS::Operand f[RS::AHEAD];
+#pragma unroll
+        for (int i = 0; i < RS::AHEAD; ++i) f[i] = RS::fetch(tile, r0, i);
+        pin_order();
+#pragma unroll
+        for (int i = 0; i < RS::STEPS; ++i) {
+            RS::step(i, f[i % RS::AHEAD], tail, acc);
+            RS::step(i, f[i % RS::AHEAD], head, acc);
+            if (i + RS::AHEAD < RS::STEPS) f[i % RS::AHEAD] = RS::fetch(tile, r0, i + RS::AHEAD);
+            pin_order();
+        }
+    }
 }
 
 // Value of the other half's lane with the same column, combined by max or sum.

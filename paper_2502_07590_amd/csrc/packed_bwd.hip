@@ -47,11 +47,6 @@ template <typename T, int D, int WK> struct BwdShape {
     static_assert(TILE / (NBUF == 2 ? 1 : 2) >= 32 * D * 4, "a wave's sums fit its part of the tiles");
 };
 
-constexpr int kPairKeys = 64;
-template <typename T, int D> struct PairShape {
-    static constexpr int ROWS = 64, NBUF = 2 * 2 * ROWS * D * (int)sizeof(T) <= 128 * 1024 ? 2 : 1;
-};
-
 // The four waves' sums of the same 32 rows, joined in LDS: thread t's share is channels 4 g .. 4 g + 3 of row t % 32 for g = t / 32, + 8, ...
 // area(w): where wave w's 32 rows of D sums go.
 template <int D, typename A, typename F> __device__ __forceinline__ void join_waves(A area, const floatx16_t (&acc)[D / 32], int wave, F put)
@@ -133,7 +128,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
         for (int t = 0; t < Sh::RT; ++t) {
             const int sub = (WK == 1 ? 0 : wave * 32) + 32 * t;
             floatx16_t s, dp;
-            tile_scores2<T, D>(kt, vt, sub + n, qf, gf, s, dp);
+            tile_scores2<T, D>(kt, vt, sub + n, qf, gf, s, dp, [](int) {});
             if (edge) {
                 const int lim = min(seen, kcut) - k0 - sub - 4 * half;
 #pragma unroll
@@ -141,7 +136,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = fast_exp2(fmaf(s[i], c, -rs.x)) * (dp[i] - rs.y);
-            weighted_rows<T, D>(kt, sub, s, acc);
+            precise_weighted_rows<T, D>(kt, sub, s, acc);
         }
     };
     if (kbeg < kend) {
@@ -186,13 +181,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
     }
 }
 
-template <typename T, int D, int WK>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 && D == 64 ? 2 : 1) void packed_dkdv_kernel(
+// Calls of few keys, and fp32: 32 keys a block, the four waves take 32 rows each of a tile of 128.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 1) void packed_dkdv_few_kernel(
     const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V, const T *__restrict__ dO, const float2 *__restrict__ stat, T *__restrict__ dK,
     T *__restrict__ dV, float *__restrict__ part_k, float *__restrict__ part_v, PackedArgs a)
 {
     typedef RowTile<T, D> RT;
-    typedef BwdShape<T, D, WK> Sh;
+    typedef BwdShape<T, D, 4> Sh;
     constexpr int NM = RT::RB / 32, NB = D / 32;
     // every tile an array of its own: reads of one then need not wait for the loads into another
     __shared__ __align__(1024) unsigned char qa[Sh::TILE], ga[Sh::TILE], qb[Sh::NBUF == 2 ? Sh::TILE : 16], gb[Sh::NBUF == 2 ? Sh::TILE : 16];
@@ -205,7 +201,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 && D == 64 ? 2 : 1) 
     const int key0 = (slot - first_slot(a.cu_k[si], a.total_k, 1, Sh::OWN, si)) * Sh::OWN;
     if (key0 < 0 || key0 >= sq.nk) return;
     const int rows = sq.nq * a.group, past = sq.nk - sq.nq;
-    const int key = key0 + (WK == 1 ? wave * 32 : 0) + n, kc = min(key, sq.nk - 1);
+    const int key = key0 + n, kc = min(key, sq.nk - 1);
     int rbeg = split * a.chunk;
     const int rend = a.chunk ? min(rows, rbeg + a.chunk) : rows;
     if (a.chunk && rbeg >= rows && split > 0) return;  // no such piece of this sequence
@@ -243,16 +239,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 && D == 64 ? 2 : 1) 
     floatx16_t dk[NB], dv[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) dk[nb] = dv[nb] = zero16();
+    const int first_seen = a.causal ? min(max(key - past, 0), sq.nq) * a.group : 0;  // key j is seen by rows from (j - past) * group on
     auto tile = [&](int r0, const unsigned char *qt, const unsigned char *gt, int b) __attribute__((always_inline)) {
         const bool edge = a.causal && key0 + Sh::OWN > row_token(a, r0) + past + 1;
-#pragma unroll
-        for (int t = 0; t < Sh::RT; ++t) {
-            const int sub = (WK == 1 ? 0 : wave * 32) + 32 * t;
+        const int sub = wave * 32;
+        {
             floatx16_t s, dp;
-            tile_scores2<T, D>(qt, gt, sub + n, kf, vf, s, dp);
+            tile_scores2<T, D>(qt, gt, sub + n, kf, vf, s, dp, [](int) {});
             if (edge) {
+                const int lim = first_seen - r0 - sub - 4 * half;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = key <= row_token(a, r0 + sub + 8 * (i >> 2) + 4 * half + (i & 3)) + past ? s[i] : kNegInf;
+                for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) >= lim ? s[i] : kNegInf;
             }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
@@ -308,51 +305,41 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 && D == 64 ? 2 : 1) 
         if (a.splits > 1) store4(part_v + pid + ch, x, y, z, w);
         else store4(vop + ch, x, y, z, w);
     };
-    if constexpr (WK > 1) {
-        auto area = [&](int w) __attribute__((always_inline)) {
-            return reinterpret_cast<float *>(Sh::NBUF == 2 ? (w == 0 ? qa : w == 1 ? ga : w == 2 ? qb : gb) : (w < 2 ? qa : ga) + (w & 1) * (Sh::TILE / 2));
-        };
-        join_waves<D>(area, dk, wave, put_k);
-        join_waves<D>(area, dv, wave, put_v);
-    } else {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int ch = 32 * nb + 8 * g + 4 * half;
-                put_k(ch, dk[nb][4 * g], dk[nb][4 * g + 1], dk[nb][4 * g + 2], dk[nb][4 * g + 3]);
-                put_v(ch, dv[nb][4 * g], dv[nb][4 * g + 1], dv[nb][4 * g + 2], dv[nb][4 * g + 3]);
-            }
-    }
+    auto area = [&](int w) __attribute__((always_inline)) {
+        return reinterpret_cast<float *>(Sh::NBUF == 2 ? (w == 0 ? qa : w == 1 ? ga : w == 2 ? qb : gb) : (w < 2 ? qa : ga) + (w & 1) * (Sh::TILE / 2));
+    };
+    join_waves<D>(area, dk, wave, put_k);
+    join_waves<D>(area, dv, wave, put_v);
 }
 
-// The same with half the registers a wave: two waves own the same 32 keys, form S and dP of 32 of a tile's 64 rows each, hand each other the
-// weights the other one sums -- a lane's weights go to the same lane of the other wave -- and the first sums dV, the second dK.
-template <typename T, int D>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void packed_dkdv_pair_kernel(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V, const T *__restrict__ dO,
-                                                                  const float2 *__restrict__ stat, T *__restrict__ dK, T *__restrict__ dV,
-                                                                  float *__restrict__ part_k, float *__restrict__ part_v, PackedArgs a)
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkdv_kernel(
+    const bf16_t *__restrict__ Q, const bf16_t *__restrict__ K, const bf16_t *__restrict__ V, const bf16_t *__restrict__ dO, const float2 *__restrict__ stat, bf16_t *__restrict__ dK,
+    bf16_t *__restrict__ dV, float *__restrict__ part_k, float *__restrict__ part_v, PackedArgs a)
 {
+    typedef bf16_t T;
     typedef RowTile<T, D> RT;
-    constexpr int NM = RT::RB / 32, NB = D / 32, OWN = kPairKeys, ROWS = PairShape<T, D>::ROWS, TILE = ROWS * RT::RB, WP = Weights<T>::PIECES;
-    static_assert(ROWS == 64, "32 rows of a tile for either wave of a pair");
+    typedef RowSum<T, D> RS;
+    typedef BwdShape<T, D, 1> Sh;
+    constexpr int RING = D == 128 ? kRing : kRing - 2;  // (6 at d = 64 would spill)
+    static_assert(Sh::RT == 2 && Sh::NBUF == 2, "two halves of a tile");
+    constexpr int NM = RT::RB / 32, NB = D / 32;
     // every tile an array of its own: reads of one then need not wait for the loads into another
-    __shared__ __align__(1024) unsigned char qa[TILE], ga[TILE], qb[PairShape<T, D>::NBUF == 2 ? TILE : 16], gb[PairShape<T, D>::NBUF == 2 ? TILE : 16];
-    __shared__ __align__(16) uint4 hand[4][WP][64];
-    __shared__ __align__(16) float st[PairShape<T, D>::NBUF][2][ROWS];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), role = wave & 1;
+    __shared__ __align__(1024) unsigned char qa[Sh::TILE], ga[Sh::TILE], qb[Sh::NBUF == 2 ? Sh::TILE : 16], gb[Sh::NBUF == 2 ? Sh::TILE : 16];
+    __shared__ __align__(16) float st[Sh::NBUF][2][Sh::ROWS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, half = lane >> 5;
     const int hk = blockIdx.x % a.Hkv, slot = blockIdx.x / a.Hkv, split = blockIdx.y;
-    const int si = __builtin_amdgcn_readfirstlane(find_sequence(a.cu_k, a.n_seq, a.total_k, 1, OWN, slot));
+    const int si = __builtin_amdgcn_readfirstlane(find_sequence(a.cu_k, a.n_seq, a.total_k, 1, Sh::OWN, slot));
     const Sequence sq = read_sequence(a, si);
-    const int key0 = (slot - first_slot(a.cu_k[si], a.total_k, 1, OWN, si)) * OWN;
+    const int key0 = (slot - first_slot(a.cu_k[si], a.total_k, 1, Sh::OWN, si)) * Sh::OWN;
     if (key0 < 0 || key0 >= sq.nk) return;
     const int rows = sq.nq * a.group, past = sq.nk - sq.nq;
-    const int key = key0 + (wave >> 1) * 32 + n, kc = min(key, sq.nk - 1);
+    const int key = key0 + wave * 32 + n, kc = min(key, sq.nk - 1);
     int rbeg = split * a.chunk;
     const int rend = a.chunk ? min(rows, rbeg + a.chunk) : rows;
     if (a.chunk && rbeg >= rows && split > 0) return;  // no such piece of this sequence
-    if (a.causal) rbeg = max(rbeg, max(0, key0 - past) * a.group / ROWS * ROWS);  // rows before see none of these keys
+    if (a.causal) rbeg = max(rbeg, max(0, key0 - past) * a.group / Sh::ROWS * Sh::ROWS);  // rows before see none of these keys
 
     Frag<T> kf[NM], vf[NM];
     {
@@ -363,102 +350,138 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void packed_dkdv_pair_
             kf[m] = *reinterpret_cast<const Frag<T> *>(kp + (2 * m + half) * 16);
             vf[m] = *reinterpret_cast<const Frag<T> *>(vp + (2 * m + half) * 16);
         }
+        if constexpr (D == 128) {  // to the other half of the registers, where products can take them from
+#pragma unroll
+            for (int m = 0; m < NM; ++m) asm volatile("" : "+a"(kf[m].v), "+a"(vf[m].v));
+        }
     }
     const unsigned char *qp = reinterpret_cast<const unsigned char *>(Q) + (int64_t)sq.q0 * a.q_row + (int64_t)hk * a.group * a.q_head;
     const unsigned char *gp = reinterpret_cast<const unsigned char *>(dO) + (int64_t)sq.q0 * a.do_row + (int64_t)hk * a.group * a.do_head;
     const float2 *const sp = stat + (int64_t)hk * a.total_q * a.group + (int64_t)sq.q0 * a.group;
     float2 sn = make_float2(-kNegInf, 0.f);
-    RowLoads<T, D, ROWS, 4> ql, gl;
+    RowLoads<T, D, Sh::ROWS, 4> ql, gl;
     ql.set(wave, a.q_row);
     gl.set(wave, a.do_row);
     auto request = [&](int r0, unsigned char *qt, unsigned char *gt) __attribute__((always_inline)) {
         ql.rows(a, qp, a.q_row, a.q_head, r0, rows, qt);
         gl.rows(a, gp, a.do_row, a.do_head, r0, rows, gt);
-        if ((int)threadIdx.x < ROWS) sn = r0 + (int)threadIdx.x < rend ? sp[r0 + threadIdx.x] : make_float2(-kNegInf, 0.f);  // rows past the end: weights of zero
-    };
-    auto park = [&](int b) __attribute__((always_inline)) {
-        if ((int)threadIdx.x < ROWS) {
-            st[b][0][threadIdx.x] = sn.x;
-            st[b][1][threadIdx.x] = sn.y;
-        }
+        if ((int)threadIdx.x < Sh::ROWS) sn = r0 + (int)threadIdx.x < rend ? sp[r0 + threadIdx.x] : make_float2(-kNegInf, 0.f);  // rows past the end: weights of zero
     };
     const float c = a.scale * kLog2e;
-    floatx16_t acc[NB];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) acc[nb] = zero16();
-    auto tile = [&](int r0, const unsigned char *qt, const unsigned char *gt, int b) __attribute__((always_inline)) {
-        const int sub = role * 32;
-        floatx16_t s, dp;
-        tile_scores2<T, D>(qt, gt, sub + n, kf, vf, s, dp);
-        if (a.causal && key0 + OWN > row_token(a, r0) + past + 1) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = key <= row_token(a, r0 + sub + 8 * (i >> 2) + 4 * half + (i & 3)) + past ? s[i] : kNegInf;
+    auto park = [&](int b) __attribute__((always_inline)) {
+        if ((int)threadIdx.x < Sh::ROWS) {
+            st[b][0][threadIdx.x] = -sn.x / c;
+            st[b][1][threadIdx.x] = -sn.y;
         }
+    };
+    floatx16_t dk[NB], dv[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) dk[nb] = dv[nb] = zero16();
+    // Rows sub .. sub + 31 of a tile: their scores and dP, the statistics they need, the weights made of them
+    struct Part {
+        floatx16_t s, dp;
+        Weights<T> p, ds;
+    };
+    // key j is seen by rows from (j - past) * group on
+    const int first_seen = a.causal ? min(max(key - past, 0), sq.nq) * a.group : 0;
+    auto mask = [&](Part &x, int r0, int sub) __attribute__((always_inline)) {
+        const int lim = first_seen - r0 - sub - 4 * half;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x.s[i] = 8 * (i >> 2) + (i & 3) >= lim ? x.s[i] : kNegInf;
+    };
+    auto statistics = [&](Part &x, int sub, int b) __attribute__((always_inline)) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const float4 l2 = *reinterpret_cast<const float4 *>(&st[b][0][sub + 8 * g + 4 * half]);
-            const float4 dl = *reinterpret_cast<const float4 *>(&st[b][1][sub + 8 * g + 4 * half]);
-            const float l[4] = {l2.x, l2.y, l2.z, l2.w}, d[4] = {dl.x, dl.y, dl.z, dl.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[4 * g + i] = fast_exp2(fmaf(s[4 * g + i], c, -l[i]));
-                dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - d[i]);
+            const float4 l = *reinterpret_cast<const float4 *>(&st[b][0][sub + 8 * g + 4 * half]);
+            const float4 d = *reinterpret_cast<const float4 *>(&st[b][1][sub + 8 * g + 4 * half]);
+            x.s[4 * g] = l.x; x.s[4 * g + 1] = l.y; x.s[4 * g + 2] = l.z; x.s[4 * g + 3] = l.w;
+            x.dp[4 * g] = d.x; x.dp[4 * g + 1] = d.y; x.dp[4 * g + 2] = d.z; x.dp[4 * g + 3] = d.w;
+        }
+    };
+    auto weigh = [&](Part &x, int j) __attribute__((always_inline)) {  // rows 2 j, 2 j + 1 of the lane's 16
+        const float p0 = fast_exp2(x.s[2 * j] * c), p1 = fast_exp2(x.s[2 * j + 1] * c);
+        x.p.set_pair(2 * j, p0, p1);
+        x.ds.set_pair(2 * j, p0 * x.dp[2 * j], p1 * x.dp[2 * j + 1]);
+    };
+    auto tile = [&](int r0, const unsigned char *qt, const unsigned char *gt, int b) __attribute__((always_inline)) {
+        // a wave has its SIMD to itself: one row of operands for all products of the tile, read RING steps ahead, and the weights of each half made
+        // between products that do not need them
+        constexpr int NS = 2 * NM, NW = 2 * RS::STEPS, N = 2 * NS + 2 * NW;
+        Part x, y;
+        bf16x8_t ring[RING];
+        auto fetch = [&](auto at) __attribute__((always_inline)) {
+            constexpr int k = decltype(at)::value;
+            if constexpr (k < 2 * NS) {
+                ring[k % RING] = row_frag<T, D>(k & 1 ? gt : qt, (k / NS) * 32 + n, (k % NS) / 2, half).v;
+            } else {
+                constexpr int j = k - 2 * NS;
+                ring[k % RING] = RS::fetch((j % NW) < RS::STEPS ? gt : qt, (j / NW) * 32, j % RS::STEPS);
             }
-        }
-        Weights<T> p, ds, mine, other;
-        p.set(s);
-        ds.set(dp);
-#pragma unroll
-        for (int i = 0; i < WP; ++i) {
-            const uint4 x = p.piece(i), y = ds.piece(i);
-            hand[wave][i][lane] = role ? x : y;
-            mine.set_piece(i, role ? y : x);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < WP; ++i) other.set_piece(i, hand[wave ^ 1][i][lane]);
-        const unsigned char *const rt = role ? qt : gt;
-        weighted_rows<D>(rt, sub, mine, acc);
-        weighted_rows<D>(rt, 32 - sub, other, acc);
+        };
+        auto use = [&](auto at, Part &z) __attribute__((always_inline)) {
+            constexpr int k = decltype(at)::value;
+            if constexpr (k < 2 * NS) {
+                constexpr int m = (k % NS) / 2;
+                if constexpr (k & 1) z.dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[k % RING], vf[m].v, z.dp, 0, 0, 0);
+                else z.s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[k % RING], kf[m].v, z.s, 0, 0, 0);
+            } else {
+                constexpr int j = k - 2 * NS;
+                if constexpr ((j % NW) < RS::STEPS) RS::step(j % RS::STEPS, ring[k % RING], z.p, dv);
+                else RS::step(j % RS::STEPS, ring[k % RING], z.ds, dk);
+            }
+        };
+        statistics(x, 0, b);
+        static_for<RING>(fetch);
+        pin_order();
+        static_for<N>([&](auto at) __attribute__((always_inline)) {
+            constexpr int k = decltype(at)::value;
+            if constexpr (k < 2 * NS ? k < NS : k - 2 * NS < NW) use(at, x);
+            else use(at, y);
+            if constexpr (k + RING < N) fetch(std::integral_constant<int, k + RING>{});
+            if constexpr (k == NS - 4) statistics(y, 32, b);
+            if constexpr (CAUSAL && k == NS - 1) mask(x, r0, 0);
+            if constexpr (CAUSAL && k == 2 * NS - 1) mask(y, r0, 32);
+            if constexpr (k >= NS && k < 2 * NS && (k - NS) % (NS / 8) == NS / 8 - 1) weigh(x, (k - NS) / (NS / 8));
+            if constexpr (k >= 2 * NS && k < 2 * NS + NW && (k - 2 * NS) % (NW / 8) == NW / 8 - 1) weigh(y, (k - 2 * NS) / (NW / 8));
+            pin_order();
+        });
     };
     if (rbeg < rend) {
-        if constexpr (PairShape<T, D>::NBUF == 2) {
-            request(rbeg, qa, ga);
-            park(0);
-            for (int r0 = rbeg; r0 < rend; r0 += 2 * ROWS) {
+        request(rbeg, qa, ga);
+        park(0);
+        for (int r0 = rbeg; r0 < rend; r0 += 2 * Sh::ROWS) {
+            wait_loads_and_sync();
+            if (r0 + Sh::ROWS < rend) request(r0 + Sh::ROWS, qb, gb);
+            tile(r0, qa, ga, 0);
+            if (r0 + Sh::ROWS < rend) {
+                park(1);
                 wait_loads_and_sync();
-                if (r0 + ROWS < rend) request(r0 + ROWS, qb, gb);
-                tile(r0, qa, ga, 0);
-                if (r0 + ROWS < rend) {
-                    park(1);
-                    wait_loads_and_sync();
-                    if (r0 + 2 * ROWS < rend) request(r0 + 2 * ROWS, qa, ga);
-                    tile(r0 + ROWS, qb, gb, 1);
-                    if (r0 + 2 * ROWS < rend) park(0);
-                }
-            }
-        } else {
-            for (int r0 = rbeg; r0 < rend; r0 += ROWS) {
-                __syncthreads();
-                request(r0, qa, ga);
-                park(0);
-                wait_loads_and_sync();
-                tile(r0, qa, ga, 0);
+                if (r0 + 2 * Sh::ROWS < rend) request(r0 + 2 * Sh::ROWS, qa, ga);
+                tile(r0 + Sh::ROWS, qb, gb, 1);
+                if (r0 + 2 * Sh::ROWS < rend) park(0);
             }
         }
     }
-    if (key >= sq.nk) return;
-    const float f = role ? a.scale : 1.f;
-    float *const pp = (role ? part_k : part_v) + (((int64_t)(sq.k0 + key) * a.Hkv + hk) * a.splits + split) * D;
-    T *const op = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(role ? dK : dV) + (int64_t)(sq.k0 + key) * (role ? a.dk_row : a.dv_row) +
-                                        (int64_t)hk * (role ? a.dk_head : a.dv_head));
+    T *const kop = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(dK) + (int64_t)(sq.k0 + kc) * a.dk_row + (int64_t)hk * a.dk_head);
+    T *const vop = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(dV) + (int64_t)(sq.k0 + kc) * a.dv_row + (int64_t)hk * a.dv_head);
+    const int64_t pid = (((int64_t)(sq.k0 + kc) * a.Hkv + hk) * a.splits + split) * D;
+    auto put_k = [&](int ch, float x, float y, float z, float w) __attribute__((always_inline)) {
+        if (key >= sq.nk) return;
+        if (a.splits > 1) store4(part_k + pid + ch, x * a.scale, y * a.scale, z * a.scale, w * a.scale);
+        else store4(kop + ch, x * a.scale, y * a.scale, z * a.scale, w * a.scale);
+    };
+    auto put_v = [&](int ch, float x, float y, float z, float w) __attribute__((always_inline)) {
+        if (key >= sq.nk) return;
+        if (a.splits > 1) store4(part_v + pid + ch, x, y, z, w);
+        else store4(vop + ch, x, y, z, w);
+    };
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int ch = 32 * nb + 8 * g + 4 * half;
-            if (a.splits > 1) store4(pp + ch, acc[nb][4 * g] * f, acc[nb][4 * g + 1] * f, acc[nb][4 * g + 2] * f, acc[nb][4 * g + 3] * f);
-            else store4(op + ch, acc[nb][4 * g] * f, acc[nb][4 * g + 1] * f, acc[nb][4 * g + 2] * f, acc[nb][4 * g + 3] * f);
+            put_k(ch, dk[nb][4 * g], dk[nb][4 * g + 1], dk[nb][4 * g + 2], dk[nb][4 * g + 3]);
+            put_v(ch, dv[nb][4 * g], dv[nb][4 * g + 1], dv[nb][4 * g + 2], dv[nb][4 * g + 3]);
         }
 }
 
@@ -501,14 +524,20 @@ dsv_status launch_dq(const PackedArgs &a, const T *Q, const T *K, const T *V, co
     return DSV_OK;
 }
 
-template <typename T, int D, int WK>
-dsv_status launch_dkdv(const PackedArgs &a, const T *Q, const T *K, const T *V, const T *dO, const float2 *stat, T *dK, T *dV, float *part, hipStream_t st)
+template <typename T, int D>
+dsv_status launch_dkdv(const PackedArgs &a, bool few, const T *Q, const T *K, const T *V, const T *dO, const float2 *stat, T *dK, T *dV, float *part, hipStream_t st)
 {
-    const int64_t slots = tile_slots(a.total_k, 1, WK == 1 ? kPairKeys : BwdShape<T, D, WK>::OWN, a.n_seq);
+    few |= sizeof(T) == 4;  // (128 keys a block would spill)
+    const int64_t slots = tile_slots(a.total_k, 1, few ? BwdShape<T, D, 4>::OWN : BwdShape<T, D, 1>::OWN, a.n_seq);
     const dim3 grid((unsigned)(slots * a.Hkv), a.splits);
     float *const part_v = part + packed_dkdv_bytes(a.total_k, a.Hkv, D, a.splits) / 8;
-    if constexpr (WK == 1) packed_dkdv_pair_kernel<T, D><<<grid, 256, 0, st>>>(Q, K, V, dO, stat, dK, dV, part, part_v, a);
-    else packed_dkdv_kernel<T, D, WK><<<grid, 256, 0, st>>>(Q, K, V, dO, stat, dK, dV, part, part_v, a);
+    if constexpr (sizeof(T) == 2) {
+        if (few) packed_dkdv_few_kernel<T, D><<<grid, 256, 0, st>>>(Q, K, V, dO, stat, dK, dV, part, part_v, a);
+        else if (a.causal) packed_dkdv_kernel<D, true><<<grid, 256, 0, st>>>(Q, K, V, dO, stat, dK, dV, part, part_v, a);
+        else packed_dkdv_kernel<D, false><<<grid, 256, 0, st>>>(Q, K, V, dO, stat, dK, dV, part, part_v, a);
+    } else {
+        packed_dkdv_few_kernel<T, D><<<grid, 256, 0, st>>>(Q, K, V, dO, stat, dK, dV, part, part_v, a);
+    }
     DSV_LAUNCH_CHECK();
     if (a.splits > 1) {
         packed_sum_kernel<T, D, true><<<dim3(merge_blocks<D / 4>(a.total_k, a.Hkv), 2), 256, 0, st>>>(part, part_v, dK, dV, a);
@@ -537,7 +566,7 @@ dsv_status launch_t(PackedArgs a, const PackedBwdPlan &pl, const void *Qv, const
     if (a.total_k > 0) {
         a.splits = pl.splits_k;
         a.chunk = pl.chunk_k;
-        s = pl.few_k ? launch_dkdv<T, D, 4>(a, Q, K, V, dO, stat, dK, dV, part, st) : launch_dkdv<T, D, 1>(a, Q, K, V, dO, stat, dK, dV, part, st);
+        s = launch_dkdv<T, D>(a, pl.few_k, Q, K, V, dO, stat, dK, dV, part, st);
     }
     return s;
 }
