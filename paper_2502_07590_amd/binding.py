@@ -515,11 +515,10 @@ class Packed:
         self.n_seq, self.total_q, self.total_k, self.max_q, self.max_k = int(n_seq), int(total_q), int(total_k), int(max_q), int(max_k)
         self.Hq, self.Hkv, self.d, self.scale, self.causal = int(Hq), int(Hkv), int(d), float(scale), bool(causal)
         self.torch_dtype = dtype
+        self.q_shape, self.k_shape = (self.total_q, self.Hq, self.d), (self.total_k, self.Hkv, self.d)
+        q, k = _CRows(self.Hq * self.d, self.d), _CRows(self.Hkv * self.d, self.d)
         self._c = _CPacked(self.n_seq, self.total_q, self.total_k, self.max_q, self.max_k, self.Hq, self.Hkv, self.d, _DTYPE_CODE.get(dtype, -1),
-                           int(self.causal), self.scale, 0)
-        q, k = (self.Hq * self.d, self.d), (self.Hkv * self.d, self.d)
-        for name, rows in (("q", q), ("k", k), ("v", k), ("o", q), ("dO", q), ("dq", q), ("dk", k), ("dv", k)):
-            setattr(self._c, name, rows)
+                           int(self.causal), self.scale, 0, q, k, k, q, q, q, k, k)
 
     @property
     def c(self):
@@ -534,9 +533,9 @@ class Norm:
             dtype = _DTYPE_NAME[dtype]
         self.tokens, self.n, self.eps, self.heads = int(tokens), int(n), float(eps), int(heads)
         self.torch_dtype = dtype
-        self._c = _CNorm(self.tokens, self.heads, self.n, _DTYPE_CODE.get(dtype, -1), self.eps, 0)
-        for name in ("x", "y", "dy", "dx"):
-            setattr(self._c, name, (self.heads * self.n, self.n))
+        self.shape = (self.tokens, self.heads, self.n)
+        rows = _CRows(self.heads * self.n, self.n)
+        self._c = _CNorm(self.tokens, self.heads, self.n, _DTYPE_CODE.get(dtype, -1), self.eps, 0, rows, rows, rows, rows)
 
     @property
     def c(self):
@@ -544,26 +543,27 @@ class Norm:
 
 
 def _rows(c, name: str, t: torch.Tensor, shape, dtype, device):
-    """Pointer of a tensor of rows [tokens, heads, n]; its strides go into the descriptor `c`."""
+    """Pointer of a tensor of rows [tokens, heads, n].  Its strides go into the descriptor `c`, which says contiguous ones."""
     if t.device != device:
         raise DsvError(f"libdsv takes device tensors, all on one device: {t.device} beside {device}")
-    if tuple(t.shape) != shape or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         raise DsvError(f"{name}: expected {dtype} of shape {shape}, got {t.dtype} of shape {tuple(t.shape)}")
-    row, head, one = t.stride()
-    if one != 1 and shape[2] > 1:
-        raise DsvError(f"{name}: the elements of a row must lie side by side")
-    # the stride of an axis that is never stepped along says nothing
-    setattr(c, name, (row if shape[0] > 1 else shape[1] * shape[2], head if shape[1] > 1 else shape[2]))
-    return ctypes.c_void_p(t.data_ptr())
+    if not t.is_contiguous():
+        row, head, one = t.stride()
+        if one != 1 and shape[2] > 1:
+            raise DsvError(f"{name}: the elements of a row must lie side by side")
+        # the stride of an axis that is never stepped along says nothing
+        setattr(c, name, (row if shape[0] > 1 else shape[1] * shape[2], head if shape[1] > 1 else shape[2]))
+    return t.data_ptr()
 
 
 def _flat(what: str, t, shape, dtype, device):
     """Pointer of a contiguous tensor, None for None."""
     if t is None:
         return None
-    if t.device != device or tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+    if t.device != device or t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise DsvError(f"{what}: expected contiguous {dtype} of shape {shape} on {device}, got {t.dtype} of shape {tuple(t.shape)} on {t.device}")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 class _On:
@@ -574,16 +574,17 @@ class _On:
             raise DsvError("libdsv takes device tensors")
         if stream is not None and stream.device != t.device:
             raise DsvError(f"tensors on {t.device}, stream on {stream.device}")
-        self._device, self._stream, self._ctx = t.device, stream, None
+        self._ctx = None
+        if stream is not None:
+            self._ctx, self.ptr = torch.cuda.stream(stream), stream.cuda_stream
+        else:
+            if t.device.index != torch.cuda.current_device():
+                self._ctx = torch.cuda.device(t.device)
+            self.ptr = _raw_stream(t.device.index)
 
     def __enter__(self):
-        if self._stream is not None:
-            self._ctx = torch.cuda.stream(self._stream)
-        elif self._device.index != torch.cuda.current_device():
-            self._ctx = torch.cuda.device(self._device)
         if self._ctx is not None:
             self._ctx.__enter__()
-        self.ptr = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
         return self
 
     def __exit__(self, *exc):
@@ -591,15 +592,19 @@ class _On:
             self._ctx.__exit__(*exc)
 
 
+# handle of a device's current stream; the short way spares the Stream object, a third of a small call's time on the host
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _scratch(nbytes: int, device, workspace):
-    """(pointer, bytes) of the caller's workspace, or of one made here, in the current stream's memory."""
+    """(pointer, bytes, the tensor) of the caller's workspace, or of one made here, in the current stream's memory."""
     if workspace is None:
         if nbytes == 0:
             return None, 0, None
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    elif workspace.device != device:
-        raise DsvError(f"workspace on {workspace.device}, tensors on {device}")
-    return _ptr(workspace), workspace.numel() * workspace.element_size(), workspace
+    elif workspace.device != device or not workspace.is_contiguous():
+        raise DsvError(f"workspace: a contiguous tensor on {device}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def packed_attn_fwd_workspace(p: Packed) -> int:
@@ -611,14 +616,13 @@ def packed_attn_fwd(p: Packed, Q, K, V, cu_q, cu_k, O=None, lse=None, O_tail=Non
     tokens and heads; cu_q, cu_k int32 [n_seq + 1] on the device.  O is made like Q.  O_tail (bf16 [total_q, Hq, d]): filled for the backward."""
     lib = load_library()
     with _On(Q, stream) as on:
-        dev, td, c = Q.device, p.torch_dtype, _CPacked.from_buffer_copy(p._c)
-        q, k = (p.total_q, p.Hq, p.d), (p.total_k, p.Hkv, p.d)
+        dev, td, c, q, k, cu = Q.device, p.torch_dtype, _CPacked.from_buffer_copy(p._c), p.q_shape, p.k_shape, (p.n_seq + 1,)
         O = torch.empty_like(Q) if O is None else O
         lse = torch.empty((p.Hq, p.total_q), dtype=torch.float32, device=dev) if lse is None else lse
-        args = [_rows(c, "q", Q, q, td, dev), _rows(c, "k", K, k, td, dev), _rows(c, "v", V, k, td, dev),
-                _flat("cu_q", cu_q, (p.n_seq + 1,), torch.int32, dev), _flat("cu_k", cu_k, (p.n_seq + 1,), torch.int32, dev),
-                _rows(c, "o", O, q, td, dev), _flat("O_tail", O_tail, q, td, dev), _flat("lse", lse, (p.Hq, p.total_q), torch.float32, dev)]
-        ws, nbytes, held = _scratch(int(lib.dsv_packed_attn_fwd_workspace(c)), dev, workspace)
+        args = (_rows(c, "q", Q, q, td, dev), _rows(c, "k", K, k, td, dev), _rows(c, "v", V, k, td, dev),
+                _flat("cu_q", cu_q, cu, torch.int32, dev), _flat("cu_k", cu_k, cu, torch.int32, dev),
+                _rows(c, "o", O, q, td, dev), _flat("O_tail", O_tail, q, td, dev), _flat("lse", lse, (p.Hq, p.total_q), torch.float32, dev))
+        ws, nbytes, held = _scratch(lib.dsv_packed_attn_fwd_workspace(c), dev, workspace)
         _check(lib.dsv_packed_attn_fwd(c, *args, ws, nbytes, on.ptr), "dsv_packed_attn_fwd")
     return O, lse
 
@@ -631,16 +635,15 @@ def packed_attn_bwd(p: Packed, Q, K, V, cu_q, cu_k, O, lse, dO, dQ=None, dK=None
     """(dQ, dK, dV) of packed_attn_fwd; the gradients are made like Q, K and V."""
     lib = load_library()
     with _On(Q, stream) as on:
-        dev, td, c = Q.device, p.torch_dtype, _CPacked.from_buffer_copy(p._c)
-        q, k = (p.total_q, p.Hq, p.d), (p.total_k, p.Hkv, p.d)
+        dev, td, c, q, k, cu = Q.device, p.torch_dtype, _CPacked.from_buffer_copy(p._c), p.q_shape, p.k_shape, (p.n_seq + 1,)
         dQ = torch.empty_like(Q) if dQ is None else dQ
         dK = torch.empty_like(K) if dK is None else dK
         dV = torch.empty_like(V) if dV is None else dV
-        args = [_rows(c, "q", Q, q, td, dev), _rows(c, "k", K, k, td, dev), _rows(c, "v", V, k, td, dev),
-                _flat("cu_q", cu_q, (p.n_seq + 1,), torch.int32, dev), _flat("cu_k", cu_k, (p.n_seq + 1,), torch.int32, dev),
+        args = (_rows(c, "q", Q, q, td, dev), _rows(c, "k", K, k, td, dev), _rows(c, "v", V, k, td, dev),
+                _flat("cu_q", cu_q, cu, torch.int32, dev), _flat("cu_k", cu_k, cu, torch.int32, dev),
                 _rows(c, "o", O, q, td, dev), _flat("O_tail", O_tail, q, td, dev), _flat("lse", lse, (p.Hq, p.total_q), torch.float32, dev),
-                _rows(c, "dO", dO, q, td, dev), _rows(c, "dq", dQ, q, td, dev), _rows(c, "dk", dK, k, td, dev), _rows(c, "dv", dV, k, td, dev)]
-        ws, nbytes, held = _scratch(int(lib.dsv_packed_attn_bwd_workspace(c)), dev, workspace)
+                _rows(c, "dO", dO, q, td, dev), _rows(c, "dq", dQ, q, td, dev), _rows(c, "dk", dK, k, td, dev), _rows(c, "dv", dV, k, td, dev))
+        ws, nbytes, held = _scratch(lib.dsv_packed_attn_bwd_workspace(c), dev, workspace)
         _check(lib.dsv_packed_attn_bwd(c, *args, ws, nbytes, on.ptr), "dsv_packed_attn_bwd")
     return dQ, dK, dV
 
@@ -649,13 +652,13 @@ def layer_norm_fwd(p: Norm, X, gamma=None, beta=None, Y=None, mean=None, rstd=No
     """(Y, mean, rstd): X [tokens, heads, n], any strides between tokens and heads; gamma, beta [n] or None; mean, rstd float [tokens, heads]."""
     lib = load_library()
     with _On(X, stream) as on:
-        dev, td, c, shape = X.device, p.torch_dtype, _CNorm.from_buffer_copy(p._c), (p.tokens, p.heads, p.n)
+        dev, td, c, shape = X.device, p.torch_dtype, _CNorm.from_buffer_copy(p._c), p.shape
         Y = torch.empty_like(X) if Y is None else Y
         mean = torch.empty(shape[:2], dtype=torch.float32, device=dev) if mean is None else mean
         rstd = torch.empty(shape[:2], dtype=torch.float32, device=dev) if rstd is None else rstd
-        args = [_rows(c, "x", X, shape, td, dev), _flat("gamma", gamma, (p.n,), td, dev), _flat("beta", beta, (p.n,), td, dev), _rows(c, "y", Y, shape, td, dev),
-                _flat("mean", mean, shape[:2], torch.float32, dev), _flat("rstd", rstd, shape[:2], torch.float32, dev)]
-        _check(lib.dsv_layer_norm_fwd(c, *args, on.ptr), "dsv_layer_norm_fwd")
+        _check(lib.dsv_layer_norm_fwd(c, _rows(c, "x", X, shape, td, dev), _flat("gamma", gamma, shape[2:], td, dev), _flat("beta", beta, shape[2:], td, dev),
+                                      _rows(c, "y", Y, shape, td, dev), _flat("mean", mean, shape[:2], torch.float32, dev),
+                                      _flat("rstd", rstd, shape[:2], torch.float32, dev), on.ptr), "dsv_layer_norm_fwd")
     return Y, mean, rstd
 
 
@@ -667,15 +670,15 @@ def layer_norm_bwd(p: Norm, X, gamma, mean, rstd, dY, dX=None, dgamma=None, dbet
     """(dX, dgamma, dbeta): dX made like X, dgamma and dbeta float [n]; both None where gamma is None and neither was passed."""
     lib = load_library()
     with _On(X, stream) as on:
-        dev, td, c, shape = X.device, p.torch_dtype, _CNorm.from_buffer_copy(p._c), (p.tokens, p.heads, p.n)
+        dev, td, c, shape = X.device, p.torch_dtype, _CNorm.from_buffer_copy(p._c), p.shape
         dX = torch.empty_like(X) if dX is None else dX
         if gamma is not None or dgamma is not None or dbeta is not None:
             dgamma = torch.empty(p.n, dtype=torch.float32, device=dev) if dgamma is None else dgamma
             dbeta = torch.empty(p.n, dtype=torch.float32, device=dev) if dbeta is None else dbeta
-        args = [_rows(c, "x", X, shape, td, dev), _flat("gamma", gamma, (p.n,), td, dev), _flat("mean", mean, shape[:2], torch.float32, dev),
+        args = (_rows(c, "x", X, shape, td, dev), _flat("gamma", gamma, shape[2:], td, dev), _flat("mean", mean, shape[:2], torch.float32, dev),
                 _flat("rstd", rstd, shape[:2], torch.float32, dev), _rows(c, "dy", dY, shape, td, dev), _rows(c, "dx", dX, shape, td, dev),
-                _flat("dgamma", dgamma, (p.n,), torch.float32, dev), _flat("dbeta", dbeta, (p.n,), torch.float32, dev)]
-        ws, nbytes, held = _scratch(int(lib.dsv_layer_norm_bwd_workspace(c)) if dgamma is not None else 0, dev, workspace)
+                _flat("dgamma", dgamma, shape[2:], torch.float32, dev), _flat("dbeta", dbeta, shape[2:], torch.float32, dev))
+        ws, nbytes, held = _scratch(lib.dsv_layer_norm_bwd_workspace(c) if dgamma is not None else 0, dev, workspace)
         _check(lib.dsv_layer_norm_bwd(c, *args, ws, nbytes, on.ptr), "dsv_layer_norm_bwd")
     return dX, dgamma, dbeta
 

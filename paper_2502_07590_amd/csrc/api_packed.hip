@@ -83,46 +83,83 @@ PackedArgs packed_args(const dsv_packed &p, const int32_t *cu_q, const int32_t *
     return a;
 }
 
-// How a step walks: own rows (queries times the heads that share, or keys) in tiles of 128, or of 32 where those would not fill the chip or the
-// sequences are short; and the other axis in pieces where even the small tiles are few.
+// How a step walks: own rows (queries times the heads that share, or keys) in tiles of 128, or of 32 whose four waves share the other axis; and
+// that axis in pieces, joined afterwards.
 struct Walk {
     bool few;
     int splits, chunk;
 };
-Walk plan_walk(int64_t own, int64_t heads, int64_t n_seq, int64_t other, int64_t max_other)
+// A step's cost: blocks of 128 rows a CU runs at once, operations a pair of rows (and channel), the rate it reaches with the chip full, and
+// how many results a piece leaves per own row.
+struct StepCost {
+    int per_cu;
+    double flops, rate;
+    int results;
+};
+Walk plan_walk(const StepCost &cost, int d, bool causal, int64_t own, int64_t heads, int64_t n_seq, int64_t other, int64_t max_other)
 {
-    constexpr int64_t kFew = 256, kWork = 512, kUnit = 128, kMinChunk = 256, kMaxSplits = 64;
+    constexpr int64_t kUnit = 128, kMinChunk = 256, kMaxSplits = 64, kCus = 256;
     Walk w{};
-    w.few = (own / 128 + 1) * heads < kFew || own / n_seq <= 64;
     w.splits = 1;
-    if (!w.few) return w;
-    const int64_t tiles = own / 32 + n_seq, blocks = tiles * heads;
-    if (blocks >= 2 * kWork) return w;
-    // pieces so long that all blocks together walk about kWork of them
-    const int64_t work = (int64_t)((double)tiles / (double)n_seq * (double)other * (double)heads) / kWork;
-    const int64_t chunk = (std::max({work, kMinChunk, (max_other + kMaxSplits - 1) / kMaxSplits}) + kUnit - 1) / kUnit * kUnit;
+    const int64_t pieces = std::max<int64_t>(1, max_other / kMinChunk);
+    // small tiles where large ones would be mostly empty, or not fill the chip even in the shortest pieces
+    w.few = own / n_seq <= 64 || (own / 128 + 1) * heads * pieces < kCus;
+    int64_t chunk = max_other;
+    if (w.few) {
+        const int64_t tiles = own / 32 + n_seq;
+        if (tiles * heads < 4 * kCus) {  // pieces so long that all blocks together walk about 512 of them
+            const int64_t work = (int64_t)((double)tiles / (double)n_seq * (double)other * (double)heads) / (2 * kCus);
+            chunk = std::max({work, kMinChunk, (max_other + kMaxSplits - 1) / kMaxSplits});
+        }
+    } else {
+        // The last round of blocks leaves CUs idle; pieces make rounds shorter, and cost writing and reading their results.  L = 20280, four
+        // heads, bf16, d = 128 (636 blocks): forward, dq, dkdv in one piece 1.01, 1.59, 1.77 ms, in four, four and two 0.88, 1.43, 1.62.
+        const double slots = (double)kCus * cost.per_cu, tiles = n_seq == 1 ? (double)((own + 127) / 128) : (double)(own / 128 + (n_seq + 1) / 2);
+        const double full = tiles * (double)heads * (double)other / ((double)n_seq * (double)std::max<int64_t>(max_other, 1)) * (causal ? 0.5 : 1.0);
+        const bool alike = n_seq == 1 && !causal;  // all blocks as long: whole rounds of them
+        const double block_s = cost.flops * d * 128.0 * (double)max_other / (cost.rate / slots);
+        const double piece_s = (double)own * (double)heads * d * 8.0 * cost.results / 4e12;  // written and read
+        double best = 0;
+        for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            if (s > pieces) break;
+            const double t = (alike ? std::ceil(full * s / slots) / s : std::max(full / slots, 1.0 / s)) * block_s + (s > 1 ? s * piece_s + 5e-6 : 0.0);
+            if (s == 1 || t < 0.97 * best) {
+                best = t;
+                chunk = (max_other + s - 1) / s;
+            }
+        }
+    }
+    chunk = (chunk + kUnit - 1) / kUnit * kUnit;
     if (chunk >= max_other) return w;
     w.chunk = (int)chunk;
     w.splits = (int)((max_other + chunk - 1) / chunk);
     return w;
 }
-Walk walk_q(const dsv_packed &p) { return plan_walk((int64_t)p.total_q * (p.Hq / p.Hkv), p.Hkv, p.n_seq, p.total_k, std::min(p.max_k, p.total_k)); }
-Walk walk_k(const dsv_packed &p)
+enum Step { kFwd, kDq, kDkdv };
+Walk walk_of(const dsv_packed &p, Step step)
 {
+    const bool bf16 = p.dtype == DSV_BF16;
     const int64_t g = p.Hq / p.Hkv;
-    // (fp32 always takes the small tiles)
-    return plan_walk(p.total_k, p.Hkv, p.n_seq, (int64_t)p.total_q * g, std::min(p.max_q, p.total_q) * g);
+    // flops of a pair and channel, and rates: as measured at 32768 tokens
+    StepCost c{};
+    c.per_cu = step == kDkdv ? (p.d == 64 ? 2 : 1) : bf16 ? (p.d == 64 ? 3 : 2) : (p.d == 64 ? 2 : 1);
+    c.flops = step == kFwd ? 4 : 8;
+    c.rate = bf16 ? 1.1e15 : 1e14;
+    c.results = step == kDkdv ? 2 : 1;
+    if (step == kDkdv)
+        return plan_walk(c, p.d, p.causal != 0, p.total_k, p.Hkv, p.n_seq, (int64_t)p.total_q * g, std::min(p.max_q, p.total_q) * g);
+    return plan_walk(c, p.d, p.causal != 0, (int64_t)p.total_q * g, p.Hkv, p.n_seq, p.total_k, std::min(p.max_k, p.total_k));
 }
 
 size_t fwd_bytes(const dsv_packed &p)
 {
-    const Walk w = walk_q(p);
+    const Walk w = walk_of(p, kFwd);
     return w.splits > 1 ? packed_fwd_acc_bytes(p.total_q, p.Hq, p.d, w.splits) + align_up((size_t)p.total_q * p.Hq * w.splits * 8, 256) : 0;
 }
 size_t bwd_bytes(const dsv_packed &p)
 {
     return packed_stat_bytes(p.total_q, p.Hq) +
-           std::max(packed_dq_bytes(p.total_q, p.Hq, p.d, walk_q(p).splits), packed_dkdv_bytes(p.total_k, p.Hkv, p.d, walk_k(p).splits));
+           std::max(packed_dq_bytes(p.total_q, p.Hq, p.d, walk_of(p, kDq).splits), packed_dkdv_bytes(p.total_k, p.Hkv, p.d, walk_of(p, kDkdv).splits));
 }
 
 dsv_status check_norm(const dsv_norm *p, bool grad)
@@ -182,7 +219,7 @@ dsv_status dsv_packed_attn_fwd(const dsv_packed *p, const void *Q, const void *K
     st = check_workspace(workspace, ws_bytes, fwd_bytes(*p));
     if (st != DSV_OK) return st;
     if (p->total_q == 0) return DSV_OK;
-    const Walk w = walk_q(*p);
+    const Walk w = walk_of(*p, kFwd);
     PackedArgs a = packed_args(*p, cu_q, cu_k);
     a.splits = w.splits;
     a.chunk = w.chunk;
@@ -207,7 +244,7 @@ dsv_status dsv_packed_attn_bwd(const dsv_packed *p, const void *Q, const void *K
     if (O_tail && (p->dtype != DSV_BF16 || !aligned16(O_tail))) return DSV_EINVAL;
     st = check_workspace(workspace, ws_bytes, bwd_bytes(*p));
     if (st != DSV_OK) return st;
-    const Walk q = walk_q(*p), k = walk_k(*p);
+    const Walk q = walk_of(*p, kDq), k = walk_of(*p, kDkdv);
     const PackedBwdPlan plan{q.few, k.few, q.splits, q.chunk, k.splits, k.chunk};
     return launch_packed_bwd(packed_args(*p, cu_q, cu_k), plan, p->dtype, p->d, Q, K, V, O, O_tail, lse, dO, dQ, dK, dV, static_cast<char *>(workspace),
                              static_cast<hipStream_t>(hip_stream));

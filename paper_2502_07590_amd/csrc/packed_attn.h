@@ -422,21 +422,46 @@ __device__ __forceinline__ void store_out(bf16_t *p, bf16_t *tail, float a, floa
 }
 __device__ __forceinline__ void store_out(float *p, bf16_t *, float a, float b, float c, float d) { store4(p, a, b, c, d); }
 
-// Kernels that join pieces: a wave takes 64 / LPR heads of one token, LPR lanes each.  False behind the last token (whole waves); heads past the
-// last one are the caller's to leave out.
-template <int LPR> __device__ __forceinline__ bool merge_row(int total, int heads, int &tok, int &head)
+// Kernels that join pieces: LPR lanes to a row (token and head) and piece.  GROUPS = 1: a wave takes 64 / LPR heads of one token; false behind the
+// last token (whole waves), heads past the last one are the caller's to leave out.  Else a block takes one row, GROUPS pieces at a time.
+template <int LPR, int GROUPS> __device__ __forceinline__ bool merge_row(int total, int heads, int &tok, int &head)
 {
-    constexpr int HPW = 64 / LPR;
-    const int per = (heads + HPW - 1) / HPW;
-    const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    tok = (int)(w / per);
-    head = (int)(w - (int64_t)tok * per) * HPW + (threadIdx.x & 63) / LPR;
+    if constexpr (GROUPS > 1) {
+        tok = (int)(blockIdx.x / (unsigned)heads);
+        head = (int)(blockIdx.x - (unsigned)tok * (unsigned)heads);
+    } else {
+        constexpr int HPW = 64 / LPR;
+        const int per = (heads + HPW - 1) / HPW;
+        const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        tok = (int)(w / per);
+        head = (int)(w - (int64_t)tok * per) * HPW + (threadIdx.x & 63) / LPR;
+    }
     return tok < total;
 }
-template <int LPR> __host__ __forceinline__ unsigned merge_blocks(int64_t total, int heads)
+template <int LPR, int GROUPS> __host__ __forceinline__ unsigned merge_blocks(int64_t total, int heads)
 {
     constexpr int HPW = 64 / LPR;
-    return (unsigned)((total * ((heads + HPW - 1) / HPW) + 3) / 4);
+    return GROUPS > 1 ? (unsigned)(total * heads) : (unsigned)((total * ((heads + HPW - 1) / HPW) + 3) / 4);
+}
+// A row of many pieces has a block to itself where that is not too many blocks.
+__host__ __forceinline__ bool wide_merge(int splits, int64_t rows) { return splits > 8 && rows < 65536; }
+// The groups' sums of four channels each; group 0 has them all.
+template <int LPR, int GROUPS> __device__ __forceinline__ void join_groups(float (&v)[4])
+{
+    if constexpr (GROUPS > 1) {
+        __shared__ __align__(16) float part[GROUPS][LPR * 4];
+        const int lane = threadIdx.x % LPR, grp = threadIdx.x / LPR;
+        *reinterpret_cast<float4 *>(&part[grp][4 * lane]) = make_float4(v[0], v[1], v[2], v[3]);
+        __syncthreads();
+        if (grp == 0) {
+            v[0] = v[1] = v[2] = v[3] = 0.f;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                const float4 x = *reinterpret_cast<const float4 *>(&part[g][4 * lane]);
+                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+            }
+        }
+    }
 }
 
 __device__ __forceinline__ void wait_loads_and_sync()

@@ -24,7 +24,7 @@ __global__ __launch_bounds__(256) void packed_stat_kernel(const T *__restrict__ 
 {
     constexpr int LPR = D * (int)sizeof(T) / 16, CH = 16 / (int)sizeof(T);
     int tok, head;
-    if (!merge_row<LPR>(a.total_q, a.Hq, tok, head)) return;
+    if (!merge_row<LPR, 1>(a.total_q, a.Hq, tok, head)) return;
     const int lane = threadIdx.x % LPR;
     const int hc = min(head, a.Hq - 1);
     const T *go = reinterpret_cast<const T *>(reinterpret_cast<const unsigned char *>(dO) + (int64_t)tok * a.do_row + (int64_t)hc * a.do_head) + lane * CH;
@@ -486,29 +486,41 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkdv_kernel(
 }
 
 // Sums of the pieces.  KEYS: of dK and dV (blockIdx.y), pieces of the rows; else of dQ, pieces of the keys.
-template <typename T, int D, bool KEYS>
+template <typename T, int D, bool KEYS, int GROUPS>
 __global__ __launch_bounds__(256) void packed_sum_kernel(const float *__restrict__ p0, const float *__restrict__ p1, T *__restrict__ out0, T *__restrict__ out1, PackedArgs a)
 {
     constexpr int LPR = D / 4;
-    const int heads = KEYS ? a.Hkv : a.Hq;
+    const int heads = KEYS ? a.Hkv : a.Hq, total = KEYS ? a.total_k : a.total_q;
     int tok, head;
-    if (!merge_row<LPR>(KEYS ? a.total_k : a.total_q, heads, tok, head)) return;
-    const int lane = threadIdx.x % LPR;
-    const Sequence sq = read_sequence(a, __builtin_amdgcn_readfirstlane(find_sequence(KEYS ? a.cu_k : a.cu_q, a.n_seq, KEYS ? a.total_k : a.total_q, 1, 0, tok)));
+    if (!merge_row<LPR, GROUPS>(total, heads, tok, head)) return;
+    const int lane = threadIdx.x % LPR, grp = GROUPS > 1 ? threadIdx.x / LPR : 0;
+    const Sequence sq = read_sequence(a, __builtin_amdgcn_readfirstlane(find_sequence(KEYS ? a.cu_k : a.cu_q, a.n_seq, total, 1, 0, tok)));
     const int t0 = KEYS ? sq.k0 : sq.q0, nt = KEYS ? sq.nk : sq.nq;
     if (tok < t0 || tok >= t0 + nt || head >= heads) return;
     const int pieces = max(1, ((KEYS ? sq.nq * a.group : sq.nk) + a.chunk - 1) / a.chunk);
     const bool second = KEYS && blockIdx.y;
     const float *p = (second ? p1 : p0) + ((int64_t)tok * heads + head) * a.splits * D + 4 * lane;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = 0; s < pieces; ++s) {
-        const float4 x = *reinterpret_cast<const float4 *>(p + s * D);
+#pragma unroll 8
+    for (int s = grp; s < pieces; s += GROUPS) {
+        const float4 x = *reinterpret_cast<const float4 *>(p + (int64_t)s * D);
         v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
     }
+    join_groups<LPR, GROUPS>(v);
+    if (grp > 0) return;
     const int64_t rb = KEYS ? (second ? a.dv_row : a.dk_row) : a.dq_row, hb = KEYS ? (second ? a.dv_head : a.dk_head) : a.dq_head;
     T *op = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(second ? out1 : out0) + (int64_t)tok * rb + (int64_t)head * hb);
     store4(op + 4 * lane, v[0], v[1], v[2], v[3]);
+}
+template <typename T, int D, bool KEYS> void launch_sum(const PackedArgs &a, const float *p0, const float *p1, T *out0, T *out1, hipStream_t st)
+{
+    constexpr int LPR = D / 4, G = 256 / LPR;
+    const int64_t total = KEYS ? a.total_k : a.total_q;
+    const int heads = KEYS ? a.Hkv : a.Hq;
+    if (wide_merge(a.splits, total * heads))
+        packed_sum_kernel<T, D, KEYS, G><<<dim3(merge_blocks<LPR, G>(total, heads), KEYS ? 2 : 1), 256, 0, st>>>(p0, p1, out0, out1, a);
+    else
+        packed_sum_kernel<T, D, KEYS, 1><<<dim3(merge_blocks<LPR, 1>(total, heads), KEYS ? 2 : 1), 256, 0, st>>>(p0, p1, out0, out1, a);
 }
 
 template <typename T, int D, int WK>
@@ -518,7 +530,7 @@ dsv_status launch_dq(const PackedArgs &a, const T *Q, const T *K, const T *V, co
     packed_dq_kernel<T, D, WK><<<dim3((unsigned)(slots * a.Hkv), a.splits), 256, 0, st>>>(Q, K, V, dO, stat, dQ, part, a);
     DSV_LAUNCH_CHECK();
     if (a.splits > 1) {
-        packed_sum_kernel<T, D, false><<<merge_blocks<D / 4>(a.total_q, a.Hq), 256, 0, st>>>(part, nullptr, dQ, nullptr, a);
+        launch_sum<T, D, false>(a, part, nullptr, dQ, nullptr, st);
         DSV_LAUNCH_CHECK();
     }
     return DSV_OK;
@@ -540,7 +552,7 @@ dsv_status launch_dkdv(const PackedArgs &a, bool few, const T *Q, const T *K, co
     }
     DSV_LAUNCH_CHECK();
     if (a.splits > 1) {
-        packed_sum_kernel<T, D, true><<<dim3(merge_blocks<D / 4>(a.total_k, a.Hkv), 2), 256, 0, st>>>(part, part_v, dK, dV, a);
+        launch_sum<T, D, true>(a, part, part_v, dK, dV, st);
         DSV_LAUNCH_CHECK();
     }
     return DSV_OK;
@@ -556,7 +568,7 @@ dsv_status launch_t(PackedArgs a, const PackedBwdPlan &pl, const void *Qv, const
     float *const part = reinterpret_cast<float *>(ws + packed_stat_bytes(a.total_q, a.Hq));  // of dQ, then, when that is done, of dK and dV
     dsv_status s = DSV_OK;
     if (a.total_q > 0) {
-        packed_stat_kernel<T, D><<<merge_blocks<D *(int)sizeof(T) / 16>(a.total_q, a.Hq), 256, 0, st>>>(static_cast<const T *>(Ov), static_cast<const T *>(tail), dO, lse, stat, a);
+        packed_stat_kernel<T, D><<<merge_blocks<D *(int)sizeof(T) / 16, 1>(a.total_q, a.Hq), 256, 0, st>>>(static_cast<const T *>(Ov), static_cast<const T *>(tail), dO, lse, stat, a);
         DSV_LAUNCH_CHECK();
         a.splits = pl.splits_q;
         a.chunk = pl.chunk_q;

@@ -15,11 +15,11 @@ namespace {
 template <typename T, int D, int WK> struct FwdShape {
     static constexpr int ROWS = WK == 1 ? 128 : 32, KEYS = WK == 1 ? 64 : 128, KT = KEYS / 32 / WK;
     static constexpr int TILE = KEYS * D * (int)sizeof(T);
-    static constexpr int NBUF = 2 * 2 * TILE <= 128 * 1024 ? 2 : 1;
+    static constexpr int NBUF = WK == 1 || (sizeof(T) == 4 && D == 64) ? 2 : 1;  // fp32 is bound by the products: two blocks on a CU would leave others idle
 };
 
 template <typename T, int D, int WK>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed_fwd_kernel(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V,
+__global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2) void packed_fwd_kernel(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V,
                                                                                         T *__restrict__ O, bf16_t *__restrict__ O_tail, float *__restrict__ lse,
                                                                                         float2 *__restrict__ pml, float *__restrict__ pacc, PackedArgs a)
 {
@@ -69,10 +69,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) acc[nb] = zero16();
     float mrun = kNegInf, l = 0.f, lr = 0.f;  // lr: sum of the weights as the second product takes them
-    auto tile = [&](int k0, const unsigned char *kt, const unsigned char *vt) __attribute__((always_inline)) {
-        const int sub = WK == 1 ? 0 : wave * 32;
-        floatx16_t s[KT];
-        tile_scores<T, D, KT>(kt, sub + n, qf, s);
+    const int sub = WK == 1 ? 0 : wave * 32;
+    auto scores = [&](const unsigned char *kt, floatx16_t (&s)[KT]) __attribute__((always_inline)) { tile_scores<T, D, KT>(kt, sub + n, qf, s); };
+    auto rest = [&](int k0, floatx16_t (&s)[KT], const unsigned char *vt) __attribute__((always_inline)) {
         // the tile's last key is behind the end, or not seen by the wave's first row
         const bool edge = k0 + Sh::KEYS > kcut || (a.causal && k0 + Sh::KEYS > row_token(a, row0) + past + 1);
         if (edge) {
@@ -116,6 +115,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
         l += lt;
         lr += lrt;
     };
+    auto tile = [&](int k0, const unsigned char *kt, const unsigned char *vt) __attribute__((always_inline)) {
+        floatx16_t s[KT];
+        scores(kt, s);
+        rest(k0, s, vt);
+    };
     if (kbeg < kend) {
         if constexpr (Sh::NBUF == 2) {
             request(kbeg, ka, va);
@@ -130,11 +134,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
                 }
             }
         } else {
+            // one tile of each, V on its way while the scores are formed and the next K while V is summed: room for two blocks
+            kl.keys(kp, a.k_row, kbeg, sq.nk, ka);
             for (int k0 = kbeg; k0 < kend; k0 += Sh::KEYS) {
-                __syncthreads();
-                request(k0, ka, va);
                 wait_loads_and_sync();
-                tile(k0, ka, va);
+                vl.keys(vp, a.v_row, k0, sq.nk, va);
+                floatx16_t s[KT];
+                scores(ka, s);
+                wait_loads_and_sync();
+                if (k0 + Sh::KEYS < kend) kl.keys(kp, a.k_row, k0 + Sh::KEYS, sq.nk, ka);
+                rest(k0, s, va);
             }
         }
     }
@@ -219,31 +228,59 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
     }
 }
 
-// The pieces of a row joined: weights 2^(m_s - max).  A wave takes 64 / (D / 4) heads of one query, D / 4 lanes each.
-template <typename T, int D>
+// The pieces of a row joined: weights 2^(m_s - max).
+template <typename T, int D, int GROUPS>
 __global__ __launch_bounds__(256) void packed_fwd_merge_kernel(const float2 *__restrict__ pml, const float *__restrict__ pacc, T *__restrict__ O,
                                                                bf16_t *__restrict__ O_tail, float *__restrict__ lse, PackedArgs a)
 {
-    constexpr int LPR = D / 4;
+    constexpr int LPR = D / 4, PL = 64 / LPR;  // pieces a lane weighs, of 64 at most
     int tok, head;
-    if (!merge_row<LPR>(a.total_q, a.Hq, tok, head)) return;
-    const int lane = threadIdx.x % LPR;
+    if (!merge_row<LPR, GROUPS>(a.total_q, a.Hq, tok, head)) return;
+    const int lane = threadIdx.x % LPR, grp = GROUPS > 1 ? threadIdx.x / LPR : 0;
     const Sequence sq = read_sequence(a, __builtin_amdgcn_readfirstlane(find_sequence(a.cu_q, a.n_seq, a.total_q, 1, 0, tok)));
     if (tok < sq.q0 || tok >= sq.q0 + sq.nq || head >= a.Hq) return;
     const int64_t rid = (int64_t)tok * a.Hq + head;
     const int pieces = max(1, (sq.nk + a.chunk - 1) / a.chunk);
     const float2 *const ml = pml + rid * a.splits;
     const float *const pa = pacc + rid * a.splits * D + 4 * lane;
-    float m = kNegInf, l = 0.f;
-    for (int s = 0; s < pieces; ++s) m = fmaxf(m, ml[s].x);
-    const float mref = m == kNegInf ? 0.f : m;
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    float v[4] = {0.f, 0.f, 0.f, 0.f}, m = kNegInf, l = 0.f;
+    auto add = [&](int s, float w) __attribute__((always_inline)) {
+        const float4 x = *reinterpret_cast<const float4 *>(pa + (int64_t)s * D);
+        v[0] = fmaf(x.x, w, v[0]); v[1] = fmaf(x.y, w, v[1]); v[2] = fmaf(x.z, w, v[2]); v[3] = fmaf(x.w, w, v[3]);
+    };
+    if constexpr (GROUPS > 1) {
+        __shared__ float weight[64];
+        float2 mine[PL];
+#pragma unroll
+        for (int i = 0; i < PL; ++i) {
+            mine[i] = lane + i * LPR < pieces ? ml[lane + i * LPR] : make_float2(kNegInf, 0.f);
+            m = fmaxf(m, mine[i].x);
+        }
+#pragma unroll
+        for (int s = LPR / 2; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor(m, s));
+        const float mref = m == kNegInf ? 0.f : m;
+#pragma unroll
+        for (int i = 0; i < PL; ++i) {
+            const float f = fast_exp2(mine[i].x - mref);
+            l = fmaf(mine[i].y, f, l);
+            if (grp == 0) weight[lane + i * LPR] = f;
+        }
+#pragma unroll
+        for (int s = LPR / 2; s > 0; s >>= 1) l += __shfl_xor(l, s);
+        __syncthreads();
+#pragma unroll 8
+        for (int s = grp; s < pieces; s += GROUPS) add(s, weight[s]);
+        join_groups<LPR, GROUPS>(v);
+        if (grp > 0) return;
+    } else {
+        for (int s = 0; s < pieces; ++s) m = fmaxf(m, ml[s].x);
+        const float mref = m == kNegInf ? 0.f : m;
 #pragma unroll 4
-    for (int s = 0; s < pieces; ++s) {
-        const float f = fast_exp2(ml[s].x - mref);
-        l = fmaf(ml[s].y, f, l);
-        const float4 x = *reinterpret_cast<const float4 *>(pa + s * D);
-        v[0] = fmaf(x.x, f, v[0]); v[1] = fmaf(x.y, f, v[1]); v[2] = fmaf(x.z, f, v[2]); v[3] = fmaf(x.w, f, v[3]);
+        for (int s = 0; s < pieces; ++s) {
+            const float f = fast_exp2(ml[s].x - mref);
+            l = fmaf(ml[s].y, f, l);
+            add(s, f);
+        }
     }
     const float inv = l > 0.f ? 1.f / l : 0.f;
     T *op = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(O) + (int64_t)tok * a.o_row + (int64_t)head * a.o_head);
@@ -261,7 +298,11 @@ dsv_status launch_t(const PackedArgs &a, const void *Q, const void *K, const voi
         static_cast<const T *>(Q), static_cast<const T *>(K), static_cast<const T *>(V), static_cast<T *>(O), static_cast<bf16_t *>(O_tail), lse, pml, pacc, a);
     DSV_LAUNCH_CHECK();
     if (a.splits > 1) {
-        packed_fwd_merge_kernel<T, D><<<merge_blocks<D / 4>(a.total_q, a.Hq), 256, 0, st>>>(pml, pacc, static_cast<T *>(O), static_cast<bf16_t *>(O_tail), lse, a);
+        constexpr int LPR = D / 4, G = 256 / LPR;
+        if (wide_merge(a.splits, (int64_t)a.total_q * a.Hq))
+            packed_fwd_merge_kernel<T, D, G><<<merge_blocks<LPR, G>(a.total_q, a.Hq), 256, 0, st>>>(pml, pacc, static_cast<T *>(O), static_cast<bf16_t *>(O_tail), lse, a);
+        else
+            packed_fwd_merge_kernel<T, D, 1><<<merge_blocks<LPR, 1>(a.total_q, a.Hq), 256, 0, st>>>(pml, pacc, static_cast<T *>(O), static_cast<bf16_t *>(O_tail), lse, a);
         DSV_LAUNCH_CHECK();
     }
     return DSV_OK;

@@ -156,14 +156,15 @@ def test_tensors_that_the_binding_refuses(dsv):
     with pytest.raises(dsv.DsvError):
         dsv.layer_norm_bwd(n, x, None, torch.zeros(4, 2), torch.zeros(4, 2), x)
     from paper_2502_07590_amd import binding as b
-    c, cpu = b._CPacked(), torch.device("cpu")
+    c, cpu = b._CPacked.from_buffer_copy(p._c), torch.device("cpu")
+    assert (c.q.row, c.q.head, c.dv.row, c.dv.head) == (128, 64, 128, 64)      # contiguous until a tensor says otherwise
     for bad in (x[:3], x.float(), x.transpose(1, 2), torch.zeros(4, 2, 128, dtype=torch.bfloat16)[:, :, ::2], x[0]):
         with pytest.raises(dsv.DsvError):
             b._rows(c, "q", bad, (4, 2, 64), torch.bfloat16, cpu)
     b._rows(c, "q", x.transpose(0, 1).contiguous().transpose(0, 1), (4, 2, 64), torch.bfloat16, cpu)
     assert (c.q.row, c.q.head) == (64, 256)
-    b._rows(c, "q", x[:1].expand(1, 2, 64)[:, :1], (1, 1, 64), torch.bfloat16, cpu)
-    assert (c.q.row, c.q.head) == (64, 64)                  # axes of one step
+    b._rows(c, "q", x[:, :1], (4, 1, 64), torch.bfloat16, cpu)
+    assert (c.q.row, c.q.head) == (128, 64)                 # an axis of one step
     for bad in (cu.long(), cu[:1], torch.zeros(4, dtype=torch.int32)[::2]):
         with pytest.raises(dsv.DsvError):
             b._flat("cu_q", bad, (2,), torch.int32, cpu)
