@@ -3,7 +3,9 @@
 //   mu = mean x, r = 1 / sqrt(mean (x - mu)^2 + eps), xh = (x - mu) r, y = xh gamma + beta
 //   g = dy gamma;  dx = r (g - mean g - xh mean(g xh));  dgamma = sum over rows of dy xh, dbeta = sum over rows of dy
 //
-// Bound by memory: a row is read once into registers, LPR lanes to a row (8 .. 64 of a wave, or the whole block), CH elements a load.
+// Bound by memory: a row is read once into registers, LPR lanes to a row (8 .. 64 of a wave, or the whole block), CH elements a load, while
+// the row before it is worked on.  Of 64 M elements, bytes read and written over time: forward 5.0 .. 6.3 TB/s, backward with the sums of
+// dgamma and dbeta 4.0 .. 5.6 TB/s (a copy of 1 GiB: 5.1).  Without the read ahead the backward pass had 3.4 TB/s at n = 2048.
 // The variance is formed from the differences in registers, not from sums of squares.
 #include <algorithm>
 #include <type_traits>
@@ -71,16 +73,16 @@ template <int LPR> __device__ __forceinline__ float2 row_sums(float a, float b, 
 // Rows first, first + gridDim * RPB, ... of a lane group, as token and head without a division a row.
 template <int LPR> struct RowWalk {
     static constexpr int RPB = 256 / LPR;
-    int tok, head, step_tok, step_head;
-    int64_t id, step;
+    int head, step_head;
+    int64_t id, step, tok, step_tok;  // past the last token by up to a step
     __device__ __forceinline__ RowWalk(const NormArgs &a)
     {
         id = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR;
         step = (int64_t)gridDim.x * RPB;
-        tok = (int)(id / a.heads);
-        head = (int)(id - (int64_t)tok * a.heads);
-        step_tok = (int)(step / a.heads);
-        step_head = (int)(step - (int64_t)step_tok * a.heads);
+        tok = id / a.heads;
+        head = (int)(id - tok * a.heads);
+        step_tok = step / a.heads;
+        step_head = (int)(step - step_tok * a.heads);
     }
     __device__ __forceinline__ void next(const NormArgs &a)
     {
@@ -110,12 +112,16 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(const T *__restrict__ X, 
         if (gamma && in[i]) gp[i] = *reinterpret_cast<const Piece<T, CH> *>(gamma + e);
         if (beta && in[i]) bp[i] = *reinterpret_cast<const Piece<T, CH> *>(beta + e);
     }
-    for (RowWalk<LPR> w(a); w.tok < a.tokens; w.next(a)) {
+    Piece<T, CH> xp[NP];
+    auto load = [&](const RowWalk<LPR> &w) __attribute__((always_inline)) {
         const T *x = X + w.tok * a.x_row + w.head * a.x_head;
-        Piece<T, CH> xp[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i)
             if (in[i]) xp[i] = *reinterpret_cast<const Piece<T, CH> *>(x + (lane + i * LPR) * CH);
+    };
+    RowWalk<LPR> w(a);
+    if (w.tok < a.tokens) load(w);
+    while (w.tok < a.tokens) {
         float f[NP][CH], s = 0.f;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
@@ -132,6 +138,9 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(const T *__restrict__ X, 
                 f[i][c] -= mu;
                 s += in[i] ? f[i][c] * f[i][c] : 0.f;
             }
+        RowWalk<LPR> next = w;
+        next.next(a);
+        if (next.tok < a.tokens) load(next);  // on its way while this row is finished
         const float r = 1.f / sqrtf(fmaf(row_sums<LPR>(s, 0.f, red[1]).x, inv_n, a.eps));
         T *y = Y + w.tok * a.y_row + w.head * a.y_head;
 #pragma unroll
@@ -152,6 +161,7 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(const T *__restrict__ X, 
             mean[w.id] = mu;
             rstd[w.id] = r;
         }
+        w = next;
     }
 }
 
@@ -175,16 +185,32 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(const T *__restrict__ X, 
         for (int c = 0; c < CH; ++c) dg[i][c] = db[i][c] = 0.f;
     }
     int turn = 0;
-    for (RowWalk<LPR> w(a); w.tok < a.tokens; w.next(a)) {
+    Piece<T, CH> xn[NP], yn[NP];
+    float mun = 0.f, rn = 0.f;
+    auto load = [&](const RowWalk<LPR> &w) __attribute__((always_inline)) {
         const T *x = X + w.tok * a.x_row + w.head * a.x_head, *dy = dY + w.tok * a.dy_row + w.head * a.dy_head;
-        Piece<T, CH> xp[NP], yp[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i)
             if (in[i]) {
-                xp[i] = *reinterpret_cast<const Piece<T, CH> *>(x + (lane + i * LPR) * CH);
-                yp[i] = *reinterpret_cast<const Piece<T, CH> *>(dy + (lane + i * LPR) * CH);
+                xn[i] = *reinterpret_cast<const Piece<T, CH> *>(x + (lane + i * LPR) * CH);
+                yn[i] = *reinterpret_cast<const Piece<T, CH> *>(dy + (lane + i * LPR) * CH);
             }
-        const float mu = mean[w.id], r = rstd[w.id];
+        mun = mean[w.id];
+        rn = rstd[w.id];
+    };
+    RowWalk<LPR> w(a);
+    if (w.tok < a.tokens) load(w);
+    while (w.tok < a.tokens) {
+        Piece<T, CH> xp[NP], yp[NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            xp[i] = xn[i];
+            yp[i] = yn[i];
+        }
+        const float mu = mun, r = rn;
+        RowWalk<LPR> next = w;
+        next.next(a);
+        if (next.tok < a.tokens) load(next);  // on its way while this row is worked on
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
@@ -219,6 +245,7 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(const T *__restrict__ X, 
             }
             put(dx + (lane + i * LPR) * CH, o);
         }
+        w = next;
     }
     if (!part) return;
     // the block's lane groups joined, four pieces' worth of columns at a time
@@ -258,20 +285,22 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(const T *__restrict__ X, 
     }
 }
 
-// Columns of part summed over the blocks: 32 columns a block, eight rows at a time.
+// Columns of part summed over the blocks: eight columns a block, 32 rows at a time.
 __global__ __launch_bounds__(256) void norm_sum_kernel(const float *__restrict__ part, int blocks, int n, float *__restrict__ dgamma, float *__restrict__ dbeta)
 {
-    __shared__ float acc[8][33];
-    const int c = threadIdx.x & 31, g = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
+    __shared__ float acc[32][9];
+    const int c = threadIdx.x & 7, g = threadIdx.x >> 3, col = blockIdx.x * 8 + c;
     float v = 0.f;
     if (col < 2 * n) {
 #pragma unroll 8
-        for (int b = g; b < blocks; b += 8) v += part[(int64_t)b * 2 * n + col];
+        for (int b = g; b < blocks; b += 32) v += part[(int64_t)b * 2 * n + col];
     }
     acc[g][c] = v;
     __syncthreads();
     if (g == 0 && col < 2 * n) {
-        v = ((acc[0][c] + acc[1][c]) + (acc[2][c] + acc[3][c])) + ((acc[4][c] + acc[5][c]) + (acc[6][c] + acc[7][c]));
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v += acc[i][c];
         (col < n ? dgamma[col] : dbeta[col - n]) = v;
     }
 }
@@ -287,14 +316,18 @@ NormShape norm_shape(int n, int ch)
     const int pieces = (n + ch - 1) / ch;
     for (int lpr = 8; lpr <= 64; lpr *= 2)
         if (pieces <= lpr) return {lpr, 1};
-    for (int np = 2; np <= max_wave_np(ch); np *= 2)
-        if (pieces <= 64 * np) return {64, np};
+    for (int np : {2, 3, 4, 6, 8, 16})
+        if (np <= max_wave_np(ch) && pieces <= 64 * np) return {64, np};
     int np = 2;
     while (pieces > 256 * np) np *= 2;
     return {256, np};
 }
 int64_t norm_row_blocks(const NormArgs &a, int lpr) { return ((int64_t)a.tokens * a.heads + 256 / lpr - 1) / (256 / lpr); }
-constexpr int kFwdBlocks = 8192, kBwdBlocks = 1024;
+// Blocks of the two kernels, which then walk over the rows, each row's loads under way while the one before is worked on.  Backward: the more
+// elements a lane has, the more registers and the fewer blocks run at once, and each block leaves 2 n floats to sum.  64 M elements, us with
+// the sum, in 256, 512 and 768 blocks: bf16, 8 elements a lane (n 128) 128, 87, 83; 16 (n 1024) 88, 77, 93; 32 (n 2048) 83, 94, 100.
+constexpr int kFwdBlocks = 4096;
+int bwd_blocks(int per_lane) { return per_lane <= 8 ? 768 : per_lane <= 16 ? 512 : 256; }
 
 template <typename T, int CH, int LPR, int NP>
 dsv_status fwd_shape(const NormArgs &a, const T *X, const T *gamma, const T *beta, T *Y, float *mean, float *rstd, hipStream_t st)
@@ -307,13 +340,13 @@ template <typename T, int CH, int LPR, int NP>
 dsv_status bwd_shape(const NormArgs &a, const T *X, const T *gamma, const float *mean, const float *rstd, const T *dY, T *dX, float *dgamma, float *dbeta,
                      float *part, hipStream_t st)
 {
-    const int blocks = (int)std::min<int64_t>(norm_row_blocks(a, LPR), kBwdBlocks);
+    const int blocks = (int)std::min<int64_t>(norm_row_blocks(a, LPR), bwd_blocks(CH * NP));
     if (blocks > 0) {
         norm_bwd_kernel<T, CH, LPR, NP><<<blocks, 256, 0, st>>>(X, gamma, mean, rstd, dY, dX, part, a);
         DSV_LAUNCH_CHECK();
     }
     if (dgamma) {
-        norm_sum_kernel<<<(2 * a.n + 31) / 32, 256, 0, st>>>(part, blocks, a.n, dgamma, dbeta);
+        norm_sum_kernel<<<(2 * a.n + 7) / 8, 256, 0, st>>>(part, blocks, a.n, dgamma, dbeta);
         DSV_LAUNCH_CHECK();
     }
     return DSV_OK;
@@ -324,8 +357,8 @@ template <int CH, typename F> dsv_status with_shape(const NormShape &s, F f)
 {
 #define DSV_SHAPE(L, N) \
     if (s.lpr == L && s.np == N) return f(std::integral_constant<int, L>{}, std::integral_constant<int, N>{});
-    DSV_SHAPE(8, 1) DSV_SHAPE(16, 1) DSV_SHAPE(32, 1) DSV_SHAPE(64, 1) DSV_SHAPE(64, 2) DSV_SHAPE(64, 4)
-    if constexpr (CH < 8) { DSV_SHAPE(64, 8) }
+    DSV_SHAPE(8, 1) DSV_SHAPE(16, 1) DSV_SHAPE(32, 1) DSV_SHAPE(64, 1) DSV_SHAPE(64, 2) DSV_SHAPE(64, 3) DSV_SHAPE(64, 4)
+    if constexpr (CH < 8) { DSV_SHAPE(64, 6) DSV_SHAPE(64, 8) }
     if constexpr (CH == 1) { DSV_SHAPE(64, 16) }
     if constexpr (CH == 8) { DSV_SHAPE(256, 2) }
     if constexpr (CH > 1) { DSV_SHAPE(256, 4) }
@@ -365,7 +398,9 @@ dsv_status launch_norm_fwd(const NormArgs &a, int dtype, bool wide, const void *
 
 int norm_bwd_blocks(const NormArgs &a, int dtype, bool wide)
 {
-    return (int)std::min<int64_t>(norm_row_blocks(a, norm_shape(a.n, chunk_of(dtype, wide)).lpr), kBwdBlocks);
+    const int ch = chunk_of(dtype, wide);
+    const NormShape s = norm_shape(a.n, ch);
+    return (int)std::min<int64_t>(norm_row_blocks(a, s.lpr), bwd_blocks(ch * s.np));
 }
 
 dsv_status launch_norm_bwd(const NormArgs &a, int dtype, bool wide, const void *X, const void *gamma, const float *mean, const float *rstd, const void *dY,
