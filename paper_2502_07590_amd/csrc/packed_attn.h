@@ -209,10 +209,10 @@ __device__ __forceinline__ void tile_scores(const unsigned char *tile, int r, co
         pin_order();
     }
 }
-// The same of row r of two tiles, each by own rows of its own; between(m) is done between the products, m = 0 .. NM - 1.
-template <typename T, int D, typename F>
+// The same of row r of two tiles, each by own rows of its own
+template <typename T, int D>
 __device__ __forceinline__ void tile_scores2(const unsigned char *t1, const unsigned char *t2, int r, const Frag<T> (&own1)[D * sizeof(T) / 32],
-                                             const Frag<T> (&own2)[D * sizeof(T) / 32], floatx16_t &s1, floatx16_t &s2, F between)
+                                             const Frag<T> (&own2)[D * sizeof(T) / 32], floatx16_t &s1, floatx16_t &s2)
 {
     constexpr int NM = D * (int)sizeof(T) / 32;
     const int half = (threadIdx.x & 63) >> 5;
@@ -231,7 +231,6 @@ __device__ __forceinline__ void tile_scores2(const unsigned char *t1, const unsi
         s1 = product(f[m % kAhead][0], own1[m], s1);
         s2 = product(f[m % kAhead][1], own2[m], s2);
         if (m + kAhead < NM) fetch(m + kAhead);
-        between(m);
         pin_order();
     }
 }
@@ -336,29 +335,19 @@ template <int D> struct RowSum<float, D> {
         for (int nb = 0; nb < NB; ++nb) acc[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(f.v[nb], w.v[i], acc[nb], 0, 0, 0);
     }
 };
-// KT times 32 rows from r0; between(i) is done between the products, i = 0 .. KT STEPS - 1.
-template <typename T, int D, int KT, typename F>
-__device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const Weights<T> (&w)[KT], floatx16_t (&acc)[D / 32], F between)
-{
-    typedef RowSum<T, D> RS;
-    constexpr int N = KT * RS::STEPS, A = RS::AHEAD;
-    typename RS::Operand f[A];
-    auto fetch = [&](int i) __attribute__((always_inline)) { f[i % A] = RS::fetch(tile, r0 + 32 * (i / RS::STEPS), i % RS::STEPS); };
-#pragma unroll
-    for (int i = 0; i < A; ++i) fetch(i);
-    pin_order();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        RS::step(i % RS::STEPS, f[i % A], w[i / RS::STEPS], acc);
-        if (i + A < N) fetch(i + A);
-        between(i);
-        pin_order();
-    }
-}
 template <typename T, int D> __device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const Weights<T> &w, floatx16_t (&acc)[D / 32])
 {
-    const Weights<T> one[1] = {w};
-    weighted_rows<T, D, 1>(tile, r0, one, acc, [](int) {});
+    typedef RowSum<T, D> RS;
+    typename RS::Operand f[RS::AHEAD];
+#pragma unroll
+    for (int i = 0; i < RS::AHEAD; ++i) f[i] = RS::fetch(tile, r0, i);
+    pin_order();
+#pragma unroll
+    for (int i = 0; i < RS::STEPS; ++i) {
+        RS::step(i, f[i % RS::AHEAD], w, acc);
+        if (i + RS::AHEAD < RS::STEPS) f[i % RS::AHEAD] = RS::fetch(tile, r0, i + RS::AHEAD);
+        pin_order();
+    }
 }
 template <typename T, int D> __device__ __forceinline__ void weighted_rows(const unsigned char *tile, int r0, const floatx16_t &w, floatx16_t (&acc)[D / 32])
 {
@@ -412,13 +401,15 @@ __device__ __forceinline__ void store4(float *p, float a, float b, float c, floa
 
 // O rounded to its type, and what the rounding took (the backward's Delta = dO . O wants more than 8 bits of O: with O alone, queries that see
 // few keys get gradients 5e-3 off, with the tail 2.5e-3, the rounding of weights and results).
+__device__ __forceinline__ uint32_t tail_of(float a, float b)
+{
+    const uint32_t w = pack_bf16x2(a, b);
+    return pack_bf16x2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xFFFF0000u));
+}
 __device__ __forceinline__ void store_out(bf16_t *p, bf16_t *tail, float a, float b, float c, float d)
 {
-    const uint32_t w0 = pack_bf16x2(a, b), w1 = pack_bf16x2(c, d);
-    *reinterpret_cast<uint2 *>(p) = make_uint2(w0, w1);
-    if (tail)
-        *reinterpret_cast<uint2 *>(tail) = make_uint2(pack_bf16x2(a - __uint_as_float(w0 << 16), b - __uint_as_float(w0 & 0xFFFF0000u)),
-                                                      pack_bf16x2(c - __uint_as_float(w1 << 16), d - __uint_as_float(w1 & 0xFFFF0000u)));
+    store4(p, a, b, c, d);
+    if (tail) *reinterpret_cast<uint2 *>(tail) = make_uint2(tail_of(a, b), tail_of(c, d));
 }
 __device__ __forceinline__ void store_out(float *p, bf16_t *, float a, float b, float c, float d) { store4(p, a, b, c, d); }
 

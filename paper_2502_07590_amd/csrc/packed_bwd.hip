@@ -4,8 +4,8 @@
 //   dQ_i = scale sum_j dS_ij k_j;   dK_j = scale sum_i dS_ij q_i;   dV_j = sum_i p_ij dO_i   (i over the queries of every head that reads j's)
 //
 // Three kernels: the rows' statistics; dQ with a wave's 32 rows as columns against tiles of keys, as in the forward; dK and dV with a wave's 32
-// keys as columns against tiles of rows.  Scores and dP are formed in both, seven products where five would do, so that every sum has
-// one owner: no atomics, the same bits from run to run.
+// keys as columns against tiles of rows.  Scores and dP are formed in both, so that every sum has one owner: no atomics, the same bits from
+// run to run.  With dS as two bf16 words in dQ's product that makes eight products of 2 d operations a pair, where five would do.
 #include "packed_attn.h"
 
 namespace dsv {
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
         for (int t = 0; t < Sh::RT; ++t) {
             const int sub = (WK == 1 ? 0 : wave * 32) + 32 * t;
             floatx16_t s, dp;
-            tile_scores2<T, D>(kt, vt, sub + n, qf, gf, s, dp, [](int) {});
+            tile_scores2<T, D>(kt, vt, sub + n, qf, gf, s, dp);
             if (edge) {
                 const int lim = min(seen, kcut) - k0 - sub - 4 * half;
 #pragma unroll
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(256, 1) void packed_dkdv_few_kernel(
         const int sub = wave * 32;
         {
             floatx16_t s, dp;
-            tile_scores2<T, D>(qt, gt, sub + n, kf, vf, s, dp, [](int) {});
+            tile_scores2<T, D>(qt, gt, sub + n, kf, vf, s, dp);
             if (edge) {
                 const int lim = first_seen - r0 - sub - 4 * half;
 #pragma unroll

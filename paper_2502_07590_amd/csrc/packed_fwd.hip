@@ -202,10 +202,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
             else lse[(int64_t)head * a.total_q + sq.q0 + tok] = l > 0.f ? (mrun + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
         }
     } else {
-        if (row >= rows) return;
         const float inv = whole > 0.f ? 1.f / whole : 0.f;
         const int64_t rid = (int64_t)(sq.q0 + tok) * a.Hq + head;
         if (a.splits > 1) {
+            if (row >= rows) return;
             float *const pa = pacc + (rid * a.splits + split) * D;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
@@ -214,16 +214,44 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
                     store4(pa + 32 * nb + 8 * g + 4 * half, acc[nb][4 * g] * fair, acc[nb][4 * g + 1] * fair, acc[nb][4 * g + 2] * fair, acc[nb][4 * g + 3] * fair);
             if (half == 0) pml[rid * a.splits + split] = make_float2(mrun, l);
         } else {
-            T *op = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(O) + (int64_t)(sq.q0 + tok) * a.o_row + (int64_t)head * a.o_head);
+            // the wave's rows by way of LDS, so that they leave as whole lines
+            typedef RowTile<T, D> RT;
+            unsigned char *const mine = (wave < 2 ? ka : va) + (wave & 1) * (Sh::TILE / 2);
+            static_assert(Sh::TILE / 2 == 32 * RT::RB, "half a tile is a wave's rows");
+            auto place = [&](int r, int p) __attribute__((always_inline)) { return mine + r * RT::RB + ((p ^ (RT::PIECES == 8 ? (r >> 1) & 7 : r & 15)) << 4); };
+            auto send = [&](unsigned char *first, int64_t row_b, int64_t head_b) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < RT::PIECES / 2; ++i) {
+                    const int r = i * (64 / RT::PIECES) + lane / RT::PIECES, p = lane % RT::PIECES, ro = row0 + wave * 32 + r;
+                    const uint4 x = *reinterpret_cast<const uint4 *>(place(r, p));
+                    const int t = row_token(a, ro);
+                    if (ro < rows) *reinterpret_cast<uint4 *>(first + (int64_t)(sq.q0 + t) * row_b + (int64_t)(hk * a.group + ro - t * a.group) * head_b + p * 16) = x;
+                }
+            };
+            __syncthreads();
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int ch = 32 * nb + 8 * g + 4 * half;
-                    store_out(op + ch, O_tail ? O_tail + rid * D + ch : nullptr, acc[nb][4 * g] * inv, acc[nb][4 * g + 1] * inv,
-                              acc[nb][4 * g + 2] * inv, acc[nb][4 * g + 3] * inv);
+                    float v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = acc[nb][4 * g + i] * inv;
+                    const int ch = 32 * nb + 8 * g + 4 * half, at = ch * (int)sizeof(T);
+                    store4(reinterpret_cast<T *>(place(n, at >> 4) + (at & 15)), v[0], v[1], v[2], v[3]);
                 }
-            if (half == 0) lse[(int64_t)head * a.total_q + sq.q0 + tok] = l > 0.f ? (mrun + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+            send(reinterpret_cast<unsigned char *>(O), a.o_row, a.o_head);
+            if constexpr (sizeof(T) == 2)
+                if (O_tail) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            uint2 *const at = reinterpret_cast<uint2 *>(place(n, 4 * nb + g) + 8 * half);
+                            *at = make_uint2(tail_of(acc[nb][4 * g] * inv, acc[nb][4 * g + 1] * inv), tail_of(acc[nb][4 * g + 2] * inv, acc[nb][4 * g + 3] * inv));
+                        }
+                    send(reinterpret_cast<unsigned char *>(O_tail), (int64_t)a.Hq * D * 2, D * 2);
+                }
+            if (half == 0 && row < rows) lse[(int64_t)head * a.total_q + sq.q0 + tok] = l > 0.f ? (mrun + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
         }
     }
 }
