@@ -96,7 +96,7 @@ struct StepCost {
     double flops, rate;
     int results;
 };
-Walk plan_walk(const StepCost &cost, int d, bool causal, int64_t own, int64_t heads, int64_t n_seq, int64_t other, int64_t max_other)
+Walk plan_walk(const StepCost &cost, int d, bool causal, int64_t own, int64_t max_own, int64_t heads, int64_t n_seq, int64_t other, int64_t max_other)
 {
     constexpr int64_t kUnit = 128, kMinChunk = 256, kMaxSplits = 64, kCus = 256;
     Walk w{};
@@ -112,18 +112,29 @@ Walk plan_walk(const StepCost &cost, int d, bool causal, int64_t own, int64_t he
             chunk = std::max({work, kMinChunk, (max_other + kMaxSplits - 1) / kMaxSplits});
         }
     } else {
-        // The last round of blocks leaves CUs idle; pieces make rounds shorter, and cost writing and reading their results.  L = 20280, four
-        // heads, bf16, d = 128 (636 blocks): forward, dq, dkdv in one piece 1.01, 1.59, 1.77 ms, in four, four and two 0.88, 1.43, 1.62.
-        const double slots = (double)kCus * cost.per_cu, tiles = n_seq == 1 ? (double)((own + 127) / 128) : (double)(own / 128 + (n_seq + 1) / 2);
-        const double full = tiles * (double)heads * (double)other / ((double)n_seq * (double)std::max<int64_t>(max_other, 1)) * (causal ? 0.5 : 1.0);
-        const bool alike = n_seq == 1 && !causal;  // all blocks as long: whole rounds of them
-        const double block_s = cost.flops * d * 128.0 * (double)max_other / (cost.rate / slots);
-        const double piece_s = (double)own * (double)heads * d * 8.0 * cost.results / 4e12;  // written and read
+        // Without pieces the longest blocks set the time, or the CUs that run one block more than others; pieces cost writing and reading their
+        // results.  Times are in those of a block of 128 own rows by the longest other axis; one sequence is taken to be the longest, the rest alike.
+        // Measured, us with the joins, in one piece and as chosen: L = 20280, 4 heads, bf16, d = 128: forward 975, 889 (two); dq 1490, 1325 (two);
+        // dkdv 1622, 1529 (two).  Causal, 16384 tokens, 4 heads: forward 377, 351 (two); dq 551, 505 (two); dkdv 565 (one).  Causal, 4096 tokens, 4
+        // heads: 79, 48 (four); 118, 63 (four); 126, 67 (three).
+        const double cus = (double)kCus, rest = (double)(n_seq - 1), longest = (double)std::max<int64_t>(max_other, 1);
+        const double blocks = (double)((max_own + 127) / 128) * (double)heads;
+        double work = blocks;
+        if (n_seq > 1)
+            work += ((double)std::max<int64_t>(own - max_own, 0) / 128 + rest / 2) * (double)heads * (double)std::max<int64_t>(other - max_other, 0) / (rest * longest);
+        const double mean = work * (causal ? 0.5 : 1.0) / cus;
+        const double block_s = cost.flops * d * 128.0 * longest / (cost.rate / cus);  // with a CU to itself, were it then as fast as with others
+        const double alone = cost.per_cu > 1 ? 0.65 * cost.per_cu : 1.0;              // how much slower it is
+        const double piece_s = (double)own * (double)heads * d * 8.0 * cost.results * (causal ? 0.5 : 1.0) / 4e12;  // written and read
         double best = 0;
         for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
             if (s > pieces) break;
-            const double t = (alike ? std::ceil(full * s / slots) / s : std::max(full / slots, 1.0 / s)) * block_s + (s > 1 ? s * piece_s + 5e-6 : 0.0);
-            if (s == 1 || t < 0.97 * best) {
+            // blocks all alike come in whole rounds; of many lengths, longest first, they fill the CUs but for a little; their pieces are alike
+            // again, and a CU that runs one at a time is idle for half of one at the end
+            const double left = cost.per_cu > 1 ? 0.1 * cost.per_cu / s : s > 1 ? 0.5 / s : 0.1;
+            const double rounds = n_seq == 1 && !causal ? std::ceil(work * s / cus) / s : mean + left;
+            const double t = std::max(rounds, alone / s) * block_s + (s > 1 ? s * piece_s + 5e-6 : 0.0);
+            if (s == 1 || t < 0.965 * best) {
                 best = t;
                 chunk = (max_other + s - 1) / s;
             }
@@ -140,15 +151,15 @@ Walk walk_of(const dsv_packed &p, Step step)
 {
     const bool bf16 = p.dtype == DSV_BF16;
     const int64_t g = p.Hq / p.Hkv;
-    // flops of a pair and channel, and rates: as measured at 32768 tokens
+    // operations a pair and channel, and rates: as measured at 32768 tokens
     StepCost c{};
     c.per_cu = step == kDkdv ? (p.d == 64 ? 2 : 1) : bf16 ? (p.d == 64 ? 3 : 2) : (p.d == 64 ? 2 : 1);
     c.flops = step == kFwd ? 4 : 8;
     c.rate = bf16 ? 1.1e15 : 1e14;
     c.results = step == kDkdv ? 2 : 1;
     if (step == kDkdv)
-        return plan_walk(c, p.d, p.causal != 0, p.total_k, p.Hkv, p.n_seq, (int64_t)p.total_q * g, std::min(p.max_q, p.total_q) * g);
-    return plan_walk(c, p.d, p.causal != 0, (int64_t)p.total_q * g, p.Hkv, p.n_seq, p.total_k, std::min(p.max_k, p.total_k));
+        return plan_walk(c, p.d, p.causal != 0, p.total_k, std::min(p.max_k, p.total_k), p.Hkv, p.n_seq, (int64_t)p.total_q * g, std::min(p.max_q, p.total_q) * g);
+    return plan_walk(c, p.d, p.causal != 0, (int64_t)p.total_q * g, std::min(p.max_q, p.total_q) * g, p.Hkv, p.n_seq, p.total_k, std::min(p.max_k, p.total_k));
 }
 
 size_t fwd_bytes(const dsv_packed &p)

@@ -42,6 +42,13 @@ __device__ __forceinline__ Sequence read_sequence(const PackedArgs &a, int i)
     return s;
 }
 
+// Pieces of a.chunk keys that query token t of a sequence sees something of.
+__device__ __forceinline__ int pieces_seen(const PackedArgs &a, const Sequence &s, int t)
+{
+    const int seen = a.causal ? min(s.nk, t + s.nk - s.nq + 1) : s.nk;
+    return seen > 0 ? (seen + a.chunk - 1) / a.chunk : 0;
+}
+
 // Tiles of ROWS rows are numbered without a sum over the sequences before: sequence i's begin at floor(cu[i] * mul / ROWS) + i, which leaves
 // ceil(length / ROWS) places at least.  The owner of a place is the last sequence that begins at or before it; 64 candidates a step.
 // ROWS = 0: the tokens themselves, no place left empty (the owner of a token).
@@ -86,17 +93,27 @@ template <typename T, int D, int ROWS, int WAVES> struct RowLoads {
     static constexpr int N = ROWS * RT::RB / 1024 / WAVES, RPC = 1024 / RT::RB, STEP = WAVES * RPC;  // rows from a load to the next
     static constexpr int NV = STEP % 16 ? 2 : 1;  // turn() has a period of 16 rows
     static_assert(N * WAVES * 1024 == ROWS * RT::RB && (NV == 1 || STEP == 8), "every kilobyte has its wave");
-    uint32_t off[NV], piece[NV];
+    uint32_t off[NV], piece[NV], step_b;
     int wave;
     __device__ __forceinline__ int row(int i) const { return i * STEP + wave * RPC + (int)(threadIdx.x & 63) / RT::PIECES; }
-    __device__ __forceinline__ void set(int wave_, int64_t row_b)
+    __device__ __forceinline__ void set(int wave_, int64_t row_b)  // for keys()
     {
         wave = wave_;
+        step_b = (uint32_t)STEP * (uint32_t)row_b;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             piece[v] = (uint32_t)(((int)(threadIdx.x & 63) % RT::PIECES) ^ RT::turn(row(v))) << 4;
             off[v] = (uint32_t)row(0) * (uint32_t)row_b + piece[v];
         }
+    }
+    __device__ __forceinline__ void set(int wave_, int64_t row_b, const PackedArgs &a, int64_t head_b)  // for rows()
+    {
+        set(wave_, row_b);
+        if (a.group == 1) return;
+        step_b = STEP % a.group == 0 ? (uint32_t)(STEP / a.group) * (uint32_t)row_b : 0u;
+        const int tok = row_token(a, row(0));
+#pragma unroll
+        for (int v = 0; v < NV; ++v) off[v] = (uint32_t)tok * (uint32_t)row_b + (uint32_t)(row(0) - tok * a.group) * (uint32_t)head_b + piece[v];
     }
     __device__ __forceinline__ void send(const unsigned char *base, const uint32_t (&at)[N], unsigned char *lds) const
     {
@@ -107,9 +124,9 @@ template <typename T, int D, int ROWS, int WAVES> struct RowLoads {
         for (int i = 0; i < N; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (i * WAVES + wave) * 1024), 16, (int)at[i], 0, 0, 0);
     }
-    __device__ __forceinline__ void plain(int64_t row_b, int left, uint32_t (&at)[N]) const  // rows row_b apart, `left` of them to the end
+    // loads step_b apart, none behind the row at `last`
+    __device__ __forceinline__ void plain(uint32_t last, uint32_t (&at)[N]) const
     {
-        const uint32_t last = (uint32_t)(min(left, ROWS) - 1) * (uint32_t)row_b;
         uint32_t o[NV], p[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {  // hidden from the compiler, which would keep all N places in registers that the products need
@@ -118,13 +135,13 @@ template <typename T, int D, int ROWS, int WAVES> struct RowLoads {
             asm volatile("" : "+v"(o[v]), "+v"(p[v]));
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i) at[i] = min(o[i % NV] + (uint32_t)(i * STEP) * (uint32_t)row_b, last + p[i % NV]);
+        for (int i = 0; i < N; ++i) at[i] = min(o[i % NV] + (uint32_t)i * step_b, last + p[i % NV]);
     }
     // rows k0 .. of n that lie row_b apart
     __device__ __forceinline__ void keys(const unsigned char *first, int64_t row_b, int k0, int n, unsigned char *lds) const
     {
         uint32_t at[N];
-        plain(row_b, n - k0, at);
+        plain((uint32_t)(min(n - k0, ROWS) - 1) * (uint32_t)row_b, at);
         send(first + (int64_t)k0 * row_b, at, lds);
     }
     // rows r0 .. of n, row = token * group + head
@@ -133,7 +150,16 @@ template <typename T, int D, int ROWS, int WAVES> struct RowLoads {
         uint32_t at[N];
         const int tok0 = row_token(a, r0);
         if (a.group == 1) {
-            plain(row_b, n - r0, at);
+            plain((uint32_t)(min(n - r0, ROWS) - 1) * (uint32_t)row_b, at);
+        } else if (step_b && n - r0 >= ROWS) {  // whole tokens from a load to the next (the divisions and products below: a third of a tile's time)
+            uint32_t o[NV];
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                o[v] = off[v];
+                asm volatile("" : "+v"(o[v]));
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) at[i] = o[i % NV] + (uint32_t)i * step_b;
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) {

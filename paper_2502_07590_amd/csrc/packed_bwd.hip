@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && WK == 1 ? 2 : 1) void packed
     const int past = sq.nk - sq.nq, seen = a.causal ? min(sq.nk, tok + past + 1) : sq.nk;
     int kend = kcut;
     if (a.causal) kend = min(kend, row_token(a, min(row0 + Sh::OWN, rows) - 1) + past + 1);
-    if (a.chunk && kbeg >= sq.nk && split > 0) return;  // no such piece of this sequence
+    if (a.splits > 1 && kbeg >= kend) return;  // no row of this tile sees the piece: the sum does not read it
 
     Frag<T> qf[NM], gf[NM];
     {
@@ -204,8 +204,8 @@ __global__ __launch_bounds__(256, 1) void packed_dkdv_few_kernel(
     const int key = key0 + n, kc = min(key, sq.nk - 1);
     int rbeg = split * a.chunk;
     const int rend = a.chunk ? min(rows, rbeg + a.chunk) : rows;
-    if (a.chunk && rbeg >= rows && split > 0) return;  // no such piece of this sequence
     if (a.causal) rbeg = max(rbeg, max(0, key0 - past) * a.group / Sh::ROWS * Sh::ROWS);  // rows before see none of these keys
+    if (a.splits > 1 && rbeg >= rend) return;  // no row of the piece sees these keys: the sum does not read it
 
     Frag<T> kf[NM], vf[NM];
     {
@@ -222,8 +222,8 @@ __global__ __launch_bounds__(256, 1) void packed_dkdv_few_kernel(
     const float2 *const sp = stat + (int64_t)hk * a.total_q * a.group + (int64_t)sq.q0 * a.group;
     float2 sn = make_float2(-kNegInf, 0.f);
     RowLoads<T, D, Sh::ROWS, 4> ql, gl;
-    ql.set(wave, a.q_row);
-    gl.set(wave, a.do_row);
+    ql.set(wave, a.q_row, a, a.q_head);
+    gl.set(wave, a.do_row, a, a.do_head);
     auto request = [&](int r0, unsigned char *qt, unsigned char *gt) __attribute__((always_inline)) {
         ql.rows(a, qp, a.q_row, a.q_head, r0, rows, qt);
         gl.rows(a, gp, a.do_row, a.do_head, r0, rows, gt);
@@ -338,8 +338,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkdv_kernel(
     const int key = key0 + wave * 32 + n, kc = min(key, sq.nk - 1);
     int rbeg = split * a.chunk;
     const int rend = a.chunk ? min(rows, rbeg + a.chunk) : rows;
-    if (a.chunk && rbeg >= rows && split > 0) return;  // no such piece of this sequence
     if (a.causal) rbeg = max(rbeg, max(0, key0 - past) * a.group / Sh::ROWS * Sh::ROWS);  // rows before see none of these keys
+    if (a.splits > 1 && rbeg >= rend) return;  // no row of the piece sees these keys: the sum does not read it
 
     Frag<T> kf[NM], vf[NM];
     {
@@ -360,8 +360,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_dkdv_kernel(
     const float2 *const sp = stat + (int64_t)hk * a.total_q * a.group + (int64_t)sq.q0 * a.group;
     float2 sn = make_float2(-kNegInf, 0.f);
     RowLoads<T, D, Sh::ROWS, 4> ql, gl;
-    ql.set(wave, a.q_row);
-    gl.set(wave, a.do_row);
+    ql.set(wave, a.q_row, a, a.q_head);
+    gl.set(wave, a.do_row, a, a.do_head);
     auto request = [&](int r0, unsigned char *qt, unsigned char *gt) __attribute__((always_inline)) {
         ql.rows(a, qp, a.q_row, a.q_head, r0, rows, qt);
         gl.rows(a, gp, a.do_row, a.do_head, r0, rows, gt);
@@ -497,12 +497,14 @@ __global__ __launch_bounds__(256) void packed_sum_kernel(const float *__restrict
     const Sequence sq = read_sequence(a, __builtin_amdgcn_readfirstlane(find_sequence(KEYS ? a.cu_k : a.cu_q, a.n_seq, total, 1, 0, tok)));
     const int t0 = KEYS ? sq.k0 : sq.q0, nt = KEYS ? sq.nk : sq.nq;
     if (tok < t0 || tok >= t0 + nt || head >= heads) return;
-    const int pieces = max(1, ((KEYS ? sq.nq * a.group : sq.nk) + a.chunk - 1) / a.chunk);
+    // of rows that see the key, or of keys that the row sees
+    const int first = KEYS && a.causal ? min(max(tok - t0 - (sq.nk - sq.nq), 0), sq.nq) * a.group / a.chunk : 0;
+    const int pieces = KEYS ? (sq.nq * a.group + a.chunk - 1) / a.chunk : pieces_seen(a, sq, tok - t0);
     const bool second = KEYS && blockIdx.y;
     const float *p = (second ? p1 : p0) + ((int64_t)tok * heads + head) * a.splits * D + 4 * lane;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-    for (int s = grp; s < pieces; s += GROUPS) {
+    for (int s = first + grp; s < pieces; s += GROUPS) {
         const float4 x = *reinterpret_cast<const float4 *>(p + (int64_t)s * D);
         v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
     }

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
     const int past = sq.nk - sq.nq, seen = a.causal ? min(sq.nk, tok + past + 1) : sq.nk;
     int kend = kcut;
     if (a.causal) kend = min(kend, row_token(a, min(row0 + Sh::ROWS, rows) - 1) + past + 1);
-    if (a.chunk && kbeg >= sq.nk && split > 0) return;  // no such piece of this sequence: the merge does not look for it
+    if (a.splits > 1 && kbeg >= kend) return;  // no row of this tile sees the piece: the merge does not read it
 
     Frag<T> qf[NM];
     {
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(256) void packed_fwd_merge_kernel(const float2 *__r
     const Sequence sq = read_sequence(a, __builtin_amdgcn_readfirstlane(find_sequence(a.cu_q, a.n_seq, a.total_q, 1, 0, tok)));
     if (tok < sq.q0 || tok >= sq.q0 + sq.nq || head >= a.Hq) return;
     const int64_t rid = (int64_t)tok * a.Hq + head;
-    const int pieces = max(1, (sq.nk + a.chunk - 1) / a.chunk);
+    const int pieces = pieces_seen(a, sq, tok - sq.q0);
     const float2 *const ml = pml + rid * a.splits;
     const float *const pa = pacc + rid * a.splits * D + 4 * lane;
     float v[4] = {0.f, 0.f, 0.f, 0.f}, m = kNegInf, l = 0.f;
