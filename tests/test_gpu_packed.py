@@ -262,3 +262,92 @@ def test_a_captured_step_replays_on_other_lengths():
         assert math.isfinite(float(scratch))
         for n in out:      # the inputs of both cases are the same: one seed
             assert torch.equal(out[n], expect[n]), (rep, n)
+
+
+@pytest.mark.parametrize("dtype,d,Hq,Hkv,causal", [("bf16", 128, 4, 4, False), ("bf16", 128, 4, 4, True), ("bf16", 64, 8, 2, True), ("f32", 64, 4, 2, True),
+                                                   ("f32", 128, 3, 3, False), ("bf16", 64, 4, 4, False)])
+def test_large_tiles_in_pieces(dtype, d, Hq, Hkv, causal):
+    """Tiles of 128 rows that see the long axis in pieces, the pieces of short sequences and those that no row sees among them."""
+    lens = [2100, 300, 1, 190] if causal else [2300]
+    c = Case(lens, lens, Hq, Hkv, d, dtype, causal)
+    assert dsv.packed_attn_fwd_workspace(c.p) >= 2 * sum(lens) * Hq * d * 4
+    assert dsv.packed_attn_bwd_workspace(c.p) >= 2 * sum(lens) * Hq * d * 4 + sum(lens) * Hq * 8
+    c.check()
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_pieces_of_unequal_sides(causal):
+    """More queries than keys and more keys than queries, large tiles, pieces; causal: queries that see no key, keys seen by all."""
+    for lens_q, lens_k in (([1500, 700], [2600, 300]), ([2600, 300], [1500, 700])):
+        c = Case(lens_q, lens_k, 4, 2, 64, "bf16", causal)
+        assert dsv.packed_attn_fwd_workspace(c.p) > 0
+        c.check()
+
+
+@pytest.mark.parametrize("d,group", [(128, 2), (128, 8), (128, 16), (128, 32), (64, 2), (64, 16), (64, 32), (128, 5), (64, 6)])
+@pytest.mark.parametrize("layout", ["token", "head"])
+def test_groups_of_shared_heads(d, group, layout):
+    """As many heads to a group as a load brings rows, fewer, more and no divisor of it; tiles that end inside a token's heads."""
+    Hkv = 16 if group < 8 else 4
+    lens = [430, 1, 130, 77]
+    Case(lens, lens, Hkv * group, Hkv, d, "bf16", True, layout).check()
+
+
+def _wide(x, width):
+    """x [T, H, d] in rows of `width` elements."""
+    T, H, d = x.shape
+    return torch.empty(T * width, dtype=x.dtype, device=x.device)[: T * width].view(T, width)[:, : H * d].unflatten(1, (H, d)).copy_(x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_behind_four_gigabytes(dtype):
+    """A long cache of wide rows, and its gradients in such rows; then as many queries."""
+    T, width = 70001, 1 << 15
+    for lens_q, lens_k in (([1], [T]), ([T], [40])):
+        c = Case(lens_q, lens_k, 1, 1, 64, dtype, causal=lens_q == [1])
+        assert T * width * c.Q.element_size() > 1 << 32
+        if lens_k[0] == T:
+            c.K, c.V = _wide(c.K, width), _wide(c.V, width)
+            more = dict(dK=_wide(c.K, width), dV=_wide(c.V, width))
+        else:
+            c.Q, c.dO = _wide(c.Q, width), _wide(c.dO, width)
+            more = dict(dQ=_wide(c.Q, width))
+        O, lse = dsv.packed_attn_fwd(c.p, c.Q, c.K, c.V, *c.dcu, O=None if lens_k[0] == T else _wide(c.Q, width))
+        dQ, dK, dV = dsv.packed_attn_bwd(c.p, c.Q, c.K, c.V, *c.dcu, O, lse, c.dO, **more)
+        torch.cuda.synchronize()
+        want = c.want(tail=False)
+        for n, x in dict(O=O, lse=lse, dQ=dQ, dK=dK, dV=dV).items():
+            ref.assert_within(n, x, want[n])
+        del c, O, dQ, dK, dV, more
+        torch.cuda.empty_cache()
+
+
+def test_two_graphs_share_a_workspace():
+    """Replayed in turn with eager calls between; every call finds the workspace as the one before left it."""
+    a = Case([1, 1, 1], [1500, 700, 33], 8, 2, 128, "bf16", True)
+    b = Case([900], [900], 4, 4, 64, "bf16")
+    size = max(f(c.p) for c in (a, b) for f in (dsv.packed_attn_fwd_workspace, dsv.packed_attn_bwd_workspace))
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    graphs, outs, eager = [], [], [c.run(tail=False) for c in (a, b)]
+    for c, e in zip((a, b), eager):
+        out = {n: torch.zeros_like(x) for n, x in e.items()}
+
+        def step(c=c, out=out):
+            dsv.packed_attn_fwd(c.p, c.Q, c.K, c.V, *c.dcu, O=out["O"], lse=out["lse"], workspace=ws)
+            dsv.packed_attn_bwd(c.p, c.Q, c.K, c.V, *c.dcu, out["O"], out["lse"], c.dO, dQ=out["dQ"], dK=out["dK"], dV=out["dV"], workspace=ws)
+
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step()
+        graphs.append(g)
+        outs.append(out)
+    for rep in range(3):
+        for g, out, c, e in zip(graphs, outs, (a, b), eager):
+            for x in out.values():
+                x.zero_()
+            if rep:
+                ws.fill_(255)
+            g.replay()
+            again = c.run(tail=False)
+            for n in out:
+                assert torch.equal(out[n], e[n]) and torch.equal(again[n], e[n]), (rep, n)

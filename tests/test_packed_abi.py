@@ -2,6 +2,8 @@
 reference the GPU tests compare with, against brute force and differences.  CPU only."""
 import ctypes
 import math
+import os
+import subprocess
 
 import pytest
 import torch
@@ -11,7 +13,6 @@ import packed_ref as ref
 
 @pytest.fixture(scope="module")
 def dsv():
-    import os
     import paper_2502_07590_amd as m
     if not os.path.exists(m.library_path()):
         from paper_2502_07590_amd.build import build_library
@@ -226,3 +227,32 @@ def test_reference_norm_is_torchs_and_its_gradients_the_differences():
     e[3] = 1e-6
     assert abs((loss(X, gamma + e, beta) - loss(X, gamma - e, beta)) / 2e-6 - float(out["dgamma"][0][3])) < 1e-7
     assert abs((loss(X, gamma, beta + e) - loss(X, gamma, beta - e)) / 2e-6 - float(out["dbeta"][0][3])) < 1e-7
+
+
+def test_host_code_under_address_and_undefined_sanitizers(tmp_path):
+    """Split plans and workspace sizes over the range of a descriptor's numbers; device code is built as always and never launched."""
+    from concurrent.futures import ThreadPoolExecutor
+
+    from paper_2502_07590_amd.build import CSRC, HIPCC_FLAGS, _hipcc
+    here = os.path.dirname(os.path.abspath(__file__))
+    san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=all", "-g"]
+    flags = [f for f in HIPCC_FLAGS if f != "-O3"] + ["-O1"]
+
+    def run(cmd, **kw):
+        res = subprocess.run(cmd, capture_output=True, text=True, **kw)
+        assert res.returncode == 0, f"{' '.join(cmd)}\n{res.stdout[-2000:]}\n{res.stderr[-4000:]}"
+        return res
+
+    def compile_one(src):
+        obj = str(tmp_path / (src + ".o"))
+        run([_hipcc(), *flags, *san, "-c", os.path.join(CSRC, src), "-o", obj])
+        return obj
+
+    with ThreadPoolExecutor(max_workers=4) as ex:
+        objs = list(ex.map(compile_one, ["api_packed.hip", "packed_fwd.hip", "packed_bwd.hip", "norm.hip"]))
+    main_o, exe = str(tmp_path / "main.o"), str(tmp_path / "packed_san")
+    run([_hipcc(), "--offload-arch=gfx950", "-O1", "-g", "-std=c++17", *san, "-I", os.path.join(os.path.dirname(here), "include"), "-c", "-x", "c++",
+         os.path.join(here, "sanitize", "packed_checks_main.cpp"), "-o", main_o])
+    run([_hipcc(), "--offload-arch=gfx950", *san, "-o", exe, main_o, *objs])
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:abort_on_error=0", UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1")
+    assert "packed checks sanitizer run ok" in run([exe], env=env).stdout
