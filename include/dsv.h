@@ -5,7 +5,8 @@
  * low-rank projections of Q and K; stage 2 (dsv_sparse_attn_fwd / dsv_sparse_attn_bwd) computes
  * exact softmax attention, and its gradients, over only those keys.
  *
- * Conventions that hold for every entry point
+ * Conventions that hold for every entry point (packed attention and layer norm, whose descriptors have strides and sequence lengths of
+ * their own, say where they differ)
  *   - Tensor pointers are DEVICE pointers owned by the caller, contiguous, row-major, no strides:
  *       Q, K, V, O, dO, dQ, dK, dV : [B, H, L, d]   element type dsv_problem.dtype
  *       Wq, Wk                     : [H, d, r]      same element type (one predictor pair per head)
@@ -332,12 +333,15 @@ DSV_API dsv_status dsv_profile_sparsity(const dsv_problem *p, const void *Q, con
  *     but no access outside the tensors.  Rows that belong to no sequence are left as they are, in every output, and may hold anything.
  *   - O_tail (bf16; NULL: not wanted; must be NULL for F32): bf16 [total_q, Hq, d], contiguous, what rounding O took away.  Given to the
  *     backward, it forms Delta from all 16 bits: gradients within 3e-3 of the exact ones (relative, in norm), where O alone leaves 3 to 6e-3.
- *   - scale: 1e-30 to 1e30.  The weights enter the second product as bf16 (bf16 tensors), everything else is held in 32 bits.  The same
- *     results from run to run, bit for bit.
- *   - Limits: Hkv divides Hq; total_q * Hq * (Hq / Hkv) < 2^32; total_q * Hq / 32 + n_seq * Hkv < 2^24, and so for total_k * Hkv;
- *     anything larger: DSV_EUNSUPPORTED.  total_q, total_k of 0 are accepted, the tensors may then be NULL.
- *   - Workspace: the forward's, of calls with few rows, for partial results of pieces of the key axis (else the query returns 0); the backward's
- *     for two floats a row and partial sums. */
+ *   - scale: 1e-30 to 1e30.  bf16 tensors: the weights enter the products of O and dV as bf16 (O is the average by the weights as they were
+ *     rounded), dS that of dK as bf16 and that of dQ as two bf16 words; every sum, score and statistic is held in 32 bits.  fp32 tensors:
+ *     everything.  The same results from run to run, bit for bit.
+ *   - No output may overlap an input or another output; slices of one tensor, as dQ, dK and dV of a fused projection's gradient, do not.
+ *   - Limits: Hkv divides Hq; total_q * Hq * (Hq / Hkv) < 2^32; total_q * Hq / 32 + n_seq * Hkv < 2^24, and so for total_k * Hkv; strides below
+ *     2^40, of Q, K, V and dO 128 from token to token below 4 GB (the backward: and Hq / Hkv - 1 from head to head with them); anything
+ *     larger: DSV_EUNSUPPORTED (strides of 2^40: DSV_EINVAL).  total_q, total_k of 0 are accepted, the tensors may then be NULL.
+ *   - Workspace: the forward's for partial results of pieces of the key axis (calls that would not fill the chip without; else the query
+ *     returns 0); the backward's for two floats a row and such pieces. */
 typedef struct dsv_rows {
     int64_t row, head;   /* elements from one token, from one head, to the next */
 } dsv_rows;

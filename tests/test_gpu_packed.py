@@ -272,7 +272,14 @@ def test_large_tiles_in_pieces(dtype, d, Hq, Hkv, causal):
     c = Case(lens, lens, Hq, Hkv, d, dtype, causal)
     assert dsv.packed_attn_fwd_workspace(c.p) >= 2 * sum(lens) * Hq * d * 4
     assert dsv.packed_attn_bwd_workspace(c.p) >= 2 * sum(lens) * Hq * d * 4 + sum(lens) * Hq * 8
-    c.check()
+    out = c.check(tail=False)
+    # nothing is read of the workspace that this call has not written
+    ws = torch.full((max(dsv.packed_attn_fwd_workspace(c.p), dsv.packed_attn_bwd_workspace(c.p)),), 255, dtype=torch.uint8, device=DEV)
+    O, lse = dsv.packed_attn_fwd(c.p, c.Q, c.K, c.V, *c.dcu, workspace=ws)
+    ws.fill_(255)
+    dQ, dK, dV = dsv.packed_attn_bwd(c.p, c.Q, c.K, c.V, *c.dcu, O, lse, c.dO, workspace=ws)
+    for n, x in dict(O=O, lse=lse, dQ=dQ, dK=dK, dV=dV).items():
+        assert torch.equal(x, out[n]), n
 
 
 @pytest.mark.parametrize("causal", [False, True])
@@ -351,3 +358,37 @@ def test_two_graphs_share_a_workspace():
             again = c.run(tail=False)
             for n in out:
                 assert torch.equal(out[n], e[n]) and torch.equal(again[n], e[n]), (rep, n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_keys_or_no_queries_at_all(dtype):
+    c = Case([5, 0, 130], [0, 0, 0], 4, 2, 64, dtype, True)
+    out = c.run()
+    assert (out["O"] == 0).all() and (out["lse"] == -math.inf).all() and (out["dQ"] == 0).all() and out["dK"].shape == (0, 2, 64)
+    c = Case([0, 0], [3, 200], 4, 2, 64, dtype)
+    dK, dV = torch.full_like(c.K, 7), torch.full_like(c.V, 7)
+    O, lse = dsv.packed_attn_fwd(c.p, c.Q, c.K, c.V, *c.dcu)
+    dsv.packed_attn_bwd(c.p, c.Q, c.K, c.V, *c.dcu, O, lse, c.dO, dK=dK, dV=dV)
+    assert O.shape == (0, 4, 64) and (dK == 0).all() and (dV == 0).all()
+
+
+@pytest.mark.parametrize("dtype,side", [("bf16", "keys"), ("bf16", "queries"), ("f32", "keys"), ("f32", "queries")])
+def test_the_widest_rows(dtype, side):
+    """128 rows of just under 4 GB: the last 32-bit offsets inside a tile, for heads of their own and shared ones."""
+    width = (1 << 25) // ref.DTYPES[dtype].itemsize - 16
+    for Hq, T in ((2, 131), (4, 130)):
+        c = Case([T], [T], Hq, 2, 128, dtype, True)
+        more = {}
+        if side == "keys":
+            c.K, c.V = _wide(c.K, width), _wide(c.V, width)
+        else:
+            c.Q, c.dO = _wide(c.Q, width), _wide(c.dO, width)
+            more = dict(O=_wide(c.Q, width))
+        O, lse = dsv.packed_attn_fwd(c.p, c.Q, c.K, c.V, *c.dcu, **more)
+        dQ, dK, dV = (torch.full(x.shape, float("nan"), dtype=x.dtype, device=DEV) for x in (c.Q, c.K, c.V))
+        dsv.packed_attn_bwd(c.p, c.Q, c.K, c.V, *c.dcu, O, lse, c.dO, dQ=dQ, dK=dK, dV=dV)
+        want = c.want(tail=False)
+        for n, x in dict(O=O, lse=lse, dQ=dQ, dK=dK, dV=dV).items():
+            ref.assert_within(n, x, want[n])
+        del c, O, more
+        torch.cuda.empty_cache()
