@@ -92,6 +92,7 @@ struct Walk {
 // A step's cost: blocks of 128 rows a CU runs at once, operations a pair of rows (and channel), the rate it reaches with the chip full, and
 // how many results a piece leaves per own row.
 struct StepCost {
+    bool bf16;
     int per_cu;
     double flops, rate;
     int results;
@@ -105,11 +106,34 @@ Walk plan_walk(const StepCost &cost, int d, bool causal, int64_t own, int64_t ma
     // small tiles where large ones would be mostly empty, or not fill the chip even in the shortest pieces
     w.few = own / n_seq <= 64 || (own / 128 + 1) * heads * pieces < kCus;
     int64_t chunk = max_other;
+    const double rest = (double)(n_seq - 1), longest = (double)std::max<int64_t>(max_other, 1);
+    const double rest_own = (double)std::max<int64_t>(own - max_own, 0), rest_other = n_seq > 1 ? (double)std::max<int64_t>(other - max_other, 0) / rest : 0.0;
     if (w.few) {
-        const int64_t tiles = own / 32 + n_seq;
-        if (tiles * heads < 4 * kCus) {  // pieces so long that all blocks together walk about 512 of them
-            const int64_t work = (int64_t)((double)tiles / (double)n_seq * (double)other * (double)heads) / (2 * kCus);
-            chunk = std::max({work, kMinChunk, (max_other + kMaxSplits - 1) / kMaxSplits});
+        if (max_own <= 32) {
+            // One tile a sequence and head, the other axis read once: bound by memory, and pieces of any number fill it; so long that all blocks
+            // together walk about 512 of them.
+            const double tiles = (double)(own / 32 + n_seq) / (double)n_seq;
+            chunk = std::max({(int64_t)(tiles * (double)other * (double)heads) / (2 * kCus), kMinChunk, (max_other + kMaxSplits - 1) / kMaxSplits});
+        } else {
+            // Rounds of blocks, by what a block takes: the walk, and as long as two tiles of 128 to begin and to join.  Forward, us, by the rule
+            // above and by this one: fp32, 1024 + 700 tokens, two heads, d = 64: 23.4 (four pieces), 19.3 (two); 2048 tokens, one head, d = 128:
+            // fp32 45.4 (six), 31.0 (four), bf16 17.1 (six), 16.7 (eight).
+            const double at_once = (double)kCus * (cost.bf16 ? 2 : 1);
+            const double tiles = (double)((max_own + 31) / 32), more = rest_own / 32 + rest / 2;
+            double best = 0;
+            int64_t before = 0;
+            for (int64_t s = 1; s <= std::min(kMaxSplits, (max_other + kMinChunk - 1) / kMinChunk); ++s) {
+                const int64_t c = ((max_other + s - 1) / s + kUnit - 1) / kUnit * kUnit;
+                if (c == before) continue;
+                before = c;
+                const double of_longest = (double)((max_other + c - 1) / c), seen = causal ? 0.75 + 0.25 / of_longest : 1.0;
+                const double blocks = (double)heads * (tiles * of_longest + more * std::max(1.0, std::ceil(rest_other / (double)c))) * seen;
+                const double t = std::ceil(blocks / at_once) * (2.0 + (double)c / 128) + (s > 1 ? 1.0 : 0.0);
+                if (s == 1 || t < best) {
+                    best = t;
+                    chunk = c;
+                }
+            }
         }
     } else {
         // Without pieces the longest blocks set the time, or the CUs that run one block more than others; pieces cost writing and reading their
@@ -117,11 +141,11 @@ Walk plan_walk(const StepCost &cost, int d, bool causal, int64_t own, int64_t ma
         // Measured, us with the joins, in one piece and as chosen: L = 20280, 4 heads, bf16, d = 128: forward 975, 889 (two); dq 1490, 1325 (two);
         // dkdv 1622, 1529 (two).  Causal, 16384 tokens, 4 heads: forward 377, 351 (two); dq 551, 505 (two); dkdv 565 (one).  Causal, 4096 tokens, 4
         // heads: 79, 48 (four); 118, 63 (four); 126, 67 (three).
-        const double cus = (double)kCus, rest = (double)(n_seq - 1), longest = (double)std::max<int64_t>(max_other, 1);
+        const double cus = (double)kCus;
         const double blocks = (double)((max_own + 127) / 128) * (double)heads;
         double work = blocks;
         if (n_seq > 1)
-            work += ((double)std::max<int64_t>(own - max_own, 0) / 128 + rest / 2) * (double)heads * (double)std::max<int64_t>(other - max_other, 0) / (rest * longest);
+            work += (rest_own / 128 + rest / 2) * (double)heads * rest_other / longest;
         const double mean = work * (causal ? 0.5 : 1.0) / cus;
         const double block_s = cost.flops * d * 128.0 * longest / (cost.rate / cus);  // with a CU to itself, were it then as fast as with others
         const double alone = cost.per_cu > 1 ? 0.65 * cost.per_cu : 1.0;              // how much slower it is
@@ -153,6 +177,7 @@ Walk walk_of(const dsv_packed &p, Step step)
     const int64_t g = p.Hq / p.Hkv;
     // operations a pair and channel, and rates: as measured at 32768 tokens
     StepCost c{};
+    c.bf16 = bf16;
     c.per_cu = step == kDkdv ? (p.d == 64 ? 2 : 1) : bf16 ? (p.d == 64 ? 3 : 2) : (p.d == 64 ? 2 : 1);
     c.flops = step == kFwd ? 4 : 8;
     c.rate = bf16 ? 1.1e15 : 1e14;
