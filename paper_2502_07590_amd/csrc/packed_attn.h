@@ -443,22 +443,24 @@ __device__ __forceinline__ void store_out(float *p, bf16_t *, float a, float b, 
 // last token (whole waves), heads past the last one are the caller's to leave out.  Else a block takes one row, GROUPS pieces at a time.
 template <int LPR, int GROUPS> __device__ __forceinline__ bool merge_row(int total, int heads, int &tok, int &head)
 {
+    const uint32_t block = blockIdx.z * gridDim.x + blockIdx.x;  // below 2^28: total * heads is below 2^29
     if constexpr (GROUPS > 1) {
-        tok = (int)(blockIdx.x / (unsigned)heads);
-        head = (int)(blockIdx.x - (unsigned)tok * (unsigned)heads);
+        tok = (int)(block / (uint32_t)heads);
+        head = (int)(block - (uint32_t)tok * (uint32_t)heads);
     } else {
         constexpr int HPW = 64 / LPR;
-        const int per = (heads + HPW - 1) / HPW;
-        const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const uint32_t per = ((uint32_t)heads + HPW - 1) / HPW, w = block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         tok = (int)(w / per);
-        head = (int)(w - (int64_t)tok * per) * HPW + (threadIdx.x & 63) / LPR;
+        head = (int)(w - (uint32_t)tok * per) * HPW + (threadIdx.x & 63) / LPR;
     }
     return tok < total;
 }
-template <int LPR, int GROUPS> __host__ __forceinline__ unsigned merge_blocks(int64_t total, int heads)
+// Their grid, twice for y = 2.  Along x as many blocks as keep their threads below 2^32, the rest along z.
+template <int LPR, int GROUPS> __host__ __forceinline__ dim3 merge_grid(int64_t total, int heads, int y = 1)
 {
     constexpr int HPW = 64 / LPR;
-    return GROUPS > 1 ? (unsigned)(total * heads) : (unsigned)((total * ((heads + HPW - 1) / HPW) + 3) / 4);
+    const int64_t n = GROUPS > 1 ? total * heads : (total * ((heads + HPW - 1) / HPW) + 3) / 4, most = 1 << 22;
+    return dim3((unsigned)(n < most ? n : most), (unsigned)y, (unsigned)((n + most - 1) / most));
 }
 // A row of many pieces has a block to itself where that is not too many blocks.
 __host__ __forceinline__ bool wide_merge(int splits, int64_t rows) { return splits > 8 && rows < 65536; }

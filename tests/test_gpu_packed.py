@@ -392,3 +392,30 @@ def test_the_widest_rows(dtype, side):
             ref.assert_within(n, x, want[n])
         del c, O, more
         torch.cuda.empty_cache()
+
+
+def test_more_rows_than_one_axis_of_a_grid_takes():
+    """17 million queries: the kernels with a wave to a few rows need a second axis.  64 bits on the GPU, over three keys."""
+    T, nk, d = (1 << 24) + 1000, 3, 64
+    torch.manual_seed(3)
+    Q, dO = (torch.randn(T, 1, d, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    K, V = (torch.randn(nk, 1, d, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    cu = [torch.tensor([0, n], dtype=torch.int32, device=DEV) for n in (T, nk)]
+    p = dsv.Packed(1, T, nk, T, nk, 1, 1, d, "bf16", 0.125)
+    O, lse = dsv.packed_attn_fwd(p, Q, K, V, *cu)
+    dQ, dK, dV = dsv.packed_attn_bwd(p, Q, K, V, *cu, O, lse, dO)
+    k, v = K[:, 0].double(), V[:, 0].double()
+    for lo in range(0, T, 1 << 22):
+        q, do = Q[lo : lo + (1 << 22), 0].double(), dO[lo : lo + (1 << 22), 0].double()
+        x = 0.125 * q @ k.t().contiguous()
+        P = torch.softmax(x, 1)
+        o = P @ v
+        ds = P * (do @ v.t().contiguous() - (do * o).sum(1, keepdim=True))
+        # O: its rounding and the weights', 2^-8 of the values each; dQ: O's rounding in Delta (sum |dO O|) beside the result's own
+        part = slice(lo, lo + q.shape[0])
+        assert ((O[part, 0].double() - o).abs() <= 2.0 ** -8 * o.abs() + 2.0 ** -7 * P @ v.abs()).all()
+        assert (lse[0, part].double() - torch.logsumexp(x, 1)).abs().max() < 1e-4      # (d + 4) 2^-24 of scale sum |q k|, below 100 / 8
+        off = 2.0 ** -7 * (do.abs() * (o.abs() + P @ v.abs())).sum(1, keepdim=True)
+        dq, tol = 0.125 * ds @ k, 0.125 * (2.0 ** -8 * ds.abs() + P * off) @ k.abs()
+        assert ((dQ[part, 0].double() - dq).abs() <= tol + 2.0 ** -8 * dq.abs()).all()
+    assert dK.isfinite().all() and dV.isfinite().all()
