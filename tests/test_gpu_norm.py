@@ -56,6 +56,13 @@ def test_rows_from_one_to_more_than_the_blocks_take_at_once(tokens, heads, n, dt
     check(tokens, heads, n, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens,heads,n", [(140000, 1, 8), (45000, 3, 64), (140000, 1, 3), (17000, 1, 520), (4500, 1, 4104)])
+def test_more_rows_than_either_kernel_takes_at_once(tokens, heads, n, dtype):
+    """Every lane group walks: 4096 blocks of the forward, of 32 rows for the narrowest, of one for the widest."""
+    check(tokens, heads, n, dtype)
+
+
 @pytest.mark.parametrize("layout", ["head", "slice"])
 @pytest.mark.parametrize("n", [64, 77, 128])
 def test_views(layout, n):
