@@ -6,9 +6,10 @@
 // O^T = V^T P^T: a lane then holds one row's scores, the maximum and the sum are its own but for one exchange between the halves, and
 // the scores are where the second product wants them.
 //
-// Long calls are bound by products and exponentials that overlap only as the two waves of a SIMD happen to (a tile of 64 keys, d = 128: 1056
-// cycles of products, about 960 of vector work; products busy 56 % of the time a CU has blocks): 32768 tokens, 4 heads, d = 128, bf16 2.1 ms,
-// 1030 TFLOP/s, where a large library product has 1350.  Single queries against long caches are bound by memory: 104 MB of K and V in
+// Long calls are bound by power: 1.83 GHz of 2.4 under products and exponentials together (a tile of 64 keys, d = 128: 1056 cycles of
+// products, about 960 of vector work a wave, two waves a SIMD; products busy 56 % of the time a CU has blocks, and laying the weights of
+// half a tile between the products of the other changes nothing): 32768 tokens, 4 heads, d = 128, bf16 2.1 ms, 1030 TFLOP/s, where a large
+// library product has 1350. Single queries against long caches are bound by memory: 104 MB of K and V in
 // 24 + 4 us with the join, 3.7 TB/s.  Few keys (34128 queries of 16 heads against 77 .. 512, d = 64): 57 us, half of it Q and O themselves, the
 // rest the chain from lengths to rows to scores of a block that walks two to eight tiles.  fp32 is bound by its products (64 cycles each):
 // 1724 tokens of two heads, d = 64, 15 + 4 us.
