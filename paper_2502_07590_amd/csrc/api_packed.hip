@@ -43,7 +43,7 @@ dsv_status check_packed(const dsv_packed *p, bool grad)
     }
     // the kernels place the rows of a tile by 32-bit offsets from its first
     const int64_t most = 1ll << 32, group = p->Hq / p->Hkv;
-    for (const dsv_rows *s : {&p->q, &p->k, &p->v, &p->dO})
+    for (const dsv_rows *s : {&p->q, &p->k, &p->v, grad ? &p->dO : &p->q})  // the forward reads no layout of the backward: those may hold anything
         if (128 * s->row * (int64_t)es >= most) return DSV_EUNSUPPORTED;
     for (const dsv_rows *s : {&p->q, &p->dO})
         if (grad && 128 * s->row * (int64_t)es + (group - 1) * s->head * (int64_t)es >= most) return DSV_EUNSUPPORTED;
@@ -54,7 +54,7 @@ dsv_status check_packed(const dsv_packed *p, bool grad)
     return DSV_OK;
 }
 
-PackedArgs packed_args(const dsv_packed &p, const int32_t *cu_q, const int32_t *cu_k)
+PackedArgs packed_args(const dsv_packed &p, bool grad, const int32_t *cu_q, const int32_t *cu_k)
 {
     const int64_t es = (int64_t)esize(p.dtype);
     PackedArgs a{};
@@ -75,11 +75,12 @@ PackedArgs packed_args(const dsv_packed &p, const int32_t *cu_q, const int32_t *
     a.k_row = p.k.row * es, a.k_head = p.k.head * es;
     a.v_row = p.v.row * es, a.v_head = p.v.head * es;
     a.o_row = p.o.row * es, a.o_head = p.o.head * es;
+    a.splits = 1;
+    if (!grad) return a;
     a.do_row = p.dO.row * es, a.do_head = p.dO.head * es;
     a.dq_row = p.dq.row * es, a.dq_head = p.dq.head * es;
     a.dk_row = p.dk.row * es, a.dk_head = p.dk.head * es;
     a.dv_row = p.dv.row * es, a.dv_head = p.dv.head * es;
-    a.splits = 1;
     return a;
 }
 
@@ -256,7 +257,7 @@ dsv_status dsv_packed_attn_fwd(const dsv_packed *p, const void *Q, const void *K
     if (st != DSV_OK) return st;
     if (p->total_q == 0) return DSV_OK;
     const Walk w = walk_of(*p, kFwd);
-    PackedArgs a = packed_args(*p, cu_q, cu_k);
+    PackedArgs a = packed_args(*p, false, cu_q, cu_k);
     a.splits = w.splits;
     a.chunk = w.chunk;
     return launch_packed_fwd(a, p->dtype, p->d, w.few, Q, K, V, O, O_tail, lse, static_cast<char *>(workspace), static_cast<hipStream_t>(hip_stream));
@@ -282,7 +283,7 @@ dsv_status dsv_packed_attn_bwd(const dsv_packed *p, const void *Q, const void *K
     if (st != DSV_OK) return st;
     const Walk q = walk_of(*p, kDq), k = walk_of(*p, kDkdv);
     const PackedBwdPlan plan{q.few, k.few, q.splits, q.chunk, k.splits, k.chunk};
-    return launch_packed_bwd(packed_args(*p, cu_q, cu_k), plan, p->dtype, p->d, Q, K, V, O, O_tail, lse, dO, dQ, dK, dV, static_cast<char *>(workspace),
+    return launch_packed_bwd(packed_args(*p, true, cu_q, cu_k), plan, p->dtype, p->d, Q, K, V, O, O_tail, lse, dO, dQ, dK, dV, static_cast<char *>(workspace),
                              static_cast<hipStream_t>(hip_stream));
 }
 
