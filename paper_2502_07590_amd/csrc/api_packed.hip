@@ -15,12 +15,13 @@ bool ok_strides(const dsv_rows &s, size_t es)
     const int64_t unit = 16 / (int64_t)es, most = (int64_t)1 << 40;
     return s.row >= 0 && s.head >= 0 && s.row < most && s.head < most && s.row % unit == 0 && s.head % unit == 0;
 }
+typedef __int128 wide_t;  // counts below 2^31 times strides below 2^40: more than 64 bits
 bool rows_apart(const dsv_rows &s, int64_t rows, int64_t heads, int64_t n)
 {
     if (rows <= 1 && heads <= 1) return true;
     if (rows <= 1) return s.head >= n;
     if (heads <= 1) return s.row >= n;
-    return (s.head >= n && s.row >= (heads - 1) * s.head + n) || (s.row >= n && s.head >= (rows - 1) * s.row + n);
+    return (s.head >= n && s.row >= (wide_t)(heads - 1) * s.head + n) || (s.row >= n && s.head >= (wide_t)(rows - 1) * s.row + n);
 }
 
 dsv_status check_packed(const dsv_packed *p, bool grad)
@@ -46,7 +47,7 @@ dsv_status check_packed(const dsv_packed *p, bool grad)
     for (const dsv_rows *s : {&p->q, &p->k, &p->v, grad ? &p->dO : &p->q})  // the forward reads no layout of the backward: those may hold anything
         if (128 * s->row * (int64_t)es >= most) return DSV_EUNSUPPORTED;
     for (const dsv_rows *s : {&p->q, &p->dO})
-        if (grad && 128 * s->row * (int64_t)es + (group - 1) * s->head * (int64_t)es >= most) return DSV_EUNSUPPORTED;
+        if (grad && ((wide_t)128 * s->row + (wide_t)(group - 1) * s->head) * (int64_t)es >= most) return DSV_EUNSUPPORTED;
     // row / group by a 32-bit reciprocal, and the blocks of a launch
     if ((int64_t)p->total_q * p->Hq >= 1ll << 31 || (int64_t)p->total_q * p->Hq * (p->Hq / p->Hkv) >= 1ll << 32) return DSV_EUNSUPPORTED;
     if ((int64_t)p->total_q * p->Hq / 32 + (int64_t)p->n_seq * p->Hkv >= 1 << 24) return DSV_EUNSUPPORTED;

@@ -38,3 +38,50 @@ def test_the_forward_reads_no_layout_of_the_backward(dsv, dtype, left):
     assert dsv.packed_attn_fwd_workspace(p) == need
     assert fwd(dsv, p, ONE, need - 1) == -3
     assert bwd(dsv, p, ONE, 0) in (-1, -2)                             # which the backward does read
+
+
+# heads * stride just below a multiple of 2^64: in 64 bits the last head would lie before the first
+FAR = (1 << 40) - 8
+
+
+@pytest.mark.parametrize("name", ["dq", "dk", "dv"])
+def test_output_rows_on_one_another_behind_64_bits(dsv, name):
+    heads = 15728640
+    p = dsv.Packed(1, 2, 2, 2, 2, heads, heads, 64, "bf16", 0.1)
+    for other in ("q", "k", "v", "o", "dO", "dq", "dk", "dv"):
+        setattr(p._c, other, (64, 128))
+    assert bwd(dsv, p, None, 0) == -3
+    setattr(p._c, name, (0, FAR))
+    assert bwd(dsv, p, None, 0) == -1
+    p = dsv.Norm(2, 64, "bf16", heads=(1 << 30) - 1)
+    p._c.dx = (0, (1 << 34) + (1 << 6))
+    assert dsv.load_library().dsv_layer_norm_bwd(p.c, *[ONE] * 8, None, 0, None) == -1
+
+
+def test_layouts_under_address_and_undefined_sanitizers(tmp_path):
+    """Strides over their range, in host code built with sanitizers; device code is built as always and never launched."""
+    from concurrent.futures import ThreadPoolExecutor
+
+    from paper_2502_07590_amd.build import CSRC, HIPCC_FLAGS, _hipcc
+    here = os.path.dirname(os.path.abspath(__file__))
+    san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=all", "-g"]
+    flags = [f for f in HIPCC_FLAGS if f != "-O3"] + ["-O1"]
+
+    def run(cmd, **kw):
+        res = subprocess.run(cmd, capture_output=True, text=True, **kw)
+        assert res.returncode == 0, f"{' '.join(cmd)}\n{res.stdout[-2000:]}\n{res.stderr[-4000:]}"
+        return res
+
+    def compile_one(src):
+        obj = str(tmp_path / (src + ".o"))
+        run([_hipcc(), *flags, *san, "-c", os.path.join(CSRC, src), "-o", obj])
+        return obj
+
+    with ThreadPoolExecutor(max_workers=4) as ex:
+        objs = list(ex.map(compile_one, ["api_packed.hip", "packed_fwd.hip", "packed_bwd.hip", "norm.hip"]))
+    main_o, exe = str(tmp_path / "main.o"), str(tmp_path / "layouts_san")
+    run([_hipcc(), "--offload-arch=gfx950", "-O1", "-g", "-std=c++17", *san, "-I", os.path.join(os.path.dirname(here), "include"), "-c", "-x", "c++",
+         os.path.join(here, "sanitize", "packed_layouts_main.cpp"), "-o", main_o])
+    run([_hipcc(), "--offload-arch=gfx950", *san, "-o", exe, main_o, *objs])
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:abort_on_error=0", UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1")
+    assert "packed layouts sanitizer run ok" in run([exe], env=env).stdout
