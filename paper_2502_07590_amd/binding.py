@@ -505,15 +505,28 @@ def profile_sparsity(p: Problem, Q, K, rows, mass: float = 0.9, ema=None, alpha:
 
 
 # ---- full attention over packed sequences, layer norm -------------------------------------------------
+_INT32_MAX = 2 ** 31 - 1
+
+
+def _int32(what: str, x) -> int:
+    """x for a field of 32 bits, which would hold its lower half without a word."""
+    x = int(x)
+    if not -_INT32_MAX - 1 <= x <= _INT32_MAX:
+        raise DsvError(f"{what}: {x} does not fit 32 bits")
+    return x
+
+
 class Packed:
-    """Host-side descriptor of packed sequences (mirrors struct dsv_packed; the calls fill in the layouts of their tensors)."""
+    """Host-side descriptor of packed sequences (mirrors struct dsv_packed; the calls fill in the layouts of their tensors).  max_q, max_k may
+    be any number above the longest sequence."""
 
     def __init__(self, n_seq: int, total_q: int, total_k: int, max_q: int, max_k: int, Hq: int, Hkv: int, d: int, dtype, scale: float,
                  causal: bool = False):
         if isinstance(dtype, str):
             dtype = _DTYPE_NAME[dtype]
-        self.n_seq, self.total_q, self.total_k, self.max_q, self.max_k = int(n_seq), int(total_q), int(total_k), int(max_q), int(max_k)
-        self.Hq, self.Hkv, self.d, self.scale, self.causal = int(Hq), int(Hkv), int(d), float(scale), bool(causal)
+        self.n_seq, self.total_q, self.total_k = _int32("n_seq", n_seq), _int32("total_q", total_q), _int32("total_k", total_k)
+        self.max_q, self.max_k = _int32("max_q", min(max_q, _INT32_MAX)), _int32("max_k", min(max_k, _INT32_MAX))  # no sequence is longer than that
+        self.Hq, self.Hkv, self.d, self.scale, self.causal = _int32("Hq", Hq), _int32("Hkv", Hkv), _int32("d", d), float(scale), bool(causal)
         self.torch_dtype = dtype
         self.q_shape, self.k_shape = (self.total_q, self.Hq, self.d), (self.total_k, self.Hkv, self.d)
         q, k = _CRows(self.Hq * self.d, self.d), _CRows(self.Hkv * self.d, self.d)
@@ -531,7 +544,7 @@ class Norm:
     def __init__(self, tokens: int, n: int, dtype, eps: float = 1e-5, heads: int = 1):
         if isinstance(dtype, str):
             dtype = _DTYPE_NAME[dtype]
-        self.tokens, self.n, self.eps, self.heads = int(tokens), int(n), float(eps), int(heads)
+        self.tokens, self.n, self.eps, self.heads = _int32("tokens", tokens), _int32("n", n), float(eps), _int32("heads", heads)
         self.torch_dtype = dtype
         self.shape = (self.tokens, self.heads, self.n)
         rows = _CRows(self.heads * self.n, self.n)

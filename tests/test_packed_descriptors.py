@@ -85,3 +85,31 @@ def test_layouts_under_address_and_undefined_sanitizers(tmp_path):
     run([_hipcc(), "--offload-arch=gfx950", *san, "-o", exe, main_o, *objs])
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:abort_on_error=0", UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1")
     assert "packed layouts sanitizer run ok" in run([exe], env=env).stdout
+
+
+PACKED = dict(n_seq=3, total_q=300, total_k=400, max_q=200, max_k=300, Hq=8, Hkv=2, d=128, dtype="bf16", scale=0.1)
+NORM = dict(tokens=100, n=128, dtype="bf16", eps=1e-5, heads=4)
+
+
+@pytest.mark.parametrize("far", [1 << 31, (1 << 32) + 4, 1 << 64, -(1 << 31) - 1, -(1 << 32)])
+def test_numbers_outside_a_field_are_refused(dsv, far):
+    """Cut to 32 bits they would describe another call: 2^32 + 4 heads four, 2^32 tokens none."""
+    for name in ("n_seq", "total_q", "total_k", "Hq", "Hkv", "d"):
+        with pytest.raises(dsv.DsvError, match=name):
+            dsv.Packed(**{**PACKED, name: far})
+    for name in ("tokens", "n", "heads"):
+        with pytest.raises(dsv.DsvError, match=name):
+            dsv.Norm(**{**NORM, name: far})
+
+
+def test_limits_that_are_none(dsv):
+    """No sequence is longer than all tokens, and those fit a field: a limit that does not, limits nothing."""
+    plain = dsv.Packed(**{**PACKED, "max_q": (1 << 31) - 1, "max_k": (1 << 31) - 1})
+    for far in (1 << 31, 1 << 32, (1 << 32) + 4, 1 << 64):
+        p = dsv.Packed(**{**PACKED, "max_q": far, "max_k": far})
+        assert (p._c.max_q, p._c.max_k) == ((1 << 31) - 1,) * 2
+        assert dsv.packed_attn_fwd_workspace(p) == dsv.packed_attn_fwd_workspace(plain)
+        assert dsv.packed_attn_bwd_workspace(p) == dsv.packed_attn_bwd_workspace(plain) > 0
+    for name in ("max_q", "max_k"):
+        with pytest.raises(dsv.DsvError, match=name):
+            dsv.Packed(**{**PACKED, name: -(1 << 32)})
