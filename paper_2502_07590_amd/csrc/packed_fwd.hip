@@ -27,6 +27,10 @@ template <typename T, int D, int WK> struct FwdShape {
     static constexpr int NBUF = WK == 1 || (sizeof(T) == 4 && D == 64) ? 2 : 1;  // fp32 is bound by the products: two blocks on a CU would leave others idle
 };
 
+// lse of a row whose weights, against m, add up to l.  Only a sum of zero is one over no keys: a score that is no number, or infinite, makes l no
+// number, and lse and O with it; taken for a row without keys it would have gradients of zero.
+__device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? kNegInf : (m + __builtin_amdgcn_logf(l)) * kLn2; }
+
 template <typename T, int D, int WK>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2) void packed_fwd_kernel(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V,
                                                                                         T *__restrict__ O, bf16_t *__restrict__ O_tail, float *__restrict__ lse,
@@ -159,7 +163,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
     l = halves_sum(l);
     // O is the average by the weights that were summed, lse the logarithm of the unrounded ones': rounding then moves weight between the keys and
     // adds none (bf16, against 64 bits: O 2.4e-3 off when divided by l, 1.9e-3 by lr, 1.7e-3 the rounding of O alone)
-    const float whole = sizeof(T) == 2 ? halves_sum(lr) : l, fair = whole > 0.f ? l / whole : 0.f;
+    const float whole = sizeof(T) == 2 ? halves_sum(lr) : l, fair = whole == 0.f ? 0.f : l / whole;
     if constexpr (WK > 1) {  // the waves' sums over their keys, joined in LDS: wave w then holds channels 32 w / 4 .. of every row
         __shared__ float sm[128], sl[128];
         auto area = [&](int w) __attribute__((always_inline)) {  // 32 rows of D sums
@@ -190,7 +194,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
         mrun = m2;
         __syncthreads();
         if (row >= rows) return;
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
         const int64_t rid = (int64_t)(sq.q0 + tok) * a.Hq + head;
         for (int g = wave * 2 + half; g < D / 4; g += 8) {
             float v[4] = {0.f, 0.f, 0.f, 0.f};
@@ -208,10 +212,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
         }
         if (wave == 0 && half == 0) {
             if (a.splits > 1) pml[rid * a.splits + split] = make_float2(mrun, l);
-            else lse[(int64_t)head * a.total_q + sq.q0 + tok] = l > 0.f ? (mrun + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+            else lse[(int64_t)head * a.total_q + sq.q0 + tok] = row_lse(mrun, l);
         }
     } else {
-        const float inv = whole > 0.f ? 1.f / whole : 0.f;
+        const float inv = whole == 0.f ? 0.f : 1.f / whole;
         const int64_t rid = (int64_t)(sq.q0 + tok) * a.Hq + head;
         if (a.splits > 1) {
             if (row >= rows) return;
@@ -260,7 +264,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
                         }
                     send(reinterpret_cast<unsigned char *>(O_tail), (int64_t)a.Hq * D * 2, D * 2);
                 }
-            if (half == 0 && row < rows) lse[(int64_t)head * a.total_q + sq.q0 + tok] = l > 0.f ? (mrun + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+            if (half == 0 && row < rows) lse[(int64_t)head * a.total_q + sq.q0 + tok] = row_lse(mrun, l);
         }
     }
 }
@@ -319,10 +323,10 @@ __global__ __launch_bounds__(256) void packed_fwd_merge_kernel(const float2 *__r
             add(s, f);
         }
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     T *op = reinterpret_cast<T *>(reinterpret_cast<unsigned char *>(O) + (int64_t)tok * a.o_row + (int64_t)head * a.o_head);
     store_out(op + 4 * lane, O_tail ? O_tail + rid * D + 4 * lane : nullptr, v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-    if (lane == 0) lse[(int64_t)head * a.total_q + tok] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+    if (lane == 0) lse[(int64_t)head * a.total_q + tok] = row_lse(m, l);
 }
 
 template <typename T, int D, int WK>

@@ -1,4 +1,4 @@
-"""Packed attention on the GPU: roundings that it says it keeps, in norm; sums over its longest row axis."""
+"""Packed attention on the GPU: roundings that it says it keeps, in norm; rows that are not numbers; sums over its longest row axis."""
 import math
 
 import pytest
@@ -48,6 +48,64 @@ def test_the_output_and_its_tail_are_the_average_by_the_rounded_weights(lens_q, 
     assert rnd.off(O.double() + tail.double(), want) < 5e-4
     assert rnd.off(O, want) > 1e-3                       # what the tail holds
     assert (tail.float().abs() <= 2.0 ** -8 * O.float().abs()).all()
+
+
+NAN = [
+    dict(lens_q=[40, 50], lens_k=[40, 50], Hq=4, Hkv=2, d=64),                              # tiles of 32 rows
+    dict(lens_q=[1] * 4, lens_k=[2500, 1200, 31, 700], Hq=4, Hkv=2, d=128),                 # and in pieces
+    dict(lens_q=[1, 1], lens_k=[20000, 300], Hq=4, Hkv=2, d=128),                           # more than eight
+    dict(lens_q=[300, 129, 511, 128], lens_k=[300, 129, 511, 128], Hq=32, Hkv=32, d=64),    # tiles of 128 rows
+    dict(lens_q=[2300, 190], lens_k=[2300, 190], Hq=4, Hkv=4, d=128),                       # and in pieces
+    dict(lens_q=[2300, 190], lens_k=[2300, 190], Hq=4, Hkv=2, d=64),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("form", range(len(NAN)))
+@pytest.mark.parametrize("where", ["query", "key", "infinite score"])
+def test_scores_that_are_no_numbers_are_not_taken_for_no_keys(form, dtype, causal, where):
+    """A row with such a score has no O, no lse and no gradient that is a number, and so have the keys it sees; other sequences and heads keep
+    theirs bit for bit, other rows of its tile (sums are rescaled for all of a wave's rows at once) within the bounds."""
+    c = Case(dtype=dtype, causal=causal, seed=form, **NAN[form])
+    clean = c.run()
+    g, Hkv = c.p.Hq // c.p.Hkv, c.p.Hkv
+    s = 1                                                # the sequence, K/V head and row or key of it
+    a, b = slice(int(c.cu_q[s]), int(c.cu_q[s + 1])), slice(int(c.cu_k[s]), int(c.cu_k[s + 1]))
+    nq, nk, hk = a.stop - a.start, b.stop - b.start, Hkv - 1
+    i, j = nq - 1 - nq // 3, nk // 3
+    rows = torch.zeros(c.p.total_q, c.p.Hq, dtype=torch.bool, device=DEV)                   # that see such a score
+    if where == "key":
+        c.K[b.start + j, hk, 5] = float("nan")
+        rows[a.start + (max(0, j - (nk - nq)) if causal else 0) : a.stop, hk * g : (hk + 1) * g] = True
+    else:
+        if where == "query":
+            c.Q[a.start + i, hk * g, 5] = float("nan")
+        else:
+            c.Q[a.start + i, hk * g] = 1e25
+            c.K[b.start + j, hk] = 1e25
+        rows[a.start + i, hk * g] = True
+    seen = torch.zeros(c.p.total_k, Hkv, dtype=torch.bool, device=DEV)                      # keys that such a row sees
+    last = (nq - 1 if where == "key" else i) + nk - nq if causal else nk - 1
+    assert not causal or j <= last
+    seen[b.start : b.start + last + 1, hk] = True
+    mine, mine_k = torch.zeros_like(rows), torch.zeros_like(seen)                           # the sequence and heads that it is among
+    mine[a, hk * g : (hk + 1) * g], mine_k[b, hk] = True, True
+    got = c.run()
+    assert got["lse"].t()[rows].isnan().all()
+    for n in ("O", "dQ"):
+        assert got[n][rows].isnan().all(), n
+        assert torch.equal(got[n][~mine], clean[n][~mine]), n
+    for n in ("dK", "dV"):
+        assert not got[n][seen].isfinite().any(), n
+        assert torch.equal(got[n][~mine_k], clean[n][~mine_k]), n
+    assert torch.equal(got["lse"].t()[~mine], clean["lse"].t()[~mine])
+    if where == "query" or where == "key" and causal:    # rows that do not see it
+        want = c.want(grad=False)                        # from the inputs as they were
+        for n in ("O", "lse"):
+            value, bound = want[n]
+            value[rows.t().cpu() if n == "lse" else rows.cpu()] = float("nan")
+            ref.assert_within(n, got[n], (value, bound))
 
 
 def test_sums_over_seventeen_million_rows():
