@@ -483,6 +483,13 @@ template <int LPR, int GROUPS> __device__ __forceinline__ void join_groups(float
     }
 }
 
+// LDS that lanes of one wave write for others of it: keeps the compiler from moving accesses, of whatever types, across the point.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 __device__ __forceinline__ void wait_loads_and_sync()
 {
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): a barrier alone does not wait for loads into LDS

@@ -252,9 +252,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
                     const int ch = 32 * nb + 8 * g + 4 * half, at = ch * (int)sizeof(T);
                     store4(reinterpret_cast<T *>(place(n, at >> 4) + (at & 15)), v[0], v[1], v[2], v[3]);
                 }
+            wave_sync();
             send(reinterpret_cast<unsigned char *>(O), a.o_row, a.o_head);
             if constexpr (sizeof(T) == 2)
                 if (O_tail) {
+                    wave_sync();
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -262,6 +264,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
                             uint2 *const at = reinterpret_cast<uint2 *>(place(n, 4 * nb + g) + 8 * half);
                             *at = make_uint2(tail_of(acc[nb][4 * g] * inv, acc[nb][4 * g + 1] * inv), tail_of(acc[nb][4 * g + 2] * inv, acc[nb][4 * g + 3] * inv));
                         }
+                    wave_sync();
                     send(reinterpret_cast<unsigned char *>(O_tail), (int64_t)a.Hq * D * 2, D * 2);
                 }
             if (half == 0 && row < rows) lse[(int64_t)head * a.total_q + sq.q0 + tok] = row_lse(mrun, l);
