@@ -329,13 +329,16 @@ DSV_API dsv_status dsv_profile_sparsity(const dsv_problem *p, const void *Q, con
  *     must keep its rows apart (one at least d, the other beyond all of those).
  *   - lse: float [Hq, total_q].  cu_q, cu_k: DEVICE int32 [n_seq + 1], ascending from 0.  They are read by the kernels only: a call that
  *     was captured into a graph replays on whatever lengths they hold then, within the descriptor's limits.  max_q, max_k (HOST) bound
- *     the lengths; sequences longer than that, and entries that are not ascending or point behind the tensors, give undefined results
+ *     the lengths (INT32_MAX: no bound); sequences longer than that, and entries that are not ascending or point behind the tensors, give undefined results
  *     but no access outside the tensors.  Rows that belong to no sequence are left as they are, in every output, and may hold anything.
  *   - O_tail (bf16; NULL: not wanted; must be NULL for F32): bf16 [total_q, Hq, d], contiguous, what rounding O took away.  Given to the
  *     backward, it forms Delta from all 16 bits: gradients within 3e-3 of the exact ones (relative, in norm), where O alone leaves 3 to 6e-3.
+ *   - As for every call, inputs are taken to be finite.  Of those that are not: a row with a score that is no number has NaN in O, lse and dQ,
+ *     and the keys it sees in dK and dV.  A weight of zero is multiplied like any other, so a row of K, V, Q or dO that is not finite also reaches
+ *     rows of its own sequence that causal order hides it from, up to 190 tokens away.
  *   - scale: 1e-30 to 1e30.  bf16 tensors: the weights enter the products of O and dV as bf16 (O is the average by the weights as they were
- *     rounded), dS that of dK as bf16 and that of dQ as two bf16 words; every sum, score and statistic is held in 32 bits.  fp32 tensors:
- *     everything.  The same results from run to run, bit for bit.
+ *     rounded), dS that of dK as bf16 and that of dQ as two bf16 words; every sum, score and statistic is held in 32 bits.  (dsv_sparse_attn_fwd
+ *     keeps weights as two words in most of its forms: O 1.7e-3 from the exact one in norm, here up to 1.9e-3.)  fp32 tensors: everything.  The same results from run to run, bit for bit.
  *   - No output may overlap an input or another output; slices of one tensor, as dQ, dK and dV of a fused projection's gradient, do not.
  *   - Limits: Hkv divides Hq; total_q * Hq * (Hq / Hkv) < 2^32; total_q * Hq / 32 + n_seq * Hkv < 2^24, and so for total_k * Hkv; strides below
  *     2^40, of Q, K, V and dO 128 from token to token below 4 GB (the backward: and Hq / Hkv - 1 from head to head with them); anything

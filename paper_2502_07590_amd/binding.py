@@ -518,7 +518,7 @@ def _int32(what: str, x) -> int:
 
 class Packed:
     """Host-side descriptor of packed sequences (mirrors struct dsv_packed; the calls fill in the layouts of their tensors).  max_q, max_k may
-    be any number above the longest sequence."""
+    be any numbers not below the longest sequence."""
 
     def __init__(self, n_seq: int, total_q: int, total_k: int, max_q: int, max_k: int, Hq: int, Hkv: int, d: int, dtype, scale: float,
                  causal: bool = False):

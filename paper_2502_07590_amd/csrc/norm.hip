@@ -248,7 +248,7 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(const T *__restrict__ X, 
         w = next;
     }
     if (!part) return;
-    // the block's lane groups joined, four pieces' worth of columns at a time
+    // the block's lane groups joined, a piece of each lane at a time: LPR * CH columns
     constexpr int RPB = 256 / LPR;
     float *const out = part + (int64_t)blockIdx.x * 2 * a.n;
     if constexpr (RPB == 1) {

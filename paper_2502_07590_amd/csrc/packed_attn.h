@@ -316,11 +316,6 @@ template <> struct Weights<bf16_t> {
 template <> struct Weights<float> {
     floatx16_t v;
     __device__ __forceinline__ void set(const floatx16_t &w) { v = w; }
-    __device__ __forceinline__ void set_pair(int i, float a, float b)
-    {
-        v[i] = a;
-        v[i + 1] = b;
-    }
 };
 
 // acc[nb] (channels 32 nb .. + 31 by own rows) += sum over tile rows r0 .. r0 + 31 of row[channel] * w, in STEPS steps: operands of step i are read

@@ -12,7 +12,7 @@
 // library product has 1350. Single queries against long caches are bound by memory: 104 MB of K and V in
 // 24 + 4 us with the join, 3.7 TB/s.  Few keys (34128 queries of 16 heads against 77 .. 512, d = 64): 57 us, half of it Q and O themselves, the
 // rest the chain from lengths to rows to scores of a block that walks two to eight tiles.  fp32 is bound by its products (64 cycles each):
-// 1724 tokens of two heads, d = 64, 15 + 4 us.
+// 1724 tokens of two heads, d = 64, 17.5 us and 4 for the join, each by itself; 19.3 one call behind another.
 #include "packed_attn.h"
 
 namespace dsv {
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, half = lane >> 5;
     // heads side by side: with as many heads as XCDs, or a multiple or a divisor of that, a head's keys stay in the L2 of one or a few of them;
-    // causal tiles of most keys first
+    // causal tiles of most keys first, within a sequence; the last sequence's before those of the others
     const int hk = blockIdx.x % a.Hkv, place = blockIdx.x / a.Hkv, split = blockIdx.y;
     const int slot = a.causal ? (int)(gridDim.x / a.Hkv) - 1 - place : place;
     const int si = __builtin_amdgcn_readfirstlane(find_sequence(a.cu_q, a.n_seq, a.total_q, a.group, Sh::ROWS, slot));
@@ -161,7 +161,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
         }
     }
     l = halves_sum(l);
-    // O is the average by the weights that were summed, lse the logarithm of the unrounded ones': rounding then moves weight between the keys and
+    // Weights go into the product as one bf16 word: a second one, as the sparse forward has it, would make three products of two, in a kernel bound by
+    // their power.  O is the average by the weights that were summed, lse the logarithm of the unrounded ones': rounding then moves weight between the keys and
     // adds none (bf16, against 64 bits: O 2.4e-3 off when divided by l, 1.9e-3 by lr, 1.7e-3 the rounding of O alone)
     const float whole = sizeof(T) == 2 ? halves_sum(lr) : l, fair = whole == 0.f ? 0.f : l / whole;
     if constexpr (WK > 1) {  // the waves' sums over their keys, joined in LDS: wave w then holds channels 32 w / 4 .. of every row

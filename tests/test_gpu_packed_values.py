@@ -1,4 +1,5 @@
-"""Packed attention on the GPU: roundings that it says it keeps, in norm; rows that are not numbers; sums over its longest row axis."""
+"""Packed attention on the GPU: roundings that it says it keeps, in norm; rows that are not numbers; long sequences among single
+rows; sums over its longest row axis."""
 import math
 
 import pytest
@@ -106,6 +107,17 @@ def test_scores_that_are_no_numbers_are_not_taken_for_no_keys(form, dtype, causa
             value, bound = want[n]
             value[rows.t().cpu() if n == "lse" else rows.cpu()] = float("nan")
             ref.assert_within(n, got[n], (value, bound))
+
+
+@pytest.mark.parametrize("dtype,causal,Hq,Hkv", [("bf16", False, 8, 8), ("bf16", True, 8, 2), ("f32", True, 4, 4)])
+def test_a_long_sequence_among_single_rows(dtype, causal, Hq, Hkv):
+    """A prompt among new tokens of other streams, first, last and in the middle of them."""
+    for at in (0, 40, 80):
+        lens_q = [1] * 80
+        lens_k = [1 + 37 * i % 300 for i in range(80)]
+        lens_q.insert(at, 1500)
+        lens_k.insert(at, 1700)
+        Case(lens_q, lens_k, Hq, Hkv, 128, dtype, causal, seed=at).check()
 
 
 def test_sums_over_seventeen_million_rows():
