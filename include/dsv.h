@@ -5,8 +5,8 @@
  * low-rank projections of Q and K; stage 2 (dsv_sparse_attn_fwd / dsv_sparse_attn_bwd) computes
  * exact softmax attention, and its gradients, over only those keys.
  *
- * Conventions that hold for every entry point (packed attention and layer norm, whose descriptors have strides and sequence lengths of
- * their own, say where they differ)
+ * Conventions that hold for every entry point (packed attention, the norms, rotary positions and the 8-bit cache, whose descriptors have
+ * strides and sequence lengths of their own, say where they differ)
  *   - Tensor pointers are DEVICE pointers owned by the caller, contiguous, row-major, no strides:
  *       Q, K, V, O, dO, dQ, dK, dV : [B, H, L, d]   element type dsv_problem.dtype
  *       Wq, Wk                     : [H, d, r]      same element type (one predictor pair per head)
@@ -394,6 +394,142 @@ DSV_API dsv_status dsv_layer_norm_fwd(const dsv_norm *p, const void *X, const vo
 DSV_API size_t dsv_layer_norm_bwd_workspace(const dsv_norm *p);
 DSV_API dsv_status dsv_layer_norm_bwd(const dsv_norm *p, const void *X, const void *gamma, const float *mean, const float *rstd,
                                       const void *dY, void *dX, float *dgamma, float *dbeta, void *workspace, size_t ws_bytes,
+                                      void *hip_stream);
+
+/* ---- Rotary positions -----------------------------------------------------------------------------------
+ * What turns the rows of Q and K before they are scored: pair i of a row's channels (lo, hi) is a point in the plane, and
+ *     t = position * freq[i];   lo' = gain (lo cos t - hi sin t),  hi' = gain (lo sin t + hi cos t)
+ * A token has 1 to 3 coordinates (of a video: frame, row, column); the first pairs[0] pairs turn with the first of them, and so on.  The
+ * first rot = 2 * (pairs[0] + ..) channels of a row are turned, the others copied.  dsv_rotary_bwd: dX from dY, the transpose (t -> -t).
+ *
+ *   - X, Y (dY, dX): [tokens, heads, d], strides as above but of any size and alignment.  Rows of whole sixteens of channels that begin on 16
+ *     bytes, with pairs in whole eights (DSV_TURN_INTERLEAVED: any), are moved 16 bytes at a time.  Q and K of a fused projection that lie
+ *     side by side are one call of Hq + Hkv heads.  Y may be X with the same strides (in place); else they may not overlap.
+ *   - pos: DEVICE int32 [tokens, axes], any values.  freq: DEVICE double [pairs of all coordinates], radians a position.  Angles are formed in
+ *     64 bits, sines and products in 32; each result is rounded once.
+ *   - d <= 8192; tokens * heads * (d / 16 + 1) and tokens * d < 2^31 (larger: DSV_EUNSUPPORTED); gain finite. */
+typedef enum {
+    DSV_TURN_INTERLEAVED = 0, /* channels 2 i and 2 i + 1 */
+    DSV_TURN_HALVES = 1,      /* channels i and rot / 2 + i */
+    DSV_TURN_AXIS_HALVES = 2  /* the same within each coordinate's own 2 * pairs[a] channels, which lie side by side */
+} dsv_turn_layout;
+typedef struct dsv_rotary {
+    int32_t tokens, heads, d;
+    int32_t dtype;        /* dsv_dtype of X, Y */
+    int32_t axes;         /* coordinates of a position, 1 to 3 */
+    int32_t pairs[3];     /* pairs that each of them turns; those past `axes` are not read */
+    int32_t layout;       /* dsv_turn_layout */
+    float gain;           /* 1, or what a method for long contexts asks for */
+    uint32_t flags;       /* 0 */
+    dsv_rows x, y;        /* layouts of what is read (X, dY) and written (Y, dX) */
+} dsv_rotary;
+DSV_API dsv_status dsv_rotary_fwd(const dsv_rotary *p, const void *X, const int32_t *pos, const double *freq, void *Y, void *hip_stream);
+DSV_API dsv_status dsv_rotary_bwd(const dsv_rotary *p, const void *dY, const int32_t *pos, const double *freq, void *dX, void *hip_stream);
+
+/* Frequencies of one coordinate's pairs, host arithmetic: freq (HOST double [pairs]) = base^(-i / pairs), for contexts `factor` times as long as
+ * those a model was trained on changed by `scaling`; *gain (HOST, may be NULL) is what goes into dsv_rotary.gain.
+ *   DSV_SCALE_NONE    as they are;
+ *   DSV_SCALE_LINEAR  all divided by factor (positions interpolated);
+ *   DSV_SCALE_BASE    base * factor^(pairs / (pairs - 1)): the slowest divided by factor, the fastest kept;
+ *   DSV_SCALE_PARTS   by the turns r_i = original * freq / (2 pi) that a pair makes within the trained length `original`: kept from `high`
+ *                     turns upwards, divided by factor up to `low`, linear in r between; gain = 0.1 ln factor + 1.
+ * pairs >= 1, base > 1, factor >= 1; PARTS: original > 0, 0 <= low < high (DSV_EINVAL otherwise). */
+typedef enum { DSV_SCALE_NONE = 0, DSV_SCALE_LINEAR = 1, DSV_SCALE_BASE = 2, DSV_SCALE_PARTS = 3 } dsv_turn_scaling;
+DSV_API dsv_status dsv_rotary_freqs(int32_t pairs, double base, int32_t scaling, double factor, double original, double low, double high,
+                                    double *freq, float *gain);
+
+/* ---- Gate, residual and modulated norm ------------------------------------------------------------------
+ * Between two blocks of a DiT: what one adds to the stream, gated, and the norm that the next one reads, scaled and shifted.  Tokens belong to
+ * segments (clips, or frames, that share a conditioning); gate, scale and shift have one row a segment:
+ *     u = y, or N(y) (post);   h = residual * x + gate u;   z = N(h) (1 + scale) + shift
+ *     N(v) = (v - mu) r,  r = 1 / sqrt(mean (v - mu)^2 + eps),  mu = mean v, or 0 (DSV_NORM_RMS)
+ * Backward, from dZ and dH (what comes back to h by other ways), with w = dZ (1 + scale), xh = N(h), v = gate dh:
+ *     dh = dH + r (w - mean w - xh mean(w xh))  (RMS: without mean w);   dX = residual * dh;   dY = v, or r_y (v - mean v - u mean(v u))
+ *     dgate = sum dh u,  dscale = sum dZ xh,  dshift = sum dZ  over the rows of a segment
+ *
+ *   - X, Y, H, Z, dZ, dH, dX, dY: [tokens, n], each with its stride from row to row, of any alignment (rows that begin on 16 bytes and fill
+ *     whole ones are read 16 bytes at a time).  gate, scale, shift: [n_seg, n] in `dtype`, each with its stride (chunks of one projection's
+ *     output), or NULL (1, 0, 0).  Y NULL: h = residual * x, and H, gate, dY, dgate are NULL too; dH NULL: zero.
+ *     tokens = 0: nothing is written but zeros to dgate, dscale, dshift, and the tensors of rows may be NULL.
+ *   - cu: DEVICE int32 [n_seg + 1], ascending from 0, read by the kernels only, as for packed attention: segment s has rows cu[s] .. cu[s+1] - 1,
+ *     which may be none.  Rows of no segment are left as they are in every output.  Other entries: undefined results, no access outside.
+ *   - stats: float [tokens, 4], on 16 bytes: mean and 1 / deviation of h, and of y (0 without post); the forward writes them for the backward.
+ *   - The backward forms h from X and Y (the unrounded one that the forward normed), so H need not be kept for it.
+ *   - dgate, dscale, dshift: float [n_seg, n], each with its stride, each NULL where it is not wanted; zeros for a segment of no rows.
+ *   - H may be X, and dX may be dH, with the same stride (in place); no output may overlap an input otherwise, nor another output.
+ *   - n <= 8192; n_seg * ceil(n / 32) < 2^24 (larger: DSV_EUNSUPPORTED); eps >= 0, residual finite.
+ *   - Everything is summed in 32 bits, in a fixed order: the same results from run to run.  Workspace of the backward: for the sums of segments
+ *     of many rows; none is needed where dgate, dscale and dshift are all NULL. */
+typedef enum { DSV_NORM_LAYER = 0, DSV_NORM_RMS = 1 } dsv_norm_kind;
+typedef struct dsv_gated_norm {
+    int32_t tokens, n, n_seg;
+    int32_t dtype;              /* dsv_dtype of everything but stats, dgate, dscale, dshift */
+    int32_t kind;               /* dsv_norm_kind */
+    int32_t post;               /* 0, or 1: Y is normed before it is gated */
+    float eps, residual;
+    uint32_t flags;             /* 0 */
+    int64_t x, y, h, z;         /* elements from row to row; the forward reads these */
+    int64_t gate, scale, shift; /* from segment to segment */
+    int64_t dz, dh, dx, dy;     /* and the backward all but h, z and shift */
+    int64_t dgate, dscale, dshift;
+} dsv_gated_norm;
+DSV_API dsv_status dsv_gated_norm_fwd(const dsv_gated_norm *p, const void *X, const void *Y, const int32_t *cu, const void *gate, const void *scale,
+                                      const void *shift, void *Z, void *H, float *stats, void *hip_stream);
+DSV_API size_t dsv_gated_norm_bwd_workspace(const dsv_gated_norm *p);
+DSV_API dsv_status dsv_gated_norm_bwd(const dsv_gated_norm *p, const void *X, const void *Y, const int32_t *cu, const void *gate, const void *scale,
+                                      const float *stats, const void *dZ, const void *dH, void *dX, void *dY, float *dgate, float *dscale,
+                                      float *dshift, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/* ---- An 8-bit cache of K and V, and attention over it -----------------------------------------------------
+ * For samplers that make a video piece by piece: the tokens made so far stay, new ones are added behind them, and attend to them.
+ * The cache is a pool of pages of `page` tokens of all heads, held as e4m3 (4 exponent bits, 3 behind the point; largest 448) with one scale
+ * for each page and head: value = e4m3 * scale, and every scale is a power of two.
+ *     K8, V8: [n_pages, Hkv, page, d] bytes;   kscale, vscale: float [n_pages, Hkv]
+ * table: int32 [n_seq, max_pages]: token t of sequence s lies in page table[s][t / page] at place t % page.
+ * cu: int32 [n_seq + 1]: sequence s has new tokens cu[s] .. cu[s+1] - 1 of the call's tensors (possibly none); lens: int32 [n_seq]: the tokens in
+ * its cache, the new ones among them -- the same for the append that adds them and the attention that follows.  All are DEVICE arrays and read by
+ * the kernels only: captured calls replay on what they hold then.
+ *
+ * dsv_cache_append: K, V [total, Hkv, d] of the new tokens into their places; K turned on the way as by dsv_rotary_fwd (turn NULL: as it is; of
+ *   *turn, d, axes, pairs, layout and gain are read), pos [total, axes] and freq as there.  For each page and head that gets new tokens, K and V apart:
+ *       s = the least power of two with max |new| <= 448 s, or the page's scale so far where it holds earlier tokens and that is larger;
+ *       the earlier tokens' values times (their scale / s), the new ones over s, each to the nearest e4m3 (ties to even).
+ *   Moving a page to a larger scale is exact but for values that leave the normal range (below 2^-6 of the new scale).
+ *   Places of the pages behind the new tokens are left as they are, and need hold nothing in particular.
+ * dsv_cache_attn_fwd: O and lse of Q [total, Hq, d] over the cache, as dsv_packed_attn_fwd: causal: query i of nq sees keys
+ *   j <= i + len - nq, else all; a query that sees none has O = 0, lse = -inf.  Rows of no sequence are left as they are.  Forward only.
+ *
+ *   - page: a power of two from 16 to 256; d as everywhere; dtype (F32 or BF16) is that of Q, K, V, O.  Q, K, V, O: strides as for packed
+ *     attention (whole 16 bytes).  K8 and V8 begin on 16 bytes.
+ *   - A page belongs to one sequence while it grows; full pages may stand in several rows of the table.  Scales of begun pages are those that
+ *     dsv_cache_append wrote: other values than powers of two are not supported.
+ *   - Entries of cu, lens or table out of their range give undefined results but no access outside the tensors.  Table entries of pages that
+ *     lens does not reach are not used.
+ *   - Finite inputs are assumed; a value that is not becomes NaN in the cache and leaves the page's scale alone.  A K that is not finite makes the
+ *     rows that see it NaN; a V that is not also reaches rows that causal order hides it from, up to 190 tokens away.  Finite values at or above 2^127 are cut to 448 * 2^119.
+ *   - max_new, max_len: no sequence has more new tokens, or more in all (INT32_MAX: no bound but the table's).
+ *   - Roundings of the attention are those of dsv_packed_attn_fwd: widening the cache is exact.  The same results from run to run, bit for bit.
+ *   - Limits: Hkv divides Hq; total * Hq * (Hq / Hkv) < 2^32; total * Hq / 32 + n_seq * Hkv < 2^24; page * max_pages < 2^31.  Workspace of the
+ *     attention: for partial results of pieces of long caches, as sized from max_len. */
+typedef struct dsv_cache {
+    int32_t n_seq;
+    int32_t total;              /* new tokens: rows of K, V or Q, O */
+    int32_t max_new, max_len;
+    int32_t Hq, Hkv, d;
+    int32_t dtype;
+    int32_t n_pages, page, max_pages;
+    int32_t causal;             /* 0 or 1; the attention's */
+    float scale;                /* 1e-30 to 1e30; the attention's */
+    uint32_t flags;             /* 0 */
+    dsv_rows q, o;              /* layouts; the attention reads these */
+    dsv_rows k, v;              /* and the append these */
+} dsv_cache;
+DSV_API dsv_status dsv_cache_append(const dsv_cache *p, const dsv_rotary *turn, const void *K, const void *V, const int32_t *cu, const int32_t *lens,
+                                    const int32_t *table, const int32_t *pos, const double *freq, void *K8, void *V8, float *kscale, float *vscale,
+                                    void *hip_stream);
+DSV_API size_t dsv_cache_attn_fwd_workspace(const dsv_cache *p);
+DSV_API dsv_status dsv_cache_attn_fwd(const dsv_cache *p, const void *Q, const int32_t *cu, const int32_t *lens, const int32_t *table, const void *K8,
+                                      const void *V8, const float *kscale, const float *vscale, void *O, float *lse, void *workspace, size_t ws_bytes,
                                       void *hip_stream);
 
 /* ---- Optional debug check of an index tensor ---------------------------------------------------

@@ -38,6 +38,8 @@ EXPORTED_SYMBOLS = (
     "dsv_kernel_timing", "dsv_kernel_ms", "dsv_threshold_search", "dsv_threshold_sample_keys", "dsv_dense_min_k", "dsv_measure_gather_ceiling",
     "dsv_packed_attn_fwd_workspace", "dsv_packed_attn_fwd", "dsv_packed_attn_bwd_workspace", "dsv_packed_attn_bwd",
     "dsv_layer_norm_fwd", "dsv_layer_norm_bwd_workspace", "dsv_layer_norm_bwd",
+    "dsv_rotary_fwd", "dsv_rotary_bwd", "dsv_rotary_freqs", "dsv_gated_norm_fwd", "dsv_gated_norm_bwd_workspace", "dsv_gated_norm_bwd",
+    "dsv_cache_append", "dsv_cache_attn_fwd_workspace", "dsv_cache_attn_fwd",
 )
 
 
@@ -68,6 +70,22 @@ class _CPacked(ctypes.Structure):
 class _CNorm(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "heads", "n", "dtype")] + [("eps", ctypes.c_float), ("flags", ctypes.c_uint32)] + \
                [(n, _CRows) for n in ("x", "y", "dy", "dx")]
+
+
+class _CRotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "heads", "d", "dtype", "axes")] + \
+               [("pairs", ctypes.c_int32 * 3), ("layout", ctypes.c_int32), ("gain", ctypes.c_float), ("flags", ctypes.c_uint32), ("x", _CRows), ("y", _CRows)]
+
+
+class _CGatedNorm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "n", "n_seg", "dtype", "kind", "post")] + \
+               [("eps", ctypes.c_float), ("residual", ctypes.c_float), ("flags", ctypes.c_uint32)] + \
+               [(n, ctypes.c_int64) for n in ("x", "y", "h", "z", "gate", "scale", "shift", "dz", "dh", "dx", "dy", "dgate", "dscale", "dshift")]
+
+
+class _CCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seq", "total", "max_new", "max_len", "Hq", "Hkv", "d", "dtype", "n_pages", "page", "max_pages", "causal")] + \
+               [("scale", ctypes.c_float), ("flags", ctypes.c_uint32)] + [(n, _CRows) for n in ("q", "o", "k", "v")]
 
 
 class Grouping:
@@ -187,6 +205,23 @@ def load_library():
     lib.dsv_layer_norm_fwd.argtypes = [PN] + [vp] * 6 + [vp]
     lib.dsv_layer_norm_bwd.restype = ctypes.c_int
     lib.dsv_layer_norm_bwd.argtypes = [PN] + [vp] * 8 + [vp, sz, vp]
+    PR, PG_, PC, f64 = ctypes.POINTER(_CRotary), ctypes.POINTER(_CGatedNorm), ctypes.POINTER(_CCache), ctypes.c_double
+    for name in ("dsv_rotary_fwd", "dsv_rotary_bwd"):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = [PR] + [vp] * 5
+    lib.dsv_rotary_freqs.restype = ctypes.c_int
+    lib.dsv_rotary_freqs.argtypes = [i32, f64, i32, f64, f64, f64, f64, ctypes.POINTER(f64), ctypes.POINTER(ctypes.c_float)]
+    for name, descriptor in (("dsv_gated_norm_bwd_workspace", PG_), ("dsv_cache_attn_fwd_workspace", PC)):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [descriptor]
+    lib.dsv_gated_norm_fwd.restype = ctypes.c_int
+    lib.dsv_gated_norm_fwd.argtypes = [PG_] + [vp] * 9 + [vp]
+    lib.dsv_gated_norm_bwd.restype = ctypes.c_int
+    lib.dsv_gated_norm_bwd.argtypes = [PG_] + [vp] * 13 + [vp, sz, vp]
+    lib.dsv_cache_append.restype = ctypes.c_int
+    lib.dsv_cache_append.argtypes = [PC, PR] + [vp] * 11 + [vp]
+    lib.dsv_cache_attn_fwd.restype = ctypes.c_int
+    lib.dsv_cache_attn_fwd.argtypes = [PC] + [vp] * 10 + [vp, sz, vp]
     lib.dsv_measure_gather_ceiling.restype = ctypes.c_int
     lib.dsv_measure_gather_ceiling.argtypes = [i32, i32, i32, i32, i32, vp, vp, vp, vp, i32, ctypes.POINTER(ctypes.c_float), vp]
     _lib = lib
@@ -694,6 +729,220 @@ def layer_norm_bwd(p: Norm, X, gamma, mean, rstd, dY, dX=None, dgamma=None, dbet
         ws, nbytes, held = _scratch(lib.dsv_layer_norm_bwd_workspace(c) if dgamma is not None else 0, dev, workspace)
         _check(lib.dsv_layer_norm_bwd(c, *args, ws, nbytes, on.ptr), "dsv_layer_norm_bwd")
     return dX, dgamma, dbeta
+
+
+# ---- what stands around the attention: rotary positions, gated norms, an 8-bit cache --------------------
+_TURN_LAYOUT = {"interleaved": 0, "halves": 1, "axis_halves": 2}
+_TURN_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+_NORM_KIND = {"layer": 0, "rms": 1}
+
+
+def _named(what: str, names, x) -> int:
+    if x not in names:
+        raise DsvError(f"{what}: {x!r} is none of {', '.join(names)}")
+    return names[x]
+
+
+class Rotary:
+    """Host-side descriptor of rows to be turned by their positions (mirrors struct dsv_rotary; the calls fill in the layouts of their tensors).
+    pairs: pairs of channels that each coordinate turns, one to three numbers (or one, not in a list)."""
+
+    def __init__(self, tokens: int, heads: int, d: int, dtype, pairs, layout: str = "halves", gain: float = 1.0):
+        if isinstance(dtype, str):
+            dtype = _DTYPE_NAME[dtype]
+        pairs = [pairs] if isinstance(pairs, int) else list(pairs)
+        if not 1 <= len(pairs) <= 3:
+            raise DsvError(f"pairs: one to three coordinates, got {len(pairs)}")
+        self.tokens, self.heads, self.d, self.gain = _int32("tokens", tokens), _int32("heads", heads), _int32("d", d), float(gain)
+        self.pairs, self.layout, self.torch_dtype = [_int32("pairs", n) for n in pairs], layout, dtype
+        self.shape, self.pos_shape, self.freq_shape = (self.tokens, self.heads, self.d), (self.tokens, len(pairs)), (sum(self.pairs),)
+        rows = _CRows(self.heads * self.d, self.d)
+        self._c = _CRotary(self.tokens, self.heads, self.d, _DTYPE_CODE.get(dtype, -1), len(pairs), (ctypes.c_int32 * 3)(*self.pairs),
+                           _named("layout", _TURN_LAYOUT, layout), self.gain, 0, rows, rows)
+
+    @property
+    def c(self):
+        return ctypes.byref(self._c)
+
+
+def rotary_freqs(pairs, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original: float = 0.0, low: float = 1.0, high: float = 32.0):
+    """(frequencies, gain) for Rotary: a float64 CPU tensor, those of each coordinate one behind another, and what goes into Rotary(gain=).  `factor`
+    times as long contexts as those trained on, by "linear", "base" or "parts" (original: the trained length; see dsv_rotary_freqs)."""
+    out, gain = [], ctypes.c_float(1.0)
+    for n in [pairs] if isinstance(pairs, int) else pairs:
+        freq = (ctypes.c_double * max(1, n))()
+        if n:       # a coordinate may turn nothing
+            _check(load_library().dsv_rotary_freqs(_int32("pairs", n), float(base), _named("scaling", _TURN_SCALING, scaling), float(factor), float(original),
+                                                   float(low), float(high), freq, ctypes.byref(gain)), "dsv_rotary_freqs")
+        out += freq[:n]
+    return torch.tensor(out, dtype=torch.float64), float(gain.value)
+
+
+def _rotary(name: str, p: Rotary, X, pos, freq, Y, stream):
+    with _On(X, stream) as on:
+        dev, td, c, shape = X.device, p.torch_dtype, _CRotary.from_buffer_copy(p._c), p.shape
+        Y = torch.empty_like(X) if Y is None else Y
+        _check(getattr(load_library(), name)(c, _rows(c, "x", X, shape, td, dev), _flat("pos", pos, p.pos_shape, torch.int32, dev),
+                                             _flat("freq", freq, p.freq_shape, torch.float64, dev), _rows(c, "y", Y, shape, td, dev), on.ptr), name)
+    return Y
+
+
+def rotary_fwd(p: Rotary, X, pos, freq, Y=None, stream=None):
+    """Y: X [tokens, heads, d], any strides between tokens and heads, turned by pos int32 [tokens, coordinates] and freq float64 [pairs of all of
+    them], on the device.  Y is made like X; it may be X (in place)."""
+    return _rotary("dsv_rotary_fwd", p, X, pos, freq, Y, stream)
+
+
+def rotary_bwd(p: Rotary, dY, pos, freq, dX=None, stream=None):
+    """dX of rotary_fwd from dY; it is made like dY, and may be dY."""
+    return _rotary("dsv_rotary_bwd", p, dY, pos, freq, dX, stream)
+
+
+class GatedNorm:
+    """Host-side descriptor of a gate, residual and modulated norm (mirrors struct dsv_gated_norm; the calls fill in the layouts of their tensors).
+    kind: "layer" or "rms"; post: the block's output is normed before it is gated; residual: what the stream is multiplied by."""
+
+    def __init__(self, tokens: int, n: int, n_seg: int, dtype, eps: float = 1e-6, kind: str = "layer", post: bool = False, residual: float = 1.0):
+        if isinstance(dtype, str):
+            dtype = _DTYPE_NAME[dtype]
+        self.tokens, self.n, self.n_seg = _int32("tokens", tokens), _int32("n", n), _int32("n_seg", n_seg)
+        self.eps, self.kind, self.post, self.residual, self.torch_dtype = float(eps), kind, bool(post), float(residual), dtype
+        self.shape, self.mod_shape = (self.tokens, self.n), (self.n_seg, self.n)
+        self._c = _CGatedNorm(self.tokens, self.n, self.n_seg, _DTYPE_CODE.get(dtype, -1), _named("kind", _NORM_KIND, kind), int(self.post), self.eps,
+                              self.residual, 0, *[self.n] * 14)
+
+    @property
+    def c(self):
+        return ctypes.byref(self._c)
+
+
+def _row(c, name: str, t, shape, dtype, device):
+    """Pointer of a tensor of rows [rows, n], None for None.  Its stride goes into the descriptor `c`, which says contiguous ones."""
+    if t is None:
+        return None
+    if t.device != device or t.shape != shape or t.dtype != dtype:
+        raise DsvError(f"{name}: expected {dtype} of shape {shape} on {device}, got {t.dtype} of shape {tuple(t.shape)} on {t.device}")
+    if not t.is_contiguous():
+        row, one = t.stride()
+        if one != 1 and shape[1] > 1:
+            raise DsvError(f"{name}: the elements of a row must lie side by side")
+        setattr(c, name, row if shape[0] > 1 else shape[1])
+    return t.data_ptr()
+
+
+def gated_norm_fwd(p: GatedNorm, X, cu, Y=None, gate=None, scale=None, shift=None, Z=None, H=None, stats=None, stream=None):
+    """(Z, H, stats) of h = residual X + gate Y, z = norm(h) (1 + scale) + shift.  X, Y [tokens, n], gate, scale, shift [n_seg, n] or None, any strides
+    between rows; cu int32 [n_seg + 1] on the device.  Without Y there is no H (None).  H may be X.  stats (float [tokens, 4]): for the backward."""
+    lib = load_library()
+    with _On(X, stream) as on:
+        dev, td, c, shape, mod = X.device, p.torch_dtype, _CGatedNorm.from_buffer_copy(p._c), p.shape, p.mod_shape
+        Z = torch.empty(shape, dtype=td, device=dev) if Z is None else Z
+        H = torch.empty(shape, dtype=td, device=dev) if H is None and Y is not None else H
+        stats = torch.empty((p.tokens, 4), dtype=torch.float32, device=dev) if stats is None else stats
+        _check(lib.dsv_gated_norm_fwd(c, _row(c, "x", X, shape, td, dev), _row(c, "y", Y, shape, td, dev), _flat("cu", cu, (p.n_seg + 1,), torch.int32, dev),
+                                      _row(c, "gate", gate, mod, td, dev), _row(c, "scale", scale, mod, td, dev), _row(c, "shift", shift, mod, td, dev),
+                                      _row(c, "z", Z, shape, td, dev), _row(c, "h", H, shape, td, dev), _flat("stats", stats, (p.tokens, 4), torch.float32, dev),
+                                      on.ptr), "dsv_gated_norm_fwd")
+    return Z, H, stats
+
+
+def gated_norm_bwd_workspace(p: GatedNorm) -> int:
+    return int(load_library().dsv_gated_norm_bwd_workspace(p.c))
+
+
+def gated_norm_bwd(p: GatedNorm, X, cu, stats, dZ, Y=None, gate=None, scale=None, dH=None, dX=None, dY=None, dgate=None, dscale=None, dshift=None,
+                   workspace=None, stream=None):
+    """(dX, dY, dgate, dscale, dshift) of gated_norm_fwd; dY None without Y.  dgate, dscale, dshift float [n_seg, n]: made where gate, and where scale, was
+    given, and filled where they were passed; else None.  dX may be dH."""
+    lib = load_library()
+    with _On(X, stream) as on:
+        dev, td, c, shape, mod, f32 = X.device, p.torch_dtype, _CGatedNorm.from_buffer_copy(p._c), p.shape, p.mod_shape, torch.float32
+        dX = torch.empty(shape, dtype=td, device=dev) if dX is None else dX
+        dY = torch.empty(shape, dtype=td, device=dev) if dY is None and Y is not None else dY
+        dgate = torch.empty(mod, dtype=f32, device=dev) if dgate is None and gate is not None else dgate
+        if scale is not None:
+            dscale = torch.empty(mod, dtype=f32, device=dev) if dscale is None else dscale
+            dshift = torch.empty(mod, dtype=f32, device=dev) if dshift is None else dshift
+        args = (_row(c, "x", X, shape, td, dev), _row(c, "y", Y, shape, td, dev), _flat("cu", cu, (p.n_seg + 1,), torch.int32, dev),
+                _row(c, "gate", gate, mod, td, dev), _row(c, "scale", scale, mod, td, dev), _flat("stats", stats, (p.tokens, 4), f32, dev),
+                _row(c, "dz", dZ, shape, td, dev), _row(c, "dh", dH, shape, td, dev), _row(c, "dx", dX, shape, td, dev), _row(c, "dy", dY, shape, td, dev),
+                _row(c, "dgate", dgate, mod, f32, dev), _row(c, "dscale", dscale, mod, f32, dev), _row(c, "dshift", dshift, mod, f32, dev))
+        wanted = dgate is not None or dscale is not None or dshift is not None
+        ws, nbytes, held = _scratch(lib.dsv_gated_norm_bwd_workspace(c) if wanted else 0, dev, workspace)
+        _check(lib.dsv_gated_norm_bwd(c, *args, ws, nbytes, on.ptr), "dsv_gated_norm_bwd")
+    return dX, dY, dgate, dscale, dshift
+
+
+class Cache:
+    """Host-side descriptor of an 8-bit cache and of the new tokens of a call (mirrors struct dsv_cache; the calls fill in the layouts of their tensors).
+    total: rows of K, V or Q; max_new, max_len: no sequence has more new tokens, or more in all (any larger numbers; max_len None: what the table holds)."""
+
+    def __init__(self, n_seq: int, total: int, max_new: int, Hq: int, Hkv: int, d: int, dtype, n_pages: int, page: int, max_pages: int, scale: float = 1.0,
+                 causal: bool = True, max_len=None):
+        if isinstance(dtype, str):
+            dtype = _DTYPE_NAME[dtype]
+        self.n_seq, self.total, self.Hq, self.Hkv, self.d = _int32("n_seq", n_seq), _int32("total", total), _int32("Hq", Hq), _int32("Hkv", Hkv), _int32("d", d)
+        self.max_new, self.max_len = _int32("max_new", min(max_new, _INT32_MAX)), _int32("max_len", _INT32_MAX if max_len is None else min(max_len, _INT32_MAX))
+        self.n_pages, self.page, self.max_pages = _int32("n_pages", n_pages), _int32("page", page), _int32("max_pages", max_pages)
+        self.scale, self.causal, self.torch_dtype = float(scale), bool(causal), dtype
+        self.q_shape, self.k_shape = (self.total, self.Hq, self.d), (self.total, self.Hkv, self.d)
+        self.pool_shape, self.scale_shape = (self.n_pages, self.Hkv, self.page, self.d), (self.n_pages, self.Hkv)
+        q, k = _CRows(self.Hq * self.d, self.d), _CRows(self.Hkv * self.d, self.d)
+        self._c = _CCache(self.n_seq, self.total, self.max_new, self.max_len, self.Hq, self.Hkv, self.d, _DTYPE_CODE.get(dtype, -1), self.n_pages, self.page,
+                          self.max_pages, int(self.causal), self.scale, 0, q, q, k, k)
+
+    @property
+    def c(self):
+        return ctypes.byref(self._c)
+
+
+def _cache_args(p: Cache, cu, lens, table, K8, V8, kscale, vscale, dev):
+    """The pointers ahead of the pool's, and the pool's."""
+    def pool(what, t):
+        return _flat(what, t, p.pool_shape, t.dtype if t.dtype in (torch.float8_e4m3fn, torch.uint8) else torch.float8_e4m3fn, dev)
+
+    return ((_flat("cu", cu, (p.n_seq + 1,), torch.int32, dev), _flat("lens", lens, (p.n_seq,), torch.int32, dev),
+             _flat("table", table, (p.n_seq, p.max_pages), torch.int32, dev)),
+            (pool("K8", K8), pool("V8", V8), _flat("kscale", kscale, p.scale_shape, torch.float32, dev), _flat("vscale", vscale, p.scale_shape, torch.float32, dev)))
+
+
+def cache_append(p: Cache, K, V, cu, lens, table, K8, V8, kscale, vscale, rotary: Optional[Rotary] = None, pos=None, freq=None, stream=None):
+    """K, V [total, Hkv, d] of the new tokens (any strides between tokens and heads) into the pages of the cache, K turned on the way (rotary None: as it
+    is).  cu int32 [n_seq + 1]: new tokens; lens int32 [n_seq]: tokens in each sequence's cache, the new ones among them; table int32 [n_seq,
+    max_pages]; K8, V8 float8_e4m3fn (or uint8) [n_pages, Hkv, page, d] and kscale, vscale float [n_pages, Hkv] are updated."""
+    lib = load_library()
+    with _On(K, stream) as on:
+        dev, td, c = K.device, p.torch_dtype, _CCache.from_buffer_copy(p._c)
+        index, pools = _cache_args(p, cu, lens, table, K8, V8, kscale, vscale, dev)
+        turn = None
+        if rotary is not None:
+            turn = rotary.c
+            if pos is None or freq is None:
+                raise DsvError("rotary: positions and frequencies go with it")
+            pos, freq = _flat("pos", pos, (p.total, len(rotary.pairs)), torch.int32, dev), _flat("freq", freq, rotary.freq_shape, torch.float64, dev)
+        else:
+            pos = freq = None
+        _check(lib.dsv_cache_append(c, turn, _rows(c, "k", K, p.k_shape, td, dev), _rows(c, "v", V, p.k_shape, td, dev), *index, pos, freq, *pools, on.ptr),
+               "dsv_cache_append")
+
+
+def cache_attn_fwd_workspace(p: Cache) -> int:
+    return int(load_library().dsv_cache_attn_fwd_workspace(p.c))
+
+
+def cache_attn_fwd(p: Cache, Q, cu, lens, table, K8, V8, kscale, vscale, O=None, lse=None, workspace=None, stream=None):
+    """(O, lse) of Q [total, Hq, d], the new tokens' queries, over the cache: O made like Q, lse float [Hq, total].  The other arguments as for
+    cache_append, which comes first."""
+    lib = load_library()
+    with _On(Q, stream) as on:
+        dev, td, c = Q.device, p.torch_dtype, _CCache.from_buffer_copy(p._c)
+        O = torch.empty_like(Q) if O is None else O
+        lse = torch.empty((p.Hq, p.total), dtype=torch.float32, device=dev) if lse is None else lse
+        index, pools = _cache_args(p, cu, lens, table, K8, V8, kscale, vscale, dev)
+        args = (_rows(c, "q", Q, p.q_shape, td, dev), *index, *pools, _rows(c, "o", O, p.q_shape, td, dev), _flat("lse", lse, (p.Hq, p.total), torch.float32, dev))
+        ws, nbytes, held = _scratch(lib.dsv_cache_attn_fwd_workspace(c), dev, workspace)
+        _check(lib.dsv_cache_attn_fwd(c, *args, ws, nbytes, on.ptr), "dsv_cache_attn_fwd")
+    return O, lse
 
 
 def idx_validate(p: Problem, idx, workspace=None, stream=None):

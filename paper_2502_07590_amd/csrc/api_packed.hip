@@ -9,21 +9,6 @@
 namespace dsv {
 namespace {
 
-// Strides of an input: whole 16 bytes.  Of an output: also no two of its rows on the same memory.
-bool ok_strides(const dsv_rows &s, size_t es)
-{
-    const int64_t unit = 16 / (int64_t)es, most = (int64_t)1 << 40;
-    return s.row >= 0 && s.head >= 0 && s.row < most && s.head < most && s.row % unit == 0 && s.head % unit == 0;
-}
-typedef __int128 wide_t;  // counts below 2^31 times strides below 2^40: more than 64 bits
-bool rows_apart(const dsv_rows &s, int64_t rows, int64_t heads, int64_t n)
-{
-    if (rows <= 1 && heads <= 1) return true;
-    if (rows <= 1) return s.head >= n;
-    if (heads <= 1) return s.row >= n;
-    return (s.head >= n && s.row >= (wide_t)(heads - 1) * s.head + n) || (s.row >= n && s.head >= (wide_t)(rows - 1) * s.row + n);
-}
-
 dsv_status check_packed(const dsv_packed *p, bool grad)
 {
     if (!p) return DSV_EINVAL;
@@ -69,7 +54,7 @@ PackedArgs packed_args(const dsv_packed &p, bool grad, const int32_t *cu_q, cons
     a.Hq = p.Hq;
     a.Hkv = p.Hkv;
     a.group = p.Hq / p.Hkv;
-    a.magic = a.group > 1 ? (uint32_t)((1ull << 32) / (uint64_t)a.group) + 1u : 0u;
+    a.magic = reciprocal(a.group);
     a.causal = p.causal;
     a.scale = p.scale;
     a.q_row = p.q.row * es, a.q_head = p.q.head * es;
@@ -85,12 +70,6 @@ PackedArgs packed_args(const dsv_packed &p, bool grad, const int32_t *cu_q, cons
     return a;
 }
 
-// How a step walks: own rows (queries times the heads that share, or keys) in tiles of 128, or of 32 whose four waves share the other axis; and
-// that axis in pieces, joined afterwards.
-struct Walk {
-    bool few;
-    int splits, chunk;
-};
 // A step's cost: blocks of 128 rows a CU runs at once, operations a pair of rows (and channel), the rate it reaches with the chip full, and
 // how many results a piece leaves per own row.
 struct StepCost {
@@ -177,18 +156,33 @@ Walk plan_walk(const StepCost &cost, int d, bool causal, int64_t own, int64_t ma
     return w;
 }
 enum Step { kFwd, kDq, kDkdv };
-Walk walk_of(const dsv_packed &p, Step step)
+StepCost step_cost(int dtype, int d, Step step)
 {
-    const bool bf16 = p.dtype == DSV_BF16;
-    const int64_t g = p.Hq / p.Hkv;
+    const bool bf16 = dtype == DSV_BF16;
     // operations a pair and channel, and rates: as measured at 32768 tokens.  (fp32 dK and dV: those of blocks of 128 keys, where launch_dkdv runs blocks
     // of 32, one a CU: four times as many as counted, and so more pieces than they need.)
     StepCost c{};
     c.bf16 = bf16;
-    c.per_cu = step == kDkdv ? (p.d == 64 ? 2 : 1) : bf16 ? (p.d == 64 ? 3 : 2) : (p.d == 64 ? 2 : 1);
+    c.per_cu = step == kDkdv ? (d == 64 ? 2 : 1) : bf16 ? (d == 64 ? 3 : 2) : (d == 64 ? 2 : 1);
     c.flops = step == kFwd ? 4 : 8;
     c.rate = bf16 ? 1.1e15 : 1e14;
     c.results = step == kDkdv ? 2 : 1;
+    return c;
+}
+}  // namespace
+
+Walk plan_forward(int dtype, int d, bool causal, int64_t own, int64_t max_own, int64_t heads, int64_t n_seq, int64_t other, int64_t max_other)
+{
+    return plan_walk(step_cost(dtype, d, kFwd), d, causal, own, max_own, heads, n_seq, other, max_other);
+}
+
+namespace {
+Walk walk_of(const dsv_packed &p, Step step)
+{
+    const int64_t g = p.Hq / p.Hkv;
+    if (step == kFwd)
+        return plan_forward(p.dtype, p.d, p.causal != 0, (int64_t)p.total_q * g, std::min(p.max_q, p.total_q) * g, p.Hkv, p.n_seq, p.total_k, std::min(p.max_k, p.total_k));
+    const StepCost c = step_cost(p.dtype, p.d, step);
     if (step == kDkdv)
         return plan_walk(c, p.d, p.causal != 0, p.total_k, std::min(p.max_k, p.total_k), p.Hkv, p.n_seq, (int64_t)p.total_q * g, std::min(p.max_q, p.total_q) * g);
     return plan_walk(c, p.d, p.causal != 0, (int64_t)p.total_q * g, std::min(p.max_q, p.total_q) * g, p.Hkv, p.n_seq, p.total_k, std::min(p.max_k, p.total_k));
@@ -219,13 +213,6 @@ dsv_status check_norm(const dsv_norm *p, bool grad)
 NormArgs norm_args(const dsv_norm &p)
 {
     return NormArgs{p.tokens, p.heads, p.n, p.eps, p.x.row, p.x.head, p.y.row, p.y.head, p.dy.row, p.dy.head, p.dx.row, p.dx.head};
-}
-// every pointer on an element
-bool on_elements(std::initializer_list<const void *> ps, size_t es)
-{
-    for (const void *q : ps)
-        if (reinterpret_cast<uintptr_t>(q) % es) return false;
-    return true;
 }
 bool wide_rows(const dsv_norm &p, std::initializer_list<const void *> ps, std::initializer_list<dsv_rows> strides)
 {

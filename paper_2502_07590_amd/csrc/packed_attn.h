@@ -8,6 +8,7 @@
 #include <type_traits>
 #include <utility>
 
+#include "sequences.h"
 #include "stage2_core.h"
 
 namespace dsv {
@@ -26,6 +27,7 @@ struct PackedArgs {
     int32_t splits, chunk;  // the long axis in `splits` pieces of `chunk` rows (0: in one)
 };
 
+__host__ __forceinline__ uint32_t reciprocal(int32_t group) { return group > 1 ? (uint32_t)((1ull << 32) / (uint64_t)group) + 1u : 0u; }
 __device__ __forceinline__ int row_token(const PackedArgs &a, int row) { return a.group == 1 ? row : (int)__umulhi((uint32_t)row, a.magic); }
 
 // One sequence, its ends forced into the tensors: nothing an entry of cu_q or cu_k can say leads out of them.
@@ -48,28 +50,6 @@ __device__ __forceinline__ int pieces_seen(const PackedArgs &a, const Sequence &
     const int seen = a.causal ? min(s.nk, t + s.nk - s.nq + 1) : s.nk;
     return seen > 0 ? (seen + a.chunk - 1) / a.chunk : 0;
 }
-
-// Tiles of ROWS rows are numbered without a sum over the sequences before: sequence i's begin at floor(cu[i] * mul / ROWS) + i, which leaves
-// ceil(length / ROWS) places at least.  The owner of a place is the last sequence that begins at or before it; 64 candidates a step.
-// ROWS = 0: the tokens themselves, no place left empty (the owner of a token).
-__device__ __forceinline__ int first_slot(int cu, int total, int mul, int rows, int i)
-{
-    const int at = min(max(cu, 0), total) * mul;
-    return rows ? (int)((uint32_t)at / (uint32_t)rows) + i : at;
-}
-__device__ __forceinline__ int find_sequence(const int32_t *__restrict__ cu, int n_seq, int total, int mul, int rows, int slot)
-{
-    const int lane = threadIdx.x & 63;
-    int lo = 0, hi = n_seq;  // lo begins at or before the slot, hi after it
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 63) >> 6, at = lo + (lane + 1) * step;
-        const bool before = at < hi && first_slot(cu[at], total, mul, rows, at) <= slot;
-        lo += __popcll(__ballot(before)) * step;
-        hi = min(hi, lo + step);
-    }
-    return lo;
-}
-__host__ __device__ __forceinline__ int64_t tile_slots(int64_t total, int mul, int rows, int n_seq) { return total * mul / rows + n_seq; }
 
 // A tile of rows in LDS, row after row.  Piece p (16 bytes) of row r lies at place p ^ turn(r) of the row, so that what one cycle of the 64
 // banks serves lies in different ones: 16 bytes of 16 consecutive rows; for the transposing reads 64 bytes of four rows (bf16); 128 bytes of two rows
@@ -491,8 +471,26 @@ __device__ __forceinline__ void wait_loads_and_sync()
     __syncthreads();
 }
 
+// The forward's tiles.
+// WK = 1: the four waves own 32 rows each and share tiles of 64 keys.  WK = 4: they own the same 32 rows and take 32 keys each of a tile of
+// 128; for calls of few rows.  NBUF: tiles in LDS in turn.  (For WK = 1 the next tile's scores laid between the weights of this one, and
+// wave priorities by turns, were no faster; two groups of 32 rows a wave, one's products beside the other's weights: 306 us for 277 at 2 x 8192 tokens.)
+template <typename T, int D, int WK> struct FwdShape {
+    static constexpr int ROWS = WK == 1 ? 128 : 32, KEYS = WK == 1 ? 64 : 128, KT = KEYS / 32 / WK;
+    static constexpr int TILE = KEYS * D * (int)sizeof(T);
+    static constexpr int NBUF = WK == 1 || (sizeof(T) == 4 && D == 64) ? 2 : 1;  // fp32 is bound by the products: two blocks on a CU would leave others idle
+};
+
 // Bytes of the unnormalised sums of a forward in pieces; behind them, two floats a row and piece.
 inline size_t packed_fwd_acc_bytes(int64_t total_q, int Hq, int d, int splits) { return splits > 1 ? align_up((size_t)total_q * Hq * splits * d * 4, 256) : 0; }
+// How a step walks: own rows (queries times the heads that share, or keys) in tiles of 128, or of 32 whose four waves share the other axis; and
+// that axis in pieces, joined afterwards.
+struct Walk {
+    bool few;
+    int splits, chunk;
+};
+// The forward's: rows and keys of all sequences and of the longest (api_packed.hip).
+Walk plan_forward(int dtype, int d, bool causal, int64_t own, int64_t max_own, int64_t heads, int64_t n_seq, int64_t other, int64_t max_other);
 // few: tiles of 32 rows whose four waves share the long axis, else 128 rows, 32 a wave
 dsv_status launch_packed_fwd(const PackedArgs &a, int dtype, int d, bool few, const void *Q, const void *K, const void *V, void *O, void *O_tail,
                              float *lse, char *ws, hipStream_t st);

@@ -4,7 +4,7 @@
 //
 // One pass over the keys with the running maximum and sum.  A wave owns 32 rows as the columns of its products, S^T = K Q^T and
 // O^T = V^T P^T: a lane then holds one row's scores, the maximum and the sum are its own but for one exchange between the halves, and
-// the scores are where the second product wants them.
+// the scores are where the second product wants them.  Keys come from rows of the caller's tensors, or from the pages of an 8-bit cache.
 //
 // Long calls are bound by power: 1.83 GHz of 2.4 under products and exponentials together (a tile of 64 keys, d = 128: 1056 cycles of
 // products, about 960 of vector work a wave, two waves a SIMD; products busy 56 % of the time a CU has blocks, and laying the weights of
@@ -13,28 +13,77 @@
 // 24 + 4 us with the join, 3.7 TB/s.  Few keys (34128 queries of 16 heads against 77 .. 512, d = 64): 57 us, half of it Q and O themselves, the
 // rest the chain from lengths to rows to scores of a block that walks two to eight tiles.  fp32 is bound by its products (64 cycles each):
 // 1724 tokens of two heads, d = 64, 17.5 us and 4 for the join, each by itself; 19.3 one call behind another.
-#include "packed_attn.h"
+#include "cache_tiles.h"
 
 namespace dsv {
 namespace {
 
-// WK = 1: the four waves own 32 rows each and share tiles of 64 keys.  WK = 4: they own the same 32 rows and take 32 keys each of a tile of
-// 128; for calls of few rows.  NBUF: tiles in LDS in turn.  (For WK = 1 the next tile's scores laid between the weights of this one, and
-// wave priorities by turns, were no faster; two groups of 32 rows a wave, one's products beside the other's weights: 306 us for 277 at 2 x 8192 tokens.)
-template <typename T, int D, int WK> struct FwdShape {
-    static constexpr int ROWS = WK == 1 ? 128 : 32, KEYS = WK == 1 ? 64 : 128, KT = KEYS / 32 / WK;
-    static constexpr int TILE = KEYS * D * (int)sizeof(T);
-    static constexpr int NBUF = WK == 1 || (sizeof(T) == 4 && D == 64) ? 2 : 1;  // fp32 is bound by the products: two blocks on a CU would leave others idle
+// Tiles loaded directly into LDS from rows of the caller's tensors.
+template <typename T, int D, int WK> struct RowTiles {
+    typedef FwdShape<T, D, WK> Sh;
+    const T *K, *V;
+    const unsigned char *kp, *vp;
+    int nk;
+    RowLoads<T, D, Sh::KEYS, 4> kl, vl;
+    __device__ __forceinline__ void begin(const PackedArgs &a, int, const Sequence &sq, int hk, int wave)
+    {
+        kp = reinterpret_cast<const unsigned char *>(K) + (int64_t)sq.k0 * a.k_row + (int64_t)hk * a.k_head;
+        vp = reinterpret_cast<const unsigned char *>(V) + (int64_t)sq.k0 * a.v_row + (int64_t)hk * a.v_head;
+        nk = sq.nk;
+        kl.set(wave, a.k_row);
+        vl.set(wave, a.v_row);
+    }
+    template <typename Scores, typename Rest>
+    __device__ __forceinline__ void walk(const PackedArgs &a, int kbeg, int kend, unsigned char *ka, unsigned char *va, unsigned char *kb, unsigned char *vb,
+                                         Scores scores, Rest rest)
+    {
+        if constexpr (Sh::NBUF == 2) {
+            auto request = [&](int k0, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
+                kl.keys(kp, a.k_row, k0, nk, kt);
+                vl.keys(vp, a.v_row, k0, nk, vt);
+            };
+            auto tile = [&](int k0, const unsigned char *kt, const unsigned char *vt) __attribute__((always_inline)) {
+                floatx16_t s[Sh::KT];
+                scores(kt, s);
+                rest(k0, s, vt);
+            };
+            request(kbeg, ka, va);
+            for (int k0 = kbeg; k0 < kend; k0 += 2 * Sh::KEYS) {
+                wait_loads_and_sync();
+                if (k0 + Sh::KEYS < kend) request(k0 + Sh::KEYS, kb, vb);
+                tile(k0, ka, va);
+                if (k0 + Sh::KEYS < kend) {  // (a break here makes the compiler move all sums to other registers and back)
+                    wait_loads_and_sync();
+                    if (k0 + 2 * Sh::KEYS < kend) request(k0 + 2 * Sh::KEYS, ka, va);
+                    tile(k0 + Sh::KEYS, kb, vb);
+                }
+            }
+        } else {
+            // one tile of each, V on its way while the scores are formed and the next K while V is summed: room for two blocks
+            kl.keys(kp, a.k_row, kbeg, nk, ka);
+            for (int k0 = kbeg; k0 < kend; k0 += Sh::KEYS) {
+                wait_loads_and_sync();
+                vl.keys(vp, a.v_row, k0, nk, va);
+                floatx16_t s[Sh::KT];
+                scores(ka, s);
+                wait_loads_and_sync();
+                if (k0 + Sh::KEYS < kend) kl.keys(kp, a.k_row, k0 + Sh::KEYS, nk, ka);
+                rest(k0, s, va);
+            }
+        }
+    }
 };
 
 // lse of a row whose weights, against m, add up to l.  Only a sum of zero is one over no keys: a score that is no number, or infinite, makes l no
 // number, and lse and O with it; taken for a row without keys it would have gradients of zero.
 __device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? kNegInf : (m + __builtin_amdgcn_logf(l)) * kLn2; }
 
-template <typename T, int D, int WK>
-__global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2) void packed_fwd_kernel(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V,
-                                                                                        T *__restrict__ O, bf16_t *__restrict__ O_tail, float *__restrict__ lse,
-                                                                                        float2 *__restrict__ pml, float *__restrict__ pacc, PackedArgs a)
+// A: the descriptor, with read_sequence() of its own.  Tiles: brings tiles of keys into LDS,
+//   begin(a, sequence's number, sequence, head of K and V, wave)
+//   walk(a, first key, key behind the last, two tiles of K and V each (for NBUF = 1 the second two are not there), scores(K tile, s), rest(key, s, V tile))
+template <typename T, int D, int WK, typename A, typename Tiles>
+__device__ __forceinline__ void attend(const T *__restrict__ Q, T *__restrict__ O, bf16_t *__restrict__ O_tail, float *__restrict__ lse, float2 *__restrict__ pml,
+                                       float *__restrict__ pacc, const A &a, Tiles tiles)
 {
     typedef RowTile<T, D> RT;
     typedef FwdShape<T, D, WK> Sh;
@@ -67,15 +116,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
 #pragma unroll
         for (int m = 0; m < NM; ++m) qf[m] = *reinterpret_cast<const Frag<T> *>(qp + (2 * m + half) * 16);
     }
-    const unsigned char *kp = reinterpret_cast<const unsigned char *>(K) + (int64_t)sq.k0 * a.k_row + (int64_t)hk * a.k_head;
-    const unsigned char *vp = reinterpret_cast<const unsigned char *>(V) + (int64_t)sq.k0 * a.v_row + (int64_t)hk * a.v_head;
-    RowLoads<T, D, Sh::KEYS, 4> kl, vl;
-    kl.set(wave, a.k_row);
-    vl.set(wave, a.v_row);
-    auto request = [&](int k0, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
-        kl.keys(kp, a.k_row, k0, sq.nk, kt);
-        vl.keys(vp, a.v_row, k0, sq.nk, vt);
-    };
+    tiles.begin(a, si, sq, hk, wave);
 
     const float c = a.scale * kLog2e;
     floatx16_t acc[NB];
@@ -128,38 +169,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
         l += lt;
         lr += lrt;
     };
-    auto tile = [&](int k0, const unsigned char *kt, const unsigned char *vt) __attribute__((always_inline)) {
-        floatx16_t s[KT];
-        scores(kt, s);
-        rest(k0, s, vt);
-    };
-    if (kbeg < kend) {
-        if constexpr (Sh::NBUF == 2) {
-            request(kbeg, ka, va);
-            for (int k0 = kbeg; k0 < kend; k0 += 2 * Sh::KEYS) {
-                wait_loads_and_sync();
-                if (k0 + Sh::KEYS < kend) request(k0 + Sh::KEYS, kb, vb);
-                tile(k0, ka, va);
-                if (k0 + Sh::KEYS < kend) {  // (a break here makes the compiler move all sums to other registers and back)
-                    wait_loads_and_sync();
-                    if (k0 + 2 * Sh::KEYS < kend) request(k0 + 2 * Sh::KEYS, ka, va);
-                    tile(k0 + Sh::KEYS, kb, vb);
-                }
-            }
-        } else {
-            // one tile of each, V on its way while the scores are formed and the next K while V is summed: room for two blocks
-            kl.keys(kp, a.k_row, kbeg, sq.nk, ka);
-            for (int k0 = kbeg; k0 < kend; k0 += Sh::KEYS) {
-                wait_loads_and_sync();
-                vl.keys(vp, a.v_row, k0, sq.nk, va);
-                floatx16_t s[KT];
-                scores(ka, s);
-                wait_loads_and_sync();
-                if (k0 + Sh::KEYS < kend) kl.keys(kp, a.k_row, k0 + Sh::KEYS, sq.nk, ka);
-                rest(k0, s, va);
-            }
-        }
-    }
+    if (kbeg < kend) tiles.walk(a, kbeg, kend, ka, va, kb, vb, scores, rest);
     l = halves_sum(l);
     // Weights go into the product as one bf16 word: a second one, as the sparse forward has it, would make three products of two, in a kernel bound by
     // their power.  O is the average by the weights that were summed, lse the logarithm of the unrounded ones': rounding then moves weight between the keys and
@@ -274,9 +284,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
 }
 
 // The pieces of a row joined: weights 2^(m_s - max).
-template <typename T, int D, int GROUPS>
+template <typename T, int D, int GROUPS, typename A>
 __global__ __launch_bounds__(256) void packed_fwd_merge_kernel(const float2 *__restrict__ pml, const float *__restrict__ pacc, T *__restrict__ O,
-                                                               bf16_t *__restrict__ O_tail, float *__restrict__ lse, PackedArgs a)
+                                                               bf16_t *__restrict__ O_tail, float *__restrict__ lse, A a)
 {
     constexpr int LPR = D / 4, PL = 64 / LPR;  // pieces a lane weighs, of 64 at most
     int tok, head;
@@ -333,6 +343,36 @@ __global__ __launch_bounds__(256) void packed_fwd_merge_kernel(const float2 *__r
     if (lane == 0) lse[(int64_t)head * a.total_q + tok] = row_lse(m, l);
 }
 
+template <typename T, int D, typename A>
+dsv_status launch_merge(const A &a, const float2 *pml, const float *pacc, T *O, bf16_t *O_tail, float *lse, hipStream_t st)
+{
+    constexpr int LPR = D / 4, G = 256 / LPR;
+    if (wide_merge(a.splits, (int64_t)a.total_q * a.Hq))
+        packed_fwd_merge_kernel<T, D, G, A><<<merge_grid<LPR, G>(a.total_q, a.Hq), 256, 0, st>>>(pml, pacc, O, O_tail, lse, a);
+    else
+        packed_fwd_merge_kernel<T, D, 1, A><<<merge_grid<LPR, 1>(a.total_q, a.Hq), 256, 0, st>>>(pml, pacc, O, O_tail, lse, a);
+    DSV_LAUNCH_CHECK();
+    return DSV_OK;
+}
+
+template <typename T, int D, int WK>
+__global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2) void packed_fwd_kernel(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V,
+                                                                                        T *__restrict__ O, bf16_t *__restrict__ O_tail, float *__restrict__ lse,
+                                                                                        float2 *__restrict__ pml, float *__restrict__ pacc, PackedArgs a)
+{
+    RowTiles<T, D, WK> tiles;
+    tiles.K = K;
+    tiles.V = V;
+    attend<T, D, WK>(Q, O, O_tail, lse, pml, pacc, a, tiles);
+}
+
+template <typename T, int D, int WK>
+__global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2) void cache_fwd_kernel(const T *__restrict__ Q, T *__restrict__ O, float *__restrict__ lse,
+                                                                                       float2 *__restrict__ pml, float *__restrict__ pacc, CachedArgs a)
+{
+    attend<T, D, WK>(Q, O, nullptr, lse, pml, pacc, a, PageTiles<T, D, WK>(a));
+}
+
 template <typename T, int D, int WK>
 dsv_status launch_t(const PackedArgs &a, const void *Q, const void *K, const void *V, void *O, void *O_tail, float *lse, char *ws, hipStream_t st)
 {
@@ -342,15 +382,22 @@ dsv_status launch_t(const PackedArgs &a, const void *Q, const void *K, const voi
     packed_fwd_kernel<T, D, WK><<<dim3((unsigned)(slots * a.Hkv), a.splits), 256, 0, st>>>(
         static_cast<const T *>(Q), static_cast<const T *>(K), static_cast<const T *>(V), static_cast<T *>(O), static_cast<bf16_t *>(O_tail), lse, pml, pacc, a);
     DSV_LAUNCH_CHECK();
-    if (a.splits > 1) {
-        constexpr int LPR = D / 4, G = 256 / LPR;
-        if (wide_merge(a.splits, (int64_t)a.total_q * a.Hq))
-            packed_fwd_merge_kernel<T, D, G><<<merge_grid<LPR, G>(a.total_q, a.Hq), 256, 0, st>>>(pml, pacc, static_cast<T *>(O), static_cast<bf16_t *>(O_tail), lse, a);
-        else
-            packed_fwd_merge_kernel<T, D, 1><<<merge_grid<LPR, 1>(a.total_q, a.Hq), 256, 0, st>>>(pml, pacc, static_cast<T *>(O), static_cast<bf16_t *>(O_tail), lse, a);
-        DSV_LAUNCH_CHECK();
-    }
+    if (a.splits > 1) return launch_merge<T, D>(a, pml, pacc, static_cast<T *>(O), static_cast<bf16_t *>(O_tail), lse, st);
     return DSV_OK;
+}
+template <typename T, int D, int WK> dsv_status launch_cached_t(const CachedArgs &a, const void *Q, void *O, float *lse, char *ws, hipStream_t st)
+{
+    const int64_t slots = tile_slots(a.total_q, a.group, FwdShape<T, D, WK>::ROWS, a.n_seq);
+    float *const pacc = reinterpret_cast<float *>(ws);
+    float2 *const pml = reinterpret_cast<float2 *>(ws + packed_fwd_acc_bytes(a.total_q, a.Hq, D, a.splits));
+    cache_fwd_kernel<T, D, WK><<<dim3((unsigned)(slots * a.Hkv), a.splits), 256, 0, st>>>(static_cast<const T *>(Q), static_cast<T *>(O), lse, pml, pacc, a);
+    DSV_LAUNCH_CHECK();
+    if (a.splits > 1) return launch_merge<T, D>(a, pml, pacc, static_cast<T *>(O), nullptr, lse, st);
+    return DSV_OK;
+}
+template <typename T, int D> dsv_status launch_cached_d(const CachedArgs &a, bool few, const void *Q, void *O, float *lse, char *ws, hipStream_t st)
+{
+    return few ? launch_cached_t<T, D, 4>(a, Q, O, lse, ws, st) : launch_cached_t<T, D, 1>(a, Q, O, lse, ws, st);
 }
 }  // namespace
 
@@ -363,6 +410,12 @@ dsv_status launch_packed_fwd(const PackedArgs &a, int dtype, int d, bool few, co
     }
     if (d == 128) return few ? launch_t<float, 128, 4>(a, Q, K, V, O, nullptr, lse, ws, st) : launch_t<float, 128, 1>(a, Q, K, V, O, nullptr, lse, ws, st);
     return few ? launch_t<float, 64, 4>(a, Q, K, V, O, nullptr, lse, ws, st) : launch_t<float, 64, 1>(a, Q, K, V, O, nullptr, lse, ws, st);
+}
+
+dsv_status launch_cache_fwd(const CachedArgs &a, int dtype, int d, bool few, const void *Q, void *O, float *lse, char *ws, hipStream_t st)
+{
+    if (dtype == DSV_BF16) return d == 128 ? launch_cached_d<bf16_t, 128>(a, few, Q, O, lse, ws, st) : launch_cached_d<bf16_t, 64>(a, few, Q, O, lse, ws, st);
+    return d == 128 ? launch_cached_d<float, 128>(a, few, Q, O, lse, ws, st) : launch_cached_d<float, 64>(a, few, Q, O, lse, ws, st);
 }
 
 }  // namespace dsv
