@@ -154,26 +154,39 @@ __global__ __launch_bounds__(256) void gated_fwd_kernel(const T *X, const T *__r
 // A segment of several blocks leaves its sums in rows of `part` [..][3][n], 2 floor(first row / rows a block) onwards: no two such segments share one.
 __device__ __forceinline__ int64_t part_row(const GatedNormArgs &a, int first) { return 2 * (int64_t)(first / a.rows); }
 
+// What is not there -- a modulation, Y, dH, elements past the row's end -- is held as zeros (a gate that is not there as ones), so that no element asks.
+// Past the end that leaves numbers in no sum but dg, of columns that are not written.
 template <typename T, int CH, int LPR, int NP>
-__global__ __launch_bounds__(256) void gated_bwd_kernel(const T *__restrict__ X, const T *__restrict__ Y, const T *__restrict__ gate, const T *__restrict__ scale,
-                                                        const float4 *__restrict__ stats, const T *__restrict__ dZ, const T *dH, T *dX,
-                                                        T *__restrict__ dY, float *dgate, float *dscale, float *dshift, float *__restrict__ part, GatedNormArgs a)
+__global__ __launch_bounds__(256, NP * CH <= 8 ? 3 : NP * CH <= 16 ? 2 : 1) void gated_bwd_kernel(const T *__restrict__ X, const T *__restrict__ Y, const T *__restrict__ gate,
+                                                                                   const T *__restrict__ scale, const float4 *__restrict__ stats,
+                                                                                   const T *__restrict__ dZ, const T *dH, T *dX, T *__restrict__ dY, float *dgate,
+                                                                                   float *dscale, float *dshift, float *__restrict__ part, GatedNormArgs a)
 {
     typedef Lane<T, CH, LPR, NP> L;
     constexpr int RPB = 256 / LPR;
+    constexpr bool kAhead = NP * CH <= 16;  // the next row's loads under way: its registers would be others' with more elements
     __shared__ float2 red[2][4];
     const Span s = block_rows(a);
     if (s.count <= 0) return;
     const L l(a.n);
     const float inv_n = 1.f / (float)a.n;
-    typename L::P gp[NP], sp[NP], xn[NP], yn[NP], zn[NP], hn[NP];
-    if (gate) l.load(gate + s.seg * a.gate, gp);
-    if (scale) l.load(scale + s.seg * a.scale, sp);
-    float dg[NP][CH], ds[NP][CH], dt[NP][CH];
+    typename L::P xn[NP] = {}, yn[NP] = {}, zn[NP] = {}, hn[NP] = {};
+    float gf[NP][CH], mf[NP][CH], dg[NP][CH], ds[NP][CH], dt[NP][CH];
+    {
+        typename L::P gp[NP] = {}, sp[NP] = {};
+        if (gate) l.load(gate + s.seg * a.gate, gp);
+        if (scale) l.load(scale + s.seg * a.scale, sp);
 #pragma unroll
-    for (int i = 0; i < NP; ++i)
+        for (int i = 0; i < NP; ++i) {
+            unpack(gp[i], gf[i]);
+            unpack(sp[i], mf[i]);
 #pragma unroll
-        for (int c = 0; c < CH; ++c) dg[i][c] = ds[i][c] = dt[i][c] = 0.f;
+            for (int c = 0; c < CH; ++c) {
+                if (!gate && l.in[i]) gf[i][c] = 1.f;
+                dg[i][c] = ds[i][c] = dt[i][c] = 0.f;
+            }
+        }
+    }
     const int64_t base = s.first + s.row0;
     int k = threadIdx.x / LPR, turn = 0;
     float4 stn = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -184,80 +197,65 @@ __global__ __launch_bounds__(256) void gated_bwd_kernel(const T *__restrict__ X,
         if (dH) l.load(dH + row * a.dh, hn);
         stn = stats[row];
     };
-    if (k < s.count) load(base + k);
+    if (kAhead && k < s.count) load(base + k);
     for (; k < s.count; k += RPB) {
         const int64_t row = base + k;
+        if (!kAhead) load(row);
         typename L::P hp[NP];
-        const float4 st = stn;  // mean and 1 / deviation of h, of y
+        const float mu = stn.x, r = stn.y, mu_y = a.post ? stn.z : 0.f, r_y = a.post ? stn.w : 1.f;
         float u[NP][CH], xh[NP][CH], w[NP][CH], s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            float x[CH], y[CH], dz[CH], g[CH], m[CH];
+            float x[CH], y[CH], dz[CH];
             unpack(xn[i], x);
-            if (Y) unpack(yn[i], y);
+            unpack(yn[i], y);
             unpack(zn[i], dz);
             hp[i] = hn[i];
-            if (gate) unpack(gp[i], g);
-            if (scale) unpack(sp[i], m);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                float h = a.residual * x[c];
-                u[i][c] = 0.f;
-                if (Y) {
-                    u[i][c] = a.post ? (y[c] - st.z) * st.w : y[c];
-                    h += gate ? g[c] * u[i][c] : u[i][c];
-                }
-                xh[i][c] = l.in[i] ? (h - st.x) * st.y : 0.f;
-                const float d = l.in[i] ? dz[c] : 0.f;
-                w[i][c] = scale && l.in[i] ? fmaf(d, m[c], d) : d;
-                dt[i][c] += d;
-                ds[i][c] = fmaf(d, xh[i][c], ds[i][c]);
+                u[i][c] = (y[c] - mu_y) * r_y;
+                xh[i][c] = (fmaf(gf[i][c], u[i][c], a.residual * x[c]) - mu) * r;
+                w[i][c] = fmaf(dz[c], mf[i][c], dz[c]);
+                dt[i][c] += dz[c];
+                ds[i][c] = fmaf(dz[c], xh[i][c], ds[i][c]);
                 s1 += w[i][c];
                 s2 = fmaf(w[i][c], xh[i][c], s2);
             }
         }
-        if (k + RPB < s.count) load(row + RPB);  // on its way while this row is worked on
+        if (kAhead && k + RPB < s.count) load(row + RPB);  // on its way while this row is worked on
         const float2 sums = row_sums<LPR>(s1, s2, red[turn ^= 1]);
         const float m1 = a.rms ? 0.f : sums.x * inv_n, m2 = sums.y * inv_n;
         float t1 = 0.f, t2 = 0.f;
         T *const dx = dX + row * a.dx;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            float g[CH], dh[CH], o[CH];
-            if (gate) unpack(gp[i], g);
-            if (dH) unpack(hp[i], dh);
+            float dh[CH], o[CH];
+            unpack(hp[i], dh);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                float d = st.y * (w[i][c] - m1 - xh[i][c] * m2);
-                if (dH) d += dh[c];
-                d = l.in[i] ? d : 0.f;
+                const float d = fmaf(r, w[i][c] - m1 - xh[i][c] * m2, dh[c]);
                 o[c] = a.residual * d;
-                dg[i][c] = fmaf(d, l.in[i] ? u[i][c] : 0.f, dg[i][c]);
-                const float v = gate && l.in[i] ? g[c] * d : d;
-                w[i][c] = v;
-                if (a.post) {
-                    t1 += v;
-                    t2 = fmaf(v, l.in[i] ? u[i][c] : 0.f, t2);
-                }
+                dg[i][c] = fmaf(d, u[i][c], dg[i][c]);
+                w[i][c] = gf[i][c] * d;
+                t1 += w[i][c];
+                t2 = fmaf(w[i][c], u[i][c], t2);
             }
             if (l.in[i]) put(dx + l.at(i), o);
         }
         if (Y) {
-            float n1 = 0.f, n2 = 0.f, r = 1.f;
+            float n1 = 0.f, n2 = 0.f;
             if (a.post) {
                 const float2 t = row_sums<LPR>(t1, t2, red[turn ^= 1]);
                 n1 = a.rms ? 0.f : t.x * inv_n;
                 n2 = t.y * inv_n;
-                r = st.w;
             }
             T *const dy = dY + row * a.dy;
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                if (!l.in[i]) continue;
                 float o[CH];
 #pragma unroll
-                for (int c = 0; c < CH; ++c) o[c] = a.post ? r * (w[i][c] - n1 - u[i][c] * n2) : w[i][c];
-                put(dy + l.at(i), o);
+                for (int c = 0; c < CH; ++c) o[c] = r_y * (w[i][c] - n1 - u[i][c] * n2);
+                if (l.in[i]) put(dy + l.at(i), o);
             }
         }
     }
@@ -265,46 +263,42 @@ __global__ __launch_bounds__(256) void gated_bwd_kernel(const T *__restrict__ X,
     // the sums of the block's lane groups, a piece of each lane at a time
     const bool whole = s.len <= a.rows;
     float *const to = part + (whole ? 0 : (part_row(a, s.first) + s.row0 / a.rows) * 3 * a.n);
-    auto out = [&](int which, int col, float v) __attribute__((always_inline)) {
-        if (!whole) {
-            to[(int64_t)which * a.n + col] = v;
-            return;
-        }
-        float *const d = which == 0 ? dgate : which == 1 ? dscale : dshift;
-        if (d) d[s.seg * (which == 0 ? a.dgate : which == 1 ? a.dscale : a.dshift) + col] = v;
-    };
+    float *const to0 = whole ? dgate + s.seg * a.dgate : to, *const to1 = whole ? dscale + s.seg * a.dscale : to + a.n,
+          *const to2 = whole ? dshift + s.seg * a.dshift : to + 2 * a.n;
+    const bool w0 = dgate, w1 = dscale, w2 = dshift;
     if constexpr (RPB == 1) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             if (!l.in[i]) continue;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                out(0, l.at(i) + c, dg[i][c]);
-                out(1, l.at(i) + c, ds[i][c]);
-                out(2, l.at(i) + c, dt[i][c]);
+                if (w0) to0[l.at(i) + c] = dg[i][c];
+                if (w1) to1[l.at(i) + c] = ds[i][c];
+                if (w2) to2[l.at(i) + c] = dt[i][c];
             }
         }
     } else {
-        __shared__ float acc[RPB][3][LPR * CH];
+        __shared__ float acc[RPB][LPR * CH];
         const int grp = threadIdx.x / LPR;
+        auto join = [&](const float (&v)[NP][CH], float *out) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            __syncthreads();
+            for (int i = 0; i < NP; ++i) {
+                __syncthreads();
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                acc[grp][0][l.lane * CH + c] = dg[i][c];
-                acc[grp][1][l.lane * CH + c] = ds[i][c];
-                acc[grp][2][l.lane * CH + c] = dt[i][c];
+                for (int c = 0; c < CH; ++c) acc[grp][l.lane * CH + c] = v[i][c];
+                __syncthreads();
+                for (int e = threadIdx.x; e < LPR * CH; e += 256) {
+                    const int col = i * LPR * CH + e;
+                    float x = 0.f;
+#pragma unroll
+                    for (int g = 0; g < RPB; ++g) x += acc[g][e];
+                    if (col < a.n) out[col] = x;
+                }
             }
-            __syncthreads();
-            for (int e = threadIdx.x; e < 3 * LPR * CH; e += 256) {
-                const int which = e / (LPR * CH), off = e - which * (LPR * CH), col = i * LPR * CH + off;
-                float v = 0.f;
-#pragma unroll
-                for (int g = 0; g < RPB; ++g) v += acc[g][which][off];
-                if (col < a.n) out(which, col, v);
-            }
-        }
+        };
+        if (w0) join(dg, to0);
+        if (w1) join(ds, to1);
+        if (w2) join(dt, to2);
     }
 }
 
@@ -314,6 +308,7 @@ __global__ __launch_bounds__(256) void gated_sum_kernel(const float *__restrict_
     __shared__ float acc[8][33];
     const int seg = blockIdx.x / col_blocks, c = threadIdx.x & 31, g = threadIdx.x >> 5, col = (blockIdx.x - seg * col_blocks) * 32 + c, which = blockIdx.y;
     float *const d = which == 0 ? dgate : which == 1 ? dscale : dshift;
+    const int64_t row = which == 0 ? a.dgate : which == 1 ? a.dscale : a.dshift;
     if (!d) return;
     const int first = min(max(a.cu[seg], 0), a.tokens), len = min(max(a.cu[seg + 1], first), a.tokens) - first;
     if (len > 0 && len <= a.rows) return;  // written by its one block
@@ -321,7 +316,7 @@ __global__ __launch_bounds__(256) void gated_sum_kernel(const float *__restrict_
     float v = 0.f;
     if (col < a.n) {
         const float *const p = part + (part_row(a, first) * 3 + which) * a.n + col;
-#pragma unroll 4
+#pragma unroll 8
         for (int b = g; b < blocks; b += 8) v += p[(int64_t)b * 3 * a.n];
     }
     acc[g][c] = v;
@@ -330,8 +325,42 @@ __global__ __launch_bounds__(256) void gated_sum_kernel(const float *__restrict_
         v = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v += acc[i][c];
-        d[seg * (which == 0 ? a.dgate : which == 1 ? a.dscale : a.dshift) + col] = v;
+        d[seg * row + col] = v;
     }
+}
+
+// Lanes to a row and pieces to a lane: few elements a lane, a row to a block where a wave would hold more than two pieces.  (A wave to rows of 2048, four
+// pieces a lane: the backward's registers leave one wave a SIMD, 32768 rows in bf16 346 us.)
+NormShape bwd_shape(int n, int ch)
+{
+    const int pieces = (n + ch - 1) / ch;
+    if (ch == 1) {
+        for (int np : {1, 4, 8})
+            if (pieces <= 64 * np) return {64, np};
+        int np = 4;
+        while (pieces > 256 * np) np *= 2;
+        return {256, np};
+    }
+    for (int lpr = 8; lpr <= 64; lpr *= 2)
+        if (pieces <= lpr) return {lpr, 1};
+    if (pieces <= 128) return {64, 2};
+    int np = 1;
+    while (pieces > 256 * np) np *= 2;
+    return {256, np};
+}
+// f(integral constants LPR, NP) for the shape of a row
+template <int CH, typename F> dsv_status with_bwd_shape(const NormShape &s, F f)
+{
+#define DSV_SHAPE(L, N) \
+    if (s.lpr == L && s.np == N) return f(std::integral_constant<int, L>{}, std::integral_constant<int, N>{});
+    if constexpr (CH == 1) {
+        DSV_SHAPE(64, 1) DSV_SHAPE(64, 4) DSV_SHAPE(64, 8) DSV_SHAPE(256, 4) DSV_SHAPE(256, 8) DSV_SHAPE(256, 16) DSV_SHAPE(256, 32)
+    } else {
+        DSV_SHAPE(8, 1) DSV_SHAPE(16, 1) DSV_SHAPE(32, 1) DSV_SHAPE(64, 1) DSV_SHAPE(64, 2) DSV_SHAPE(256, 1) DSV_SHAPE(256, 2) DSV_SHAPE(256, 4)
+        if constexpr (CH == 4) { DSV_SHAPE(256, 8) }
+    }
+#undef DSV_SHAPE
+    return DSV_EUNSUPPORTED;
 }
 
 int rows_a_block(int64_t tokens, int lpr, int blocks)
@@ -340,7 +369,9 @@ int rows_a_block(int64_t tokens, int lpr, int blocks)
     return (int)std::max<int64_t>(1, (tokens + (int64_t)blocks * rpb - 1) / ((int64_t)blocks * rpb)) * rpb;
 }
 constexpr int kFwdBlocks = 2048;
-constexpr int kBwdBlocks = 512;
+// Backward: three blocks of up to 8 elements a lane run on a CU at once, and each leaves 3 n floats to sum.  32768 rows of 2048 in bf16, 20280 of 1536 in
+// fp32 with post, us: 512 blocks 200, 184; 768 183, 159; 1024 (four a CU, at 128 registers) 257, 372.
+constexpr int kBwdBlocks = 768;
 int bwd_rows(int64_t tokens, int lpr) { return rows_a_block(tokens, lpr, kBwdBlocks); }
 int chunk_of(int dtype, bool wide) { return !wide ? 1 : dtype == DSV_BF16 ? 8 : 4; }
 
@@ -361,9 +392,9 @@ template <typename T, int CH>
 dsv_status bwd_t(GatedNormArgs a, const GatedNormIn &in, const float4 *stats, const void *dZ, const void *dH, void *dX, void *dY, float *dgate, float *dscale,
                  float *dshift, float *part, hipStream_t st)
 {
-    const NormShape s = norm_shape(a.n, CH);
+    const NormShape s = bwd_shape(a.n, CH);
     a.rows = bwd_rows(a.tokens, s.lpr);
-    return with_shape<CH>(s, [&](auto lpr, auto np) {
+    return with_bwd_shape<CH>(s, [&](auto lpr, auto np) {
         if (a.tokens > 0) {
             gated_bwd_kernel<T, CH, decltype(lpr)::value, decltype(np)::value><<<(unsigned)tile_slots(a.tokens, 1, a.rows, a.n_seg), 256, 0, st>>>(
                 static_cast<const T *>(in.X), static_cast<const T *>(in.Y), static_cast<const T *>(in.gate), static_cast<const T *>(in.scale), stats,
@@ -391,7 +422,7 @@ size_t gated_bwd_bytes(int64_t tokens, int n, int dtype)
 {
     size_t most = 0;
     for (bool wide : {false, true}) {
-        const int rows = bwd_rows(tokens, norm_shape(n, chunk_of(dtype, wide)).lpr);
+        const int rows = bwd_rows(tokens, bwd_shape(n, chunk_of(dtype, wide)).lpr);
         // one segment of more than `rows` at least; the last one's begins at row 2 floor(first / rows) and has ceil(len / rows)
         most = std::max(most, tokens > rows ? (size_t)(2 * (tokens / rows) + 2) * 3 * n * 4 : (size_t)0);
     }
