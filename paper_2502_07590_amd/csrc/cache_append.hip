@@ -44,91 +44,119 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float by)
     return pack_e4m3(lo[0] * by, lo[1] * by, hi[0] * by, hi[1] * by);
 }
 
-// blockIdx: x a page that some sequence may touch, y the first head (others gridDim.y further), z K or V.  N: sixteens of a page a lane.
-template <typename T, int D, int N>
-__global__ __launch_bounds__(256) void cache_append_kernel(AppendIn in, uint8_t *__restrict__ K8, uint8_t *__restrict__ V8, float *__restrict__ kscale,
-                                                           float *__restrict__ vscale, CacheArgs a)
+// Sixteens of a page's new rows, job = row * (D / 16) + sixteen: as loaded, and as numbers.
+template <typename T> struct Raw;
+template <> struct Raw<bf16_t> {
+    uint4 a, b;
+    __device__ __forceinline__ void load(const bf16_t *x, const Sixteen &s)
+    {
+        a = *reinterpret_cast<const uint4 *>(x + s.first);
+        b = *reinterpret_cast<const uint4 *>(x + s.second);
+    }
+    __device__ __forceinline__ void numbers(float (&f)[8], float (&g)[8]) const
+    {
+        unpack(Piece<bf16_t, 8>{a}, f);
+        unpack(Piece<bf16_t, 8>{b}, g);
+    }
+};
+template <> struct Raw<float> {
+    float4 a, b, c, d;
+    __device__ __forceinline__ void load(const float *x, const Sixteen &s)
+    {
+        a = *reinterpret_cast<const float4 *>(x + s.first);
+        b = *reinterpret_cast<const float4 *>(x + s.first + 4);
+        c = *reinterpret_cast<const float4 *>(x + s.second);
+        d = *reinterpret_cast<const float4 *>(x + s.second + 4);
+    }
+    __device__ __forceinline__ void numbers(float (&f)[8], float (&g)[8]) const
+    {
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+        g[0] = c.x; g[1] = c.y; g[2] = c.z; g[3] = c.w; g[4] = d.x; g[5] = d.y; g[6] = d.z; g[7] = d.w;
+    }
+};
+
+enum TurnForm { kStraight, kEights, kAnyPairs };
+
+// Sixteen channels from c0 of a row whose pairs lie anywhere.
+template <typename T> __device__ __forceinline__ void turn_any(const TurnArgs &t, const T *x, int64_t token, int c0, float (&f)[8], float (&g)[8])
 {
-    __shared__ float red[2][4];
-    const int si = __builtin_amdgcn_readfirstlane(find_sequence(a.cu, a.n_seq, a.total, 1, a.page, (int)blockIdx.x, page_gap(a)));
-    const Sequence sq = read_cached(a, si);
-    const int start = sq.nk - sq.nq, place = (int)blockIdx.x - first_slot(a.cu[si], a.total, 1, a.page, si * page_gap(a));
-    if (start < 0 || place < 0 || sq.nq == 0) return;  // a cache shorter than what goes in
-    const int page_no = (start >> a.page_log2) + place;
-    const int64_t page0 = (int64_t)page_no << a.page_log2;
-    if (page0 >= sq.nk) return;
-    const int begun = max(start - (int)page0, 0), count = min((int)(sq.nk - page0), a.page) - begun;
-    const int pg = a.table[(int64_t)si * a.max_pages + page_no];
-    if (pg < 0 || pg >= a.n_pages) return;
+    int pos[3];
+    read_position(t, token, pos);
+    for (int i = 0; i < t.total; ++i) {
+        int lo, hi;
+        pair_channels(t, i, lo, hi);
+        if ((lo < c0 || lo >= c0 + 16) && (hi < c0 || hi >= c0 + 16)) continue;
+        float u = to_f32(x[lo]), v = to_f32(x[hi]);
+        turn<false>(u, v, turn_of(t, pos, i));
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            f[c] = lo == c0 + c ? u : hi == c0 + c ? v : f[c];
+            g[c] = lo == c0 + 8 + c ? u : hi == c0 + 8 + c ? v : g[c];
+        }
+    }
+}
 
-    const bool is_k = blockIdx.z == 0;
-    const T *const src = static_cast<const T *>(is_k ? in.K : in.V);
-    const int64_t row_s = is_k ? in.k_row : in.v_row, head_s = is_k ? in.k_head : in.v_head;
-    uint8_t *const pool = is_k ? K8 : V8;
-    float *const scales = is_k ? kscale : vscale;
-    const bool turned = is_k && in.turn.total > 0;
-    const int64_t token0 = (int64_t)sq.q0 + (page0 + begun - start);  // of the first new row of this page
+// One tensor's new rows of one page, for heads h0, h0 + step, ...: the next head's loads are under way while one is rounded.
+template <typename T, int D, int N, TurnForm FORM>
+__device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__restrict__ src, int64_t row_s, int64_t head_s, uint8_t *__restrict__ pool, float *__restrict__ scales,
+                                            const CacheArgs &a, int pg, int64_t token0, int begun, int count, int h0, int step, float (&red)[2][4])
+{
     constexpr int PER = D / 16;
-
+    const bool interleaved = turns.layout == DSV_TURN_INTERLEAVED;
     Sixteen six[N];
     int row[N];
-    float2 t[N][8];
+    float2 t[FORM == kEights ? N : 1][8];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         const int job = (int)threadIdx.x + j * (int)blockDim.x;
         row[j] = job / PER;
         six[j] = Sixteen{16 * (job % PER), 16 * (job % PER) + 8, -1};
-        if (turned && in.eights) {
-            six[j] = sixteen_of(in.turn, job % PER);
+        if constexpr (FORM == kEights) six[j] = sixteen_of(turns, job % PER);
+    }
+    Raw<T> raw[N];
+    auto load = [&](int h) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (row[j] < count) raw[j].load(src + (token0 + row[j]) * row_s + h * head_s, six[j]);
+    };
+    load(h0);
+    if constexpr (FORM == kEights) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
             if (row[j] < count && six[j].pair >= 0) {
                 int pos[3];
-                read_position(in.turn, token0 + row[j], pos);
+                read_position(turns, token0 + row[j], pos);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) t[j][i] = turn_of(in.turn, pos, six[j].pair + i);
+                for (int i = 0; i < 8; ++i) t[j][i] = turn_of(turns, pos, six[j].pair + i);
             }
-        }
     }
-    int turn_no = 0;
-    for (int h = blockIdx.y; h < a.Hkv; h += gridDim.y) {
+    int flip = 0;
+    for (int h = h0; h < a.Hkv; h += step) {
         float f[N][8], g[N][8], most = 0.f;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             if (row[j] >= count) continue;
-            const T *const x = src + (token0 + row[j]) * row_s + h * head_s;
-            load8(x + six[j].first, f[j]);
-            load8(x + six[j].second, g[j]);
-            if (six[j].pair >= 0) turn_sixteen<false>(in.turn.layout == DSV_TURN_INTERLEAVED, t[j], f[j], g[j]);
-            if (turned && !in.eights) {
-                int pos[3];
-                read_position(in.turn, token0 + row[j], pos);
-                for (int i = 0; i < in.turn.total; ++i) {  // any number of pairs: those that have a channel here
-                    int lo, hi;
-                    pair_channels(in.turn, i, lo, hi);
-                    const int c0 = six[j].first;
-                    if ((lo < c0 || lo >= c0 + 16) && (hi < c0 || hi >= c0 + 16)) continue;
-                    float u = to_f32(x[lo]), v = to_f32(x[hi]);
-                    turn<false>(u, v, turn_of(in.turn, pos, i));
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        f[j][c] = lo == c0 + c ? u : hi == c0 + c ? v : f[j][c];
-                        g[j][c] = lo == c0 + 8 + c ? u : hi == c0 + 8 + c ? v : g[j][c];
-                    }
-                }
-            }
+            raw[j].numbers(f[j], g[j]);
+            if constexpr (FORM == kEights)
+                if (six[j].pair >= 0) turn_sixteen<false>(interleaved, t[j], f[j], g[j]);
+            if constexpr (FORM == kAnyPairs) turn_any(turns, src + (token0 + row[j]) * row_s + h * head_s, token0 + row[j], six[j].first, f[j], g[j]);
 #pragma unroll
             for (int c = 0; c < 8; ++c) {  // numbers alone: one infinity would leave nothing of the page's others
                 most = fabsf(f[j][c]) < __builtin_inff() ? fmaxf(most, fabsf(f[j][c])) : most;
                 most = fabsf(g[j][c]) < __builtin_inff() ? fmaxf(most, fabsf(g[j][c])) : most;
             }
         }
-#pragma unroll
-        for (int s = 32; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
-        if ((threadIdx.x & 63) == 0) red[turn_no][threadIdx.x >> 6] = most;
+        if (h + step < a.Hkv) load(h + step);
         const int64_t at = (int64_t)pg * a.Hkv + h;
         const float held = begun > 0 ? scales[at] : 0.f;
-        __syncthreads();
-        for (int w = 0; w < (int)blockDim.x / 64; ++w) most = fmaxf(most, red[turn_no][w]);
-        turn_no ^= 1;
+#pragma unroll
+        for (int s = 32; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
+        if (blockDim.x > 64) {
+            if ((threadIdx.x & 63) == 0) red[flip][threadIdx.x >> 6] = most;
+            __syncthreads();
+            for (int w = 0; w < (int)blockDim.x / 64; ++w) most = fmaxf(most, red[flip][w]);
+            flip ^= 1;
+        }
         const float s = fmaxf(held, scale_of(most)), inv = 1.f / s;  // exact: a power of two
         uint8_t *const to = pool + at * a.page * D;
         if (held > 0.f && s != held) {  // the values that the page holds, to the larger scale
@@ -143,19 +171,53 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendIn in, uint8_t 
         for (int j = 0; j < N; ++j) {
             if (row[j] >= count) continue;
             uint8_t *const y = to + (begun + row[j]) * D;
-            *reinterpret_cast<uint2 *>(y + six[j].first) = pack8(f[j], inv);
-            *reinterpret_cast<uint2 *>(y + six[j].second) = pack8(g[j], inv);
+            if (!interleaved && FORM == kEights) {
+                *reinterpret_cast<uint2 *>(y + six[j].first) = pack8(f[j], inv);
+                *reinterpret_cast<uint2 *>(y + six[j].second) = pack8(g[j], inv);
+            } else {  // side by side
+                const uint2 lo = pack8(f[j], inv), hi = pack8(g[j], inv);
+                *reinterpret_cast<uint4 *>(y + six[j].first) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            }
         }
         if (threadIdx.x == 0) scales[at] = s;
     }
 }
 
+// blockIdx: x a page that some sequence may touch, y the first head (others gridDim.y further), z K or V.  N: sixteens of a page a lane.
+template <typename T, int D, int N, TurnForm FORM>
+__global__ __launch_bounds__(256) void cache_append_kernel(AppendIn in, uint8_t *__restrict__ K8, uint8_t *__restrict__ V8, float *__restrict__ kscale,
+                                                           float *__restrict__ vscale, CacheArgs a)
+{
+    __shared__ float red[2][4];
+    const int si = __builtin_amdgcn_readfirstlane(find_sequence(a.cu, a.n_seq, a.total, 1, a.page, (int)blockIdx.x, page_gap(a)));
+    const Sequence sq = read_cached(a, si);
+    const int start = sq.nk - sq.nq, place = (int)blockIdx.x - first_slot(a.cu[si], a.total, 1, a.page, si * page_gap(a));
+    if (start < 0 || place < 0 || sq.nq == 0) return;  // a cache shorter than what goes in
+    const int page_no = (start >> a.page_log2) + place;
+    const int64_t page0 = (int64_t)page_no << a.page_log2;
+    if (page0 >= sq.nk) return;
+    const int begun = max(start - (int)page0, 0), count = min((int)(sq.nk - page0), a.page) - begun;
+    const int pg = a.table[(int64_t)si * a.max_pages + page_no];
+    if (pg < 0 || pg >= a.n_pages) return;
+    const int64_t token0 = (int64_t)sq.q0 + (page0 + begun - start);  // of the first new row of this page
+    if (blockIdx.z == 0)
+        append_page<T, D, N, FORM>(in.turn, static_cast<const T *>(in.K), in.k_row, in.k_head, K8, kscale, a, pg, token0, begun, count, blockIdx.y, gridDim.y, red);
+    else
+        append_page<T, D, N, kStraight>(in.turn, static_cast<const T *>(in.V), in.v_row, in.v_head, V8, vscale, a, pg, token0, begun, count, blockIdx.y, gridDim.y, red);
+}
+
+// Heads to a block, one after another with the sines that they share: as many as leave 2048 blocks.  32568 tokens of 16 heads, d = 128, bf16, us: in 1024
+// blocks (of both tensors together) 115, 3084 96, 4112 101, 7200 106, 15420 142.
+constexpr int64_t kBlocks = 2048;
 template <typename T, int D, int N>
 dsv_status launch_n(const CacheArgs &a, const AppendIn &in, int threads, uint8_t *K8, uint8_t *V8, float *kscale, float *vscale, hipStream_t st)
 {
     const int64_t slots = page_slots(a);
-    const int64_t heads = std::min<int64_t>(a.Hkv, std::max<int64_t>(1, 2048 / slots));
-    cache_append_kernel<T, D, N><<<dim3((unsigned)slots, (unsigned)heads, 2), threads, 0, st>>>(in, K8, V8, kscale, vscale, a);
+    const int64_t heads = std::min<int64_t>(a.Hkv, std::max<int64_t>(1, kBlocks / slots));
+    const dim3 grid((unsigned)slots, (unsigned)heads, 2);
+    if (in.turn.total == 0) cache_append_kernel<T, D, N, kStraight><<<grid, threads, 0, st>>>(in, K8, V8, kscale, vscale, a);
+    else if (in.eights) cache_append_kernel<T, D, N, kEights><<<grid, threads, 0, st>>>(in, K8, V8, kscale, vscale, a);
+    else cache_append_kernel<T, D, N, kAnyPairs><<<grid, threads, 0, st>>>(in, K8, V8, kscale, vscale, a);
     DSV_LAUNCH_CHECK();
     return DSV_OK;
 }
