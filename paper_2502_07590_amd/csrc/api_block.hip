@@ -136,10 +136,29 @@ CacheArgs cache_args(const dsv_cache &p, const int32_t *cu, const int32_t *lens,
     a.max_len = std::min(p.max_len, p.page * p.max_pages);
     return a;
 }
+// As the packed forward's, but for the pieces: lengths of caches, which the kernels alone know, are anything up to the longest, so there are pieces enough
+// that the blocks of a few long ones fill the chip (blocks of a piece that a cache does not reach end at once).
 Walk walk_of(const dsv_cache &p)
 {
-    const int64_t g = p.Hq / p.Hkv, longest = std::min(p.max_len, p.page * p.max_pages);
-    return plan_forward(p.dtype, p.d, p.causal != 0, (int64_t)p.total * g, (int64_t)std::min(p.max_new, p.total) * g, p.Hkv, p.n_seq, p.n_seq * longest, longest);
+    const int64_t g = p.Hq / p.Hkv, longest = std::min(p.max_len, p.page * p.max_pages), own = p.total * g, max_own = (int64_t)std::min(p.max_new, p.total) * g;
+    Walk w = plan_forward(p.dtype, p.d, p.causal != 0, own, max_own, p.Hkv, p.n_seq, p.n_seq * longest, longest);
+    const int64_t rows = w.few ? 32 : 128;
+    const int64_t tiles = std::min<int64_t>((int64_t)p.n_seq * ((max_own + rows - 1) / rows), own / rows + p.n_seq) * p.Hkv;
+    int64_t chunk;
+    if (w.few) {
+        // Bound by memory.  Twelve caches of up to 16001, four heads, group 4, d = 128, us without the join: pieces of 256 keys 23.6, 384 21.1, 512 19.9, 768
+        // 18.9; 64 caches of 2047 .. 19900, two heads, group 7: 640 keys 84, 1280 80, 2560 89; five of up to 1023 in fp32, two heads: 256 10, 512 15.
+        chunk = std::max(tiles * longest / 2048, std::min<int64_t>(512, std::max<int64_t>(256, tiles * longest / 512)));
+    } else {
+        // Two streams of 1560 queries against 21840 and 7800 keys, eight heads on two, d = 128, bf16, us with the join: two pieces 366, five 292, eight 256, twelve 251,
+        // sixteen 265.
+        if (tiles >= 1024) return w;
+        chunk = std::max<int64_t>((longest * tiles + 2047) / 2048, 512);
+    }
+    chunk = (std::max(chunk, (longest + 63) / 64) + 127) / 128 * 128;
+    w.chunk = chunk < longest ? (int)chunk : 0;
+    w.splits = w.chunk ? (int)((longest + chunk - 1) / chunk) : 1;
+    return w;
 }
 size_t cache_fwd_bytes(const dsv_cache &p)
 {

@@ -1,8 +1,5 @@
-// Tiles of keys out of the pages of an 8-bit cache, for the forward of attention.
-//
-// A row is half as long as in bf16 and comes by way of registers: the next tile's bytes are on their way while one is worked on, then widened with
-// the page's scale by the conversion itself (v_cvt_scalef32; exact, the scales being powers of two) and laid into LDS as rows loaded directly would be.
-// A load of a wave is one kilobyte of one page (8 or 16 tokens, and pages begin on multiples of 16), so its page and scales are the wave's.
+// Keys out of the pages of an 8-bit cache, for the forward of attention.  Values are widened with their page's scale by the conversion itself
+// (v_cvt_scalef32; exact, the scales being powers of two).  Pages begin on multiples of 16 tokens, so 16 keys in a row have one page.
 #pragma once
 
 #include "cache.h"
@@ -18,32 +15,44 @@ __device__ __forceinline__ Sequence read_sequence(const CachedArgs &a, int i) { 
 
 dsv_status launch_cache_fwd(const CachedArgs &a, int dtype, int d, bool few, const void *Q, void *O, float *lse, char *ws, hipStream_t st);
 
-// Eight values, low ones first.
-__device__ __forceinline__ void widen8(uint32_t lo, uint32_t hi, float s, bf16_t *to)
+// Values of 8 bits as operands of the products: 8 of them in bf16, 4 in fp32.
+__device__ __forceinline__ bf16x8_t widen8(uint32_t lo, uint32_t hi, float s)
 {
     const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true);
     const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true);
-    *reinterpret_cast<uint4 *>(to) = make_uint4(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d));
+    return __builtin_bit_cast(bf16x8_t, make_uint4(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c),
+                                                   __builtin_bit_cast(uint32_t, d)));
 }
-__device__ __forceinline__ void widen4(uint32_t w, float s, float *to)
+__device__ __forceinline__ floatx4_t widen4(uint32_t w, float s)
 {
     const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, true);
-    *reinterpret_cast<float4 *>(to) = make_float4(a[0], a[1], b[0], b[1]);
+    return floatx4_t{a[0], a[1], b[0], b[1]};
 }
 
-template <typename T, int D, int WK> struct PageTiles {
-    typedef FwdShape<T, D, WK> Sh;
-    typedef RowTile<T, D> RT;
-    static constexpr int RPL = 1024 / D, PPR = D / 16;     // tokens of a load, 16-byte pieces of a token
-    static constexpr int N = Sh::KEYS / RPL / 4;           // loads of a wave for a tile of K, and of V
+// Transposing LDS read of bytes (ds_read_b64_tr_b8): inside every block of 16 lanes, lane i receives eight bytes, the e-th being byte i % 8 at the
+// address passed by lane 2 e + i / 8 of the block.
+typedef int32_t s32x2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) s32x2_t lds_s32x2_t;
+
+// For blocks of 32 rows whose four waves share the keys: every wave reads 32 keys of its own, K straight into the products' registers, V by way of
+// LDS of its own, turned there; no wave waits for another.  The next 32 keys' bytes, and the pages of those after them, are on their way meanwhile.
+template <typename T, int D> struct PageWaves {
+    typedef FwdShape<T, D, 4> Sh;
+    static constexpr int NK = D / 32;                  // 16-byte pieces of a key to a lane: the pieces 2 j + half
+    static constexpr int PPR = D / 16, RPL = 64 / PPR; // pieces of a key, keys of a load of V
+    static constexpr int SUB = (int)sizeof(T);         // products' steps to such a piece
+    struct Step {
+        uint4 k[NK], v[NK];
+        float ks, vs[2];
+        int k0;
+    };
     const CachedArgs &a;
     const int32_t *pages;
-    int hk, wave, last_page, nk, row, piece;
-    uint4 k8[N], v8[N];
-    float ks[N], vs[N];
-    int at0;
+    unsigned char *vt;
+    int hk, wave, last_page, nk, pg[2];
 
-    __device__ __forceinline__ explicit PageTiles(const CachedArgs &args) : a(args) {}
+    __device__ __forceinline__ explicit PageWaves(const CachedArgs &args) : a(args) {}
+    __device__ __forceinline__ static int piece(int m, int half) { return (2 * (m / SUB) + half) * SUB + m % SUB; }
     __device__ __forceinline__ void begin(const CachedArgs &, int si, const Sequence &sq, int hk_, int wave_)
     {
         hk = hk_;
@@ -51,72 +60,235 @@ template <typename T, int D, int WK> struct PageTiles {
         nk = sq.nk;
         last_page = max(0, (sq.nk - 1) >> a.c.page_log2);
         pages = a.c.table + (int64_t)si * a.c.max_pages;
-        row = (threadIdx.x & 63) / PPR;
-        piece = (threadIdx.x & 63) % PPR;
     }
-    // bytes of the tile that begins at key k0, on their way into registers
-    __device__ __forceinline__ void request(int k0)
+    __device__ __forceinline__ void find_pages(int k0)
     {
-        at0 = k0;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int k = k0 + (i * 4 + wave) * RPL;
-            const int pg = min(max(pages[min(k >> a.c.page_log2, last_page)], 0), a.c.n_pages - 1);
-            const int64_t of = (int64_t)pg * a.Hkv + hk;
-            const int64_t at = of * a.c.page * D + (k & (a.c.page - 1)) * D + row * D + piece * 16;
-            k8[i] = *reinterpret_cast<const uint4 *>(a.K8 + at);
-            v8[i] = *reinterpret_cast<const uint4 *>(a.V8 + at);
-            ks[i] = a.kscale[of];
-            vs[i] = a.vscale[of];
-        }
+        for (int g = 0; g < 2; ++g) pg[g] = min(max(pages[min((k0 + 16 * g) >> a.c.page_log2, last_page)], 0), a.c.n_pages - 1);
     }
-    __device__ __forceinline__ void put(uint4 w, float s, int r, unsigned char *tile) const
+    // the bytes of keys k0 .. + 31, whose pages were found; and the pages of keys `then`
+    __device__ __forceinline__ void request(int k0, int then, Step &st)
     {
-        if constexpr (sizeof(T) == 2) {
-            widen8(w.x, w.y, s, reinterpret_cast<bf16_t *>(tile + RT::at(r, 2 * piece)));
-            widen8(w.z, w.w, s, reinterpret_cast<bf16_t *>(tile + RT::at(r, 2 * piece + 1)));
-        } else {
-            widen4(w.x, s, reinterpret_cast<float *>(tile + RT::at(r, 4 * piece)));
-            widen4(w.y, s, reinterpret_cast<float *>(tile + RT::at(r, 4 * piece + 1)));
-            widen4(w.z, s, reinterpret_cast<float *>(tile + RT::at(r, 4 * piece + 2)));
-            widen4(w.w, s, reinterpret_cast<float *>(tile + RT::at(r, 4 * piece + 3)));
-        }
-    }
-    // the tile asked for last, into LDS; behind the sequence's end zeros, whatever the page holds there (a weight of zero times a NaN is one)
-    __device__ __forceinline__ void land(unsigned char *kt, unsigned char *vt)
-    {
-        const bool edge = at0 + Sh::KEYS > nk;
+        const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5, mask = a.c.page - 1;
+        const int64_t of0 = (int64_t)pg[0] * a.Hkv + hk, of1 = (int64_t)pg[1] * a.Hkv + hk, page_b = (int64_t)a.c.page * D;
+        const int64_t at0 = of0 * page_b + (int64_t)(k0 & mask) * D, at1 = of1 * page_b + (int64_t)((k0 + 16) & mask) * D;  // of keys 0 and 16
+        st.k0 = k0;
+        const uint8_t *const kp = a.K8 + (n < 16 ? at0 : at1) + (n & 15) * D + half * 16;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int r = (i * 4 + wave) * RPL + row;
-            if (edge && at0 + r >= nk) k8[i] = v8[i] = make_uint4(0, 0, 0, 0);
-            put(k8[i], ks[i], r, kt);
-            put(v8[i], vs[i], r, vt);
+        for (int j = 0; j < NK; ++j) st.k[j] = *reinterpret_cast<const uint4 *>(kp + 32 * j);
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            const int r0 = i * RPL;  // 8 or 16 keys of one half
+            st.v[i] = *reinterpret_cast<const uint4 *>(a.V8 + (r0 < 16 ? at0 : at1) + (r0 & 15) * D + lane * 16);
         }
+        st.ks = n < 16 ? a.kscale[of0] : a.kscale[of1];
+        st.vs[0] = a.vscale[of0];
+        st.vs[1] = a.vscale[of1];
+        find_pages(then);
+    }
+    // V's rows in LDS: piece p at place p ^ turn(r), so that the 16 rows of a transposing read lie over all banks
+    __device__ __forceinline__ static int at(int r, int p) { return r * D + ((p ^ (D == 128 ? 2 * ((r >> 1) & 3) : 2 * ((r >> 2) & 1))) << 4); }
+    __device__ __forceinline__ void scores(const Step &st, int, const Frag<T> (&own)[D * sizeof(T) / 32], floatx16_t (&s)[1]) const
+    {
+        s[0] = zero16();
+#pragma unroll
+        for (int j = 0; j < NK; ++j) {
+            const uint32_t w[4] = {st.k[j].x, st.k[j].y, st.k[j].z, st.k[j].w};
+#pragma unroll
+            for (int i = 0; i < SUB; ++i) {
+                Frag<T> f;
+                if constexpr (sizeof(T) == 2) f.v = widen8(w[2 * i], w[2 * i + 1], st.ks);
+                else f.v = widen4(w[i], st.ks);
+                s[0] = product(f, own[j * SUB + i], s[0]);
+            }
+        }
+    }
+    __device__ __forceinline__ void add(const Step &st, int, const Weights<T> &w, floatx16_t (&acc)[D / 32]) const
+    {
+        const int lane = threadIdx.x & 63, e = (lane >> 1) & 7, half = lane >> 5;
+        const int r = (e < 4 ? e : 4 + e) + 4 * half, p = (lane >> 4) & 1, sub = (lane & 1) * 8;
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int nb = 0; nb < D / 32; ++nb) {
+                const s32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_s32x2_t *)(vt + at(16 * g + r, 2 * nb + p) + sub));
+                if constexpr (sizeof(T) == 2) {
+                    acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8((uint32_t)x[0], (uint32_t)x[1], st.vs[g]), w.v[g], acc[nb], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const floatx4_t f = widen4((uint32_t)x[q], st.vs[g]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(f[i], w.v[8 * g + 4 * q + i], acc[nb], 0, 0, 0);
+                    }
+                }
+            }
     }
     template <typename Scores, typename Rest>
     __device__ __forceinline__ void walk(const CachedArgs &, int kbeg, int kend, unsigned char *ka, unsigned char *va, unsigned char *kb, unsigned char *vb, Scores scores,
                                          Rest rest)
     {
-        auto tile = [&](int k0, unsigned char *kt, unsigned char *vt) __attribute__((always_inline)) {
-            land(kt, vt);
-            __syncthreads();
-            if (k0 + Sh::KEYS < kend) request(k0 + Sh::KEYS);
+        vt = (wave & 2 ? va : ka) + (wave & 1) * (Sh::TILE / 2);
+        const int mine = 32 * wave;  // of the block's 128 keys
+        auto run = [&](int k0, Step &st) __attribute__((always_inline)) {
+            const int lane = threadIdx.x & 63;
+            const bool edge = st.k0 + 32 > nk;
+            wave_sync();  // reads of the keys before are done with
+#pragma unroll
+            for (int i = 0; i < NK; ++i) {
+                const int r = i * RPL + lane / PPR;
+                // behind the sequence's end zeros, whatever the page holds there (a weight of zero times a NaN is one)
+                if (edge && st.k0 + r >= nk) st.v[i] = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4 *>(vt + at(r, lane % PPR)) = st.v[i];
+            }
+            wave_sync();
+            floatx16_t s[1];
+            scores(st, s);
+            rest(k0, s, st);
+        };
+        if (kbeg + mine >= kend) return;
+        Step one, two;
+        find_pages(kbeg + mine);
+        request(kbeg + mine, kbeg + 128 + mine, one);
+        for (int k0 = kbeg; k0 + mine < kend; k0 += 256) {
+            if (k0 + 128 + mine < kend) request(k0 + 128 + mine, k0 + 256 + mine, two);
+            run(k0, one);
+            if (k0 + 128 + mine < kend) {
+                if (k0 + 256 + mine < kend) request(k0 + 256 + mine, k0 + 384 + mine, one);
+                run(k0 + 128, two);
+            }
+        }
+    }
+};
+
+// For blocks of 128 rows: the waves bring the bytes of the tile after next into registers while one is worked on, and widen and lay those of the next
+// into LDS, as rows loaded directly would be, between the products of this one's scores.  A load of a wave is one kilobyte of one page, so its page
+// and scales are the wave's.
+template <typename T, int D> struct PageTiles {
+    typedef FwdShape<T, D, 1> Sh;
+    typedef RowTile<T, D> RT;
+    static constexpr int RPL = 1024 / D, PPR = D / 16;     // tokens of a load, 16-byte pieces of a token
+    static constexpr int N = Sh::KEYS / RPL / 4;           // loads of a wave for a tile of K, and of V
+    const CachedArgs &a;
+    const int32_t *pages;
+    int hk, wave, last_page, nk, row, piece_no;
+    uint4 raw[2 * N];                                       // K's, then V's
+    float scale[2 * N];
+    int at0, pg[N];
+    uint32_t of_lane;
+    unsigned char *next_k, *next_v;
+    bool more;
+
+    __device__ __forceinline__ explicit PageTiles(const CachedArgs &args) : a(args) {}
+    __device__ __forceinline__ static int piece(int m, int half) { return 2 * m + half; }
+    __device__ __forceinline__ void begin(const CachedArgs &, int si, const Sequence &sq, int hk_, int wave_)
+    {
+        hk = hk_;
+        wave = wave_;
+        nk = sq.nk;
+        last_page = max(0, (sq.nk - 1) >> a.c.page_log2);
+        pages = a.c.table + (int64_t)si * a.c.max_pages;
+        // A lane takes eight channels of a row's first half and the eight across from them: the eight lanes that write 16 bytes at once then write
+        // to all banks (with sixteen side by side half of them met, a quarter of all LDS cycles).  d = 64: of rows two apart.
+        const int g = (threadIdx.x & 63) / PPR;
+        row = D == 128 ? g : (g & 12) | ((g & 1) << 1) | ((g & 2) >> 1);
+        piece_no = (threadIdx.x & 63) % PPR;
+        of_lane = (uint32_t)(row * D + piece_no * 8);
+    }
+    __device__ __forceinline__ void find_pages(int k0)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) pg[i] = min(max(pages[min((k0 + (i * 4 + wave) * RPL) >> a.c.page_log2, last_page)], 0), a.c.n_pages - 1);
+    }
+    // the bytes of the tile that begins at key k0, whose pages were found, on their way into registers; and the pages of the one after it
+    __device__ __forceinline__ void request(int k0)
+    {
+        at0 = k0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int64_t of = (int64_t)pg[i] * a.Hkv + hk;
+            const int64_t at = (of * a.c.page + ((k0 + (i * 4 + wave) * RPL) & (a.c.page - 1))) * D;
+            raw[i] = halves(a.K8 + at + of_lane);
+            raw[N + i] = halves(a.V8 + at + of_lane);
+            scale[i] = a.kscale[of];
+            scale[N + i] = a.vscale[of];
+        }
+        find_pages(k0 + Sh::KEYS);
+    }
+    __device__ __forceinline__ static uint4 halves(const uint8_t *p)
+    {
+        const uint2 lo = *reinterpret_cast<const uint2 *>(p), hi = *reinterpret_cast<const uint2 *>(p + D / 2);
+        return make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+    // one of the 2 N loads into the next tile; behind the sequence's end zeros, whatever the page holds there (a weight of zero times a NaN is one)
+    __device__ __forceinline__ void put(int j)
+    {
+        const int r = (j % N * 4 + wave) * RPL + row;
+        unsigned char *const tile = j < N ? next_k : next_v;
+        uint4 w = raw[j];
+        const float s = scale[j];
+        if (at0 + Sh::KEYS > nk && at0 + r >= nk) w = make_uint4(0, 0, 0, 0);
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<bf16x8_t *>(tile + RT::at(r, piece_no)) = widen8(w.x, w.y, s);
+            *reinterpret_cast<bf16x8_t *>(tile + RT::at(r, PPR + piece_no)) = widen8(w.z, w.w, s);
+        } else {
+            *reinterpret_cast<floatx4_t *>(tile + RT::at(r, 2 * piece_no)) = widen4(w.x, s);
+            *reinterpret_cast<floatx4_t *>(tile + RT::at(r, 2 * piece_no + 1)) = widen4(w.y, s);
+            *reinterpret_cast<floatx4_t *>(tile + RT::at(r, 2 * (PPR + piece_no))) = widen4(w.z, s);
+            *reinterpret_cast<floatx4_t *>(tile + RT::at(r, 2 * (PPR + piece_no) + 1)) = widen4(w.w, s);
+        }
+    }
+    // as tile_scores(), the next tile's puts between the steps
+    __device__ __forceinline__ void scores(const unsigned char *kt, int r, const Frag<T> (&own)[D * sizeof(T) / 32], floatx16_t (&s)[Sh::KT])
+    {
+        constexpr int NM = D * (int)sizeof(T) / 32;
+        const int half = (threadIdx.x & 63) >> 5;
+        Frag<T> f[kAhead][Sh::KT];
+        auto fetch = [&](int m) __attribute__((always_inline)) {
+#pragma unroll
+            for (int t = 0; t < Sh::KT; ++t) f[m % kAhead][t] = row_frag<T, D>(kt, r + 32 * t, m, half);
+        };
+#pragma unroll
+        for (int t = 0; t < Sh::KT; ++t) s[t] = zero16();
+#pragma unroll
+        for (int m = 0; m < kAhead; ++m) fetch(m);
+        pin_order();
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+#pragma unroll
+            for (int t = 0; t < Sh::KT; ++t) s[t] = product(f[m % kAhead][t], own[m], s[t]);
+            if (m + kAhead < NM) fetch(m + kAhead);
+            if (m % 2 == 1 && m / 2 < 2 * N && more) put(m / 2);
+            pin_order();
+        }
+    }
+    __device__ __forceinline__ void add(const unsigned char *vt, int r0, const Weights<T> &w, floatx16_t (&acc)[D / 32]) const { weighted_rows<T, D>(vt, r0, w, acc); }
+    template <typename Scores, typename Rest>
+    __device__ __forceinline__ void walk(const CachedArgs &, int kbeg, int kend, unsigned char *ka, unsigned char *va, unsigned char *kb, unsigned char *vb, Scores scores,
+                                         Rest rest)
+    {
+        static_assert(Sh::NBUF == 2, "one barrier a tile: the next one is laid beside it");
+        auto tile = [&](int k0, unsigned char *kt, unsigned char *vt, unsigned char *kn, unsigned char *vn) __attribute__((always_inline)) {
+            next_k = kn;
+            next_v = vn;
+            more = k0 + Sh::KEYS < kend;
             floatx16_t s[Sh::KT];
             scores(kt, s);
+            if (k0 + 2 * Sh::KEYS < kend) request(k0 + 2 * Sh::KEYS);
             rest(k0, s, vt);
+            __syncthreads();
         };
+        find_pages(kbeg);
         request(kbeg);
-        if constexpr (Sh::NBUF == 2) {
-            for (int k0 = kbeg; k0 < kend; k0 += 2 * Sh::KEYS) {
-                tile(k0, ka, va);
-                if (k0 + Sh::KEYS < kend) tile(k0 + Sh::KEYS, kb, vb);
-            }
-        } else {
-            for (int k0 = kbeg; k0 < kend; k0 += Sh::KEYS) {
-                if (k0 > kbeg) __syncthreads();  // the tile before is done with
-                tile(k0, ka, va);
-            }
+        next_k = ka;
+        next_v = va;
+#pragma unroll
+        for (int j = 0; j < 2 * N; ++j) put(j);
+        if (kbeg + Sh::KEYS < kend) request(kbeg + Sh::KEYS);
+        __syncthreads();
+        for (int k0 = kbeg; k0 < kend; k0 += 2 * Sh::KEYS) {
+            tile(k0, ka, va, kb, vb);
+            if (k0 + Sh::KEYS < kend) tile(k0 + Sh::KEYS, kb, vb, ka, va);
         }
     }
 };

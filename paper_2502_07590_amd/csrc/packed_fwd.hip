@@ -25,6 +25,9 @@ template <typename T, int D, int WK> struct RowTiles {
     const unsigned char *kp, *vp;
     int nk;
     RowLoads<T, D, Sh::KEYS, 4> kl, vl;
+    __device__ __forceinline__ static int piece(int m, int half) { return 2 * m + half; }
+    __device__ __forceinline__ void scores(const unsigned char *kt, int r, const Frag<T> (&own)[D * sizeof(T) / 32], floatx16_t (&s)[Sh::KT]) const { tile_scores<T, D, Sh::KT>(kt, r, own, s); }
+    __device__ __forceinline__ void add(const unsigned char *vt, int r0, const Weights<T> &w, floatx16_t (&acc)[D / 32]) const { weighted_rows<T, D>(vt, r0, w, acc); }
     __device__ __forceinline__ void begin(const PackedArgs &a, int, const Sequence &sq, int hk, int wave)
     {
         kp = reinterpret_cast<const unsigned char *>(K) + (int64_t)sq.k0 * a.k_row + (int64_t)hk * a.k_head;
@@ -79,8 +82,10 @@ template <typename T, int D, int WK> struct RowTiles {
 __device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? kNegInf : (m + __builtin_amdgcn_logf(l)) * kLn2; }
 
 // A: the descriptor, with read_sequence() of its own.  Tiles: brings tiles of keys into LDS,
+//   piece(m, half): which 16 bytes of Q a half of the wave holds for step m of the scores
 //   begin(a, sequence's number, sequence, head of K and V, wave)
-//   walk(a, first key, key behind the last, two tiles of K and V each (for NBUF = 1 the second two are not there), scores(K tile, s), rest(key, s, V tile))
+//   walk(a, first key, key behind the last, two tiles of K and V each (for NBUF = 1 the second two are not there), scores(K tile, s), rest(key, s, V tile)),
+//   which come back as scores(K tile, row, own rows, s) and add(V tile, first row, weights, sums)
 template <typename T, int D, int WK, typename A, typename Tiles>
 __device__ __forceinline__ void attend(const T *__restrict__ Q, T *__restrict__ O, bf16_t *__restrict__ O_tail, float *__restrict__ lse, float2 *__restrict__ pml,
                                        float *__restrict__ pacc, const A &a, Tiles tiles)
@@ -114,7 +119,7 @@ __device__ __forceinline__ void attend(const T *__restrict__ Q, T *__restrict__ 
     {
         const unsigned char *qp = reinterpret_cast<const unsigned char *>(Q) + (int64_t)(sq.q0 + tok) * a.q_row + (int64_t)head * a.q_head;
 #pragma unroll
-        for (int m = 0; m < NM; ++m) qf[m] = *reinterpret_cast<const Frag<T> *>(qp + (2 * m + half) * 16);
+        for (int m = 0; m < NM; ++m) qf[m] = *reinterpret_cast<const Frag<T> *>(qp + Tiles::piece(m, half) * 16);
     }
     tiles.begin(a, si, sq, hk, wave);
 
@@ -124,8 +129,8 @@ __device__ __forceinline__ void attend(const T *__restrict__ Q, T *__restrict__ 
     for (int nb = 0; nb < NB; ++nb) acc[nb] = zero16();
     float mrun = kNegInf, l = 0.f, lr = 0.f;  // lr: sum of the weights as the second product takes them
     const int sub = WK == 1 ? 0 : wave * 32;
-    auto scores = [&](const unsigned char *kt, floatx16_t (&s)[KT]) __attribute__((always_inline)) { tile_scores<T, D, KT>(kt, sub + n, qf, s); };
-    auto rest = [&](int k0, floatx16_t (&s)[KT], const unsigned char *vt) __attribute__((always_inline)) {
+    auto scores = [&](const auto &kt, floatx16_t (&s)[KT]) __attribute__((always_inline)) { tiles.scores(kt, sub + n, qf, s); };
+    auto rest = [&](int k0, floatx16_t (&s)[KT], const auto &vt) __attribute__((always_inline)) {
         // the tile's last key is behind the end, or not seen by the wave's first row
         const bool edge = k0 + Sh::KEYS > kcut || (a.causal && k0 + Sh::KEYS > row_token(a, row0) + past + 1);
         if (edge) {
@@ -164,7 +169,7 @@ __device__ __forceinline__ void attend(const T *__restrict__ Q, T *__restrict__ 
             Weights<T> w;
             w.set(s[t]);
             if constexpr (sizeof(T) == 2) lrt = w.sum(lrt);
-            weighted_rows<T, D>(vt, sub + 32 * t, w, acc);
+            tiles.add(vt, sub + 32 * t, w, acc);
         }
         l += lt;
         lr += lrt;
@@ -344,10 +349,10 @@ __global__ __launch_bounds__(256) void packed_fwd_merge_kernel(const float2 *__r
 }
 
 template <typename T, int D, typename A>
-dsv_status launch_merge(const A &a, const float2 *pml, const float *pacc, T *O, bf16_t *O_tail, float *lse, hipStream_t st)
+dsv_status launch_merge(const A &a, bool wide, const float2 *pml, const float *pacc, T *O, bf16_t *O_tail, float *lse, hipStream_t st)
 {
     constexpr int LPR = D / 4, G = 256 / LPR;
-    if (wide_merge(a.splits, (int64_t)a.total_q * a.Hq))
+    if (wide)
         packed_fwd_merge_kernel<T, D, G, A><<<merge_grid<LPR, G>(a.total_q, a.Hq), 256, 0, st>>>(pml, pacc, O, O_tail, lse, a);
     else
         packed_fwd_merge_kernel<T, D, 1, A><<<merge_grid<LPR, 1>(a.total_q, a.Hq), 256, 0, st>>>(pml, pacc, O, O_tail, lse, a);
@@ -370,7 +375,8 @@ template <typename T, int D, int WK>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2) void cache_fwd_kernel(const T *__restrict__ Q, T *__restrict__ O, float *__restrict__ lse,
                                                                                        float2 *__restrict__ pml, float *__restrict__ pacc, CachedArgs a)
 {
-    attend<T, D, WK>(Q, O, nullptr, lse, pml, pacc, a, PageTiles<T, D, WK>(a));
+    if constexpr (WK == 1) attend<T, D, WK>(Q, O, nullptr, lse, pml, pacc, a, PageTiles<T, D>(a));
+    else attend<T, D, WK>(Q, O, nullptr, lse, pml, pacc, a, PageWaves<T, D>(a));
 }
 
 template <typename T, int D, int WK>
@@ -382,7 +388,8 @@ dsv_status launch_t(const PackedArgs &a, const void *Q, const void *K, const voi
     packed_fwd_kernel<T, D, WK><<<dim3((unsigned)(slots * a.Hkv), a.splits), 256, 0, st>>>(
         static_cast<const T *>(Q), static_cast<const T *>(K), static_cast<const T *>(V), static_cast<T *>(O), static_cast<bf16_t *>(O_tail), lse, pml, pacc, a);
     DSV_LAUNCH_CHECK();
-    if (a.splits > 1) return launch_merge<T, D>(a, pml, pacc, static_cast<T *>(O), static_cast<bf16_t *>(O_tail), lse, st);
+    if (a.splits > 1)
+        return launch_merge<T, D>(a, wide_merge(a.splits, (int64_t)a.total_q * a.Hq), pml, pacc, static_cast<T *>(O), static_cast<bf16_t *>(O_tail), lse, st);
     return DSV_OK;
 }
 template <typename T, int D, int WK> dsv_status launch_cached_t(const CachedArgs &a, const void *Q, void *O, float *lse, char *ws, hipStream_t st)
@@ -392,7 +399,9 @@ template <typename T, int D, int WK> dsv_status launch_cached_t(const CachedArgs
     float2 *const pml = reinterpret_cast<float2 *>(ws + packed_fwd_acc_bytes(a.total_q, a.Hq, D, a.splits));
     cache_fwd_kernel<T, D, WK><<<dim3((unsigned)(slots * a.Hkv), a.splits), 256, 0, st>>>(static_cast<const T *>(Q), static_cast<T *>(O), lse, pml, pacc, a);
     DSV_LAUNCH_CHECK();
-    if (a.splits > 1) return launch_merge<T, D>(a, pml, pacc, static_cast<T *>(O), nullptr, lse, st);
+    // caches come in more pieces than rows of tensors: 24960 rows of 12 took 40 us with a block to a row, 18 with several rows to a wave
+    const int64_t rows = (int64_t)a.total_q * a.Hq;
+    if (a.splits > 1) return launch_merge<T, D>(a, wide_merge(a.splits, rows) && rows < 8192, pml, pacc, static_cast<T *>(O), nullptr, lse, st);
     return DSV_OK;
 }
 template <typename T, int D> dsv_status launch_cached_d(const CachedArgs &a, bool few, const void *Q, void *O, float *lse, char *ws, hipStream_t st)
