@@ -592,6 +592,8 @@ class Norm:
 
 def _rows(c, name: str, t: torch.Tensor, shape, dtype, device):
     """Pointer of a tensor of rows [tokens, heads, n].  Its strides go into the descriptor `c`, which says contiguous ones."""
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
     if t.device != device:
         raise DsvError(f"libdsv takes device tensors, all on one device: {t.device} beside {device}")
     if t.shape != shape or t.dtype != dtype:
@@ -609,6 +611,8 @@ def _flat(what: str, t, shape, dtype, device):
     """Pointer of a contiguous tensor, None for None."""
     if t is None:
         return None
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.device == device:
+        return t.data_ptr()
     if t.device != device or t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise DsvError(f"{what}: expected contiguous {dtype} of shape {shape} on {device}, got {t.dtype} of shape {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
@@ -732,6 +736,7 @@ def layer_norm_bwd(p: Norm, X, gamma, mean, rstd, dY, dX=None, dgamma=None, dbet
 
 
 # ---- what stands around the attention: rotary positions, gated norms, an 8-bit cache --------------------
+_Pairs = ctypes.c_int32 * 3
 _TURN_LAYOUT = {"interleaved": 0, "halves": 1, "axis_halves": 2}
 _TURN_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3}
 _NORM_KIND = {"layer": 0, "rms": 1}
@@ -750,14 +755,14 @@ class Rotary:
     def __init__(self, tokens: int, heads: int, d: int, dtype, pairs, layout: str = "halves", gain: float = 1.0):
         if isinstance(dtype, str):
             dtype = _DTYPE_NAME[dtype]
-        pairs = [pairs] if isinstance(pairs, int) else list(pairs)
+        pairs = [pairs] if isinstance(pairs, int) else pairs
         if not 1 <= len(pairs) <= 3:
             raise DsvError(f"pairs: one to three coordinates, got {len(pairs)}")
         self.tokens, self.heads, self.d, self.gain = _int32("tokens", tokens), _int32("heads", heads), _int32("d", d), float(gain)
         self.pairs, self.layout, self.torch_dtype = [_int32("pairs", n) for n in pairs], layout, dtype
         self.shape, self.pos_shape, self.freq_shape = (self.tokens, self.heads, self.d), (self.tokens, len(pairs)), (sum(self.pairs),)
         rows = _CRows(self.heads * self.d, self.d)
-        self._c = _CRotary(self.tokens, self.heads, self.d, _DTYPE_CODE.get(dtype, -1), len(pairs), (ctypes.c_int32 * 3)(*self.pairs),
+        self._c = _CRotary(self.tokens, self.heads, self.d, _DTYPE_CODE.get(dtype, -1), len(pairs), _Pairs(*self.pairs),
                            _named("layout", _TURN_LAYOUT, layout), self.gain, 0, rows, rows)
 
     @property
@@ -820,6 +825,8 @@ def _row(c, name: str, t, shape, dtype, device):
     """Pointer of a tensor of rows [rows, n], None for None.  Its stride goes into the descriptor `c`, which says contiguous ones."""
     if t is None:
         return None
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
     if t.device != device or t.shape != shape or t.dtype != dtype:
         raise DsvError(f"{name}: expected {dtype} of shape {shape} on {device}, got {t.dtype} of shape {tuple(t.shape)} on {t.device}")
     if not t.is_contiguous():
@@ -836,8 +843,8 @@ def gated_norm_fwd(p: GatedNorm, X, cu, Y=None, gate=None, scale=None, shift=Non
     lib = load_library()
     with _On(X, stream) as on:
         dev, td, c, shape, mod = X.device, p.torch_dtype, _CGatedNorm.from_buffer_copy(p._c), p.shape, p.mod_shape
-        Z = torch.empty(shape, dtype=td, device=dev) if Z is None else Z
-        H = torch.empty(shape, dtype=td, device=dev) if H is None and Y is not None else H
+        Z = torch.empty_like(X) if Z is None else Z
+        H = torch.empty_like(X) if H is None and Y is not None else H
         stats = torch.empty((p.tokens, 4), dtype=torch.float32, device=dev) if stats is None else stats
         _check(lib.dsv_gated_norm_fwd(c, _row(c, "x", X, shape, td, dev), _row(c, "y", Y, shape, td, dev), _flat("cu", cu, (p.n_seg + 1,), torch.int32, dev),
                                       _row(c, "gate", gate, mod, td, dev), _row(c, "scale", scale, mod, td, dev), _row(c, "shift", shift, mod, td, dev),
@@ -857,8 +864,8 @@ def gated_norm_bwd(p: GatedNorm, X, cu, stats, dZ, Y=None, gate=None, scale=None
     lib = load_library()
     with _On(X, stream) as on:
         dev, td, c, shape, mod, f32 = X.device, p.torch_dtype, _CGatedNorm.from_buffer_copy(p._c), p.shape, p.mod_shape, torch.float32
-        dX = torch.empty(shape, dtype=td, device=dev) if dX is None else dX
-        dY = torch.empty(shape, dtype=td, device=dev) if dY is None and Y is not None else dY
+        dX = torch.empty_like(X) if dX is None else dX
+        dY = torch.empty_like(X) if dY is None and Y is not None else dY
         dgate = torch.empty(mod, dtype=f32, device=dev) if dgate is None and gate is not None else dgate
         if scale is not None:
             dscale = torch.empty(mod, dtype=f32, device=dev) if dscale is None else dscale
@@ -898,12 +905,10 @@ class Cache:
 
 def _cache_args(p: Cache, cu, lens, table, K8, V8, kscale, vscale, dev):
     """The pointers ahead of the pool's, and the pool's."""
-    def pool(what, t):
-        return _flat(what, t, p.pool_shape, t.dtype if t.dtype in (torch.float8_e4m3fn, torch.uint8) else torch.float8_e4m3fn, dev)
-
+    k, v = (torch.uint8 if t is not None and t.dtype is torch.uint8 else torch.float8_e4m3fn for t in (K8, V8))
     return ((_flat("cu", cu, (p.n_seq + 1,), torch.int32, dev), _flat("lens", lens, (p.n_seq,), torch.int32, dev),
              _flat("table", table, (p.n_seq, p.max_pages), torch.int32, dev)),
-            (pool("K8", K8), pool("V8", V8), _flat("kscale", kscale, p.scale_shape, torch.float32, dev), _flat("vscale", vscale, p.scale_shape, torch.float32, dev)))
+            (_flat("K8", K8, p.pool_shape, k, dev), _flat("V8", V8, p.pool_shape, v, dev), _flat("kscale", kscale, p.scale_shape, torch.float32, dev), _flat("vscale", vscale, p.scale_shape, torch.float32, dev)))
 
 
 def cache_append(p: Cache, K, V, cu, lens, table, K8, V8, kscale, vscale, rotary: Optional[Rotary] = None, pos=None, freq=None, stream=None):
