@@ -151,9 +151,10 @@ Walk walk_of(const dsv_cache &p)
         chunk = std::max(tiles * longest / 2048, std::min<int64_t>(512, std::max<int64_t>(256, tiles * longest / 512)));
     } else {
         // Two streams of 1560 queries against 21840 and 7800 keys, eight heads on two, d = 128, bf16, us with the join: two pieces 366, five 292, eight 256, twelve 251,
-        // sixteen 265.
+        // sixteen 265.  In pieces for 768, 1024, 1536 and 2048 blocks at most: that call 259, 284, 260, 266; 1045 and 63 queries against 8208 and 192, twelve heads
+        // on three: 103, 96, 104, 111; eight streams of 2 .. 915 against 32 .. 17860, d = 64: 44, 39, 34, 34.
         if (tiles >= 1024) return w;
-        chunk = std::max<int64_t>((longest * tiles + 2047) / 2048, 512);
+        chunk = std::max<int64_t>((longest * tiles + 1535) / 1536, 512);
     }
     chunk = (std::max(chunk, (longest + 63) / 64) + 127) / 128 * 128;
     w.chunk = chunk < longest ? (int)chunk : 0;

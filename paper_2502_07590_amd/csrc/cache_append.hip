@@ -77,22 +77,32 @@ template <> struct Raw<float> {
 
 enum TurnForm { kStraight, kEights, kAnyPairs };
 
-// Sixteen channels from c0 of a row whose pairs lie anywhere.
-template <typename T> __device__ __forceinline__ void turn_any(const TurnArgs &t, const T *x, int64_t token, int c0, float (&f)[8], float (&g)[8])
+// Sixteen channels from c0 on whose pairs lie anywhere: what each is multiplied by, and its other channel.
+__device__ __forceinline__ void any_turns(const TurnArgs &t, int64_t token, int c0, float2 (&by)[16])
 {
     int pos[3];
     read_position(t, token, pos);
-    for (int i = 0; i < t.total; ++i) {
-        int lo, hi;
-        pair_channels(t, i, lo, hi);
-        if ((lo < c0 || lo >= c0 + 16) && (hi < c0 || hi >= c0 + 16)) continue;
-        float u = to_f32(x[lo]), v = to_f32(x[hi]);
-        turn<false>(u, v, turn_of(t, pos, i));
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            f[c] = lo == c0 + c ? u : hi == c0 + c ? v : f[c];
-            g[c] = lo == c0 + 8 + c ? u : hi == c0 + 8 + c ? v : g[c];
-        }
+    for (int c = 0; c < 16; ++c) {
+        by[c] = make_float2(1.f, 0.f);
+        if (c0 + c >= 2 * t.total) continue;
+        int pair, other;
+        bool second;
+        pair_of(t, c0 + c, pair, second, other);
+        by[c] = turn_of(t, pos, pair);
+        if (!second) by[c].y = -by[c].y;
+    }
+}
+template <typename T> __device__ __forceinline__ void turn_any(const TurnArgs &t, const float2 (&by)[16], const T *x, int c0, float (&f)[8], float (&g)[8])
+{
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+        if (c0 + c >= 2 * t.total) continue;
+        int pair, other;
+        bool second;
+        pair_of(t, c0 + c, pair, second, other);
+        float &v = c < 8 ? f[c & 7] : g[c & 7];
+        v = v * by[c].x + to_f32(x[other]) * by[c].y;
     }
 }
 
@@ -106,6 +116,8 @@ __device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__re
     Sixteen six[N];
     int row[N];
     float2 t[FORM == kEights ? N : 1][8];
+    constexpr bool kHeld = FORM == kAnyPairs && N <= 2;  // the turns of all heads; more would take all registers
+    float2 any[kHeld ? N : 1][16];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         const int job = (int)threadIdx.x + j * (int)blockDim.x;
@@ -130,6 +142,11 @@ __device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__re
                 for (int i = 0; i < 8; ++i) t[j][i] = turn_of(turns, pos, six[j].pair + i);
             }
     }
+    if constexpr (kHeld) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (row[j] < count) any_turns(turns, token0 + row[j], six[j].first, any[j]);
+    }
     int flip = 0;
     for (int h = h0; h < a.Hkv; h += step) {
         float f[N][8], g[N][8], most = 0.f;
@@ -139,7 +156,10 @@ __device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__re
             raw[j].numbers(f[j], g[j]);
             if constexpr (FORM == kEights)
                 if (six[j].pair >= 0) turn_sixteen<false>(interleaved, t[j], f[j], g[j]);
-            if constexpr (FORM == kAnyPairs) turn_any(turns, src + (token0 + row[j]) * row_s + h * head_s, token0 + row[j], six[j].first, f[j], g[j]);
+            if constexpr (FORM == kAnyPairs) {
+                if constexpr (!kHeld) any_turns(turns, token0 + row[j], six[j].first, any[0]);
+                turn_any(turns, any[kHeld ? j : 0], src + (token0 + row[j]) * row_s + h * head_s, six[j].first, f[j], g[j]);
+            }
 #pragma unroll
             for (int c = 0; c < 8; ++c) {  // numbers alone: one infinity would leave nothing of the page's others
                 most = fabsf(f[j][c]) < __builtin_inff() ? fmaxf(most, fabsf(f[j][c])) : most;

@@ -1,5 +1,8 @@
 // Keys out of the pages of an 8-bit cache, for the forward of attention.  Values are widened with their page's scale by the conversion itself
 // (v_cvt_scalef32; exact, the scales being powers of two).  Pages begin on multiples of 16 tokens, so 16 keys in a row have one page.
+//
+// Values of 8 bits are bf16 ones, whatever the queries' type; fp32 queries and weights go into the products as three bf16 words, 24 bits, whose
+// products with them are exact in the 32-bit sums: three bf16 products where eight of fp32 would take five times as long.
 #pragma once
 
 #include "cache.h"
@@ -23,11 +26,69 @@ __device__ __forceinline__ bf16x8_t widen8(uint32_t lo, uint32_t hi, float s)
     return __builtin_bit_cast(bf16x8_t, make_uint4(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c),
                                                    __builtin_bit_cast(uint32_t, d)));
 }
-__device__ __forceinline__ floatx4_t widen4(uint32_t w, float s)
-{
-    const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, true);
-    return floatx4_t{a[0], a[1], b[0], b[1]};
-}
+
+// fp32 as bf16 words, the largest first; what is left behind the last is below 2^-24 of the whole.
+constexpr int words_of(int bytes) { return bytes == 4 ? 3 : 1; }
+template <typename T, int D> struct OwnRows;
+template <int D> struct OwnRows<bf16_t, D> {  // as they are
+    Frag<bf16_t> w[1][D / 16];
+    __device__ __forceinline__ void set(const Frag<bf16_t> (&q)[D / 16])
+    {
+#pragma unroll
+        for (int m = 0; m < D / 16; ++m) w[0][m] = q[m];
+    }
+};
+template <int D> struct OwnRows<float, D> {
+    Frag<bf16_t> w[3][D / 16];
+    __device__ __forceinline__ void set(const Frag<float> (&q)[D / 8])
+    {
+#pragma unroll
+        for (int m = 0; m < D / 16; ++m) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = q[2 * m + (i >> 2)].v[i & 3];
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                uint32_t p[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    p[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+                    x[2 * i] -= __uint_as_float(p[i] << 16);
+                    x[2 * i + 1] -= __uint_as_float(p[i] & 0xFFFF0000u);
+                }
+                w[k][m].v = __builtin_bit_cast(bf16x8_t, make_uint4(p[0], p[1], p[2], p[3]));
+            }
+        }
+    }
+};
+template <typename T> struct WeightWords;
+template <> struct WeightWords<bf16_t> {
+    Weights<bf16_t> w[1];
+    __device__ __forceinline__ explicit WeightWords(const Weights<bf16_t> &x) { w[0] = x; }
+};
+template <> struct WeightWords<float> {
+    Weights<bf16_t> w[3];
+    __device__ __forceinline__ explicit WeightWords(const Weights<float> &x)
+    {
+        floatx16_t r = x.v;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            w[k].set(r);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const uint4 h = __builtin_bit_cast(uint4, w[k].v[s]);
+                const uint32_t p[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    r[8 * s + 2 * i] -= __uint_as_float(p[i] << 16);
+                    r[8 * s + 2 * i + 1] -= __uint_as_float(p[i] & 0xFFFF0000u);
+                }
+            }
+        }
+    }
+};
+// Which 16 bytes of Q hold channels c .. of step m: bf16 eight of them, fp32 four, two such to a step of eight.
+template <typename T> __device__ __forceinline__ int piece_of(int channel, int m) { return sizeof(T) == 2 ? channel / 8 : channel / 4 + (m & 1); }
 
 // Transposing LDS read of bytes (ds_read_b64_tr_b8): inside every block of 16 lanes, lane i receives eight bytes, the e-th being byte i % 8 at the
 // address passed by lane 2 e + i / 8 of the block.
@@ -37,10 +98,10 @@ typedef __attribute__((address_space(3))) s32x2_t lds_s32x2_t;
 // For blocks of 32 rows whose four waves share the keys: every wave reads 32 keys of its own, K straight into the products' registers, V by way of
 // LDS of its own, turned there; no wave waits for another.  The next 32 keys' bytes, and the pages of those after them, are on their way meanwhile.
 template <typename T, int D> struct PageWaves {
-    typedef FwdShape<T, D, 4> Sh;
-    static constexpr int NK = D / 32;                  // 16-byte pieces of a key to a lane: the pieces 2 j + half
+    typedef FwdShape<bf16_t, D, 4> Sh;
+    static constexpr int NK = D / 32;                  // 16-byte pieces of a key to a lane: the pieces 2 j + half, two steps of the products each
     static constexpr int PPR = D / 16, RPL = 64 / PPR; // pieces of a key, keys of a load of V
-    static constexpr int SUB = (int)sizeof(T);         // products' steps to such a piece
+    static constexpr int WORDS = words_of(sizeof(T));
     struct Step {
         uint4 k[NK], v[NK];
         float ks, vs[2];
@@ -50,11 +111,17 @@ template <typename T, int D> struct PageWaves {
     const int32_t *pages;
     unsigned char *vt;
     int hk, wave, last_page, nk, pg[2];
+    OwnRows<T, D> own;
 
     __device__ __forceinline__ explicit PageWaves(const CachedArgs &args) : a(args) {}
-    __device__ __forceinline__ static int piece(int m, int half) { return (2 * (m / SUB) + half) * SUB + m % SUB; }
-    __device__ __forceinline__ void begin(const CachedArgs &, int si, const Sequence &sq, int hk_, int wave_)
+    __device__ __forceinline__ static int piece(int m, int half)
     {
+        const int step = sizeof(T) == 2 ? m : m / 2;
+        return piece_of<T>(16 * (2 * (step / 2) + half) + 8 * (step & 1), m);
+    }
+    __device__ __forceinline__ void begin(const CachedArgs &, int si, const Sequence &sq, int hk_, int wave_, const Frag<T> (&q)[D * sizeof(T) / 32])
+    {
+        own.set(q);
         hk = hk_;
         wave = wave_;
         nk = sq.nk;
@@ -88,40 +155,33 @@ template <typename T, int D> struct PageWaves {
     }
     // V's rows in LDS: piece p at place p ^ turn(r), so that the 16 rows of a transposing read lie over all banks
     __device__ __forceinline__ static int at(int r, int p) { return r * D + ((p ^ (D == 128 ? 2 * ((r >> 1) & 3) : 2 * ((r >> 2) & 1))) << 4); }
-    __device__ __forceinline__ void scores(const Step &st, int, const Frag<T> (&own)[D * sizeof(T) / 32], floatx16_t (&s)[1]) const
+    __device__ __forceinline__ void scores(const Step &st, int, const Frag<T> (&)[D * sizeof(T) / 32], floatx16_t (&s)[1]) const
     {
         s[0] = zero16();
 #pragma unroll
         for (int j = 0; j < NK; ++j) {
             const uint32_t w[4] = {st.k[j].x, st.k[j].y, st.k[j].z, st.k[j].w};
 #pragma unroll
-            for (int i = 0; i < SUB; ++i) {
-                Frag<T> f;
-                if constexpr (sizeof(T) == 2) f.v = widen8(w[2 * i], w[2 * i + 1], st.ks);
-                else f.v = widen4(w[i], st.ks);
-                s[0] = product(f, own[j * SUB + i], s[0]);
+            for (int i = 0; i < 2; ++i) {
+                const Frag<bf16_t> f{widen8(w[2 * i], w[2 * i + 1], st.ks)};
+#pragma unroll
+                for (int k = WORDS - 1; k >= 0; --k) s[0] = product(f, own.w[k][2 * j + i], s[0]);
             }
         }
     }
-    __device__ __forceinline__ void add(const Step &st, int, const Weights<T> &w, floatx16_t (&acc)[D / 32]) const
+    __device__ __forceinline__ void add(const Step &st, int, const Weights<T> &weights, floatx16_t (&acc)[D / 32]) const
     {
         const int lane = threadIdx.x & 63, e = (lane >> 1) & 7, half = lane >> 5;
         const int r = (e < 4 ? e : 4 + e) + 4 * half, p = (lane >> 4) & 1, sub = (lane & 1) * 8;
+        const WeightWords<T> w(weights);
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
             for (int nb = 0; nb < D / 32; ++nb) {
                 const s32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_s32x2_t *)(vt + at(16 * g + r, 2 * nb + p) + sub));
-                if constexpr (sizeof(T) == 2) {
-                    acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8((uint32_t)x[0], (uint32_t)x[1], st.vs[g]), w.v[g], acc[nb], 0, 0, 0);
-                } else {
+                const bf16x8_t v = widen8((uint32_t)x[0], (uint32_t)x[1], st.vs[g]);
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const floatx4_t f = widen4((uint32_t)x[q], st.vs[g]);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(f[i], w.v[8 * g + 4 * q + i], acc[nb], 0, 0, 0);
-                    }
-                }
+                for (int k = WORDS - 1; k >= 0; --k) acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w.w[k].v[g], acc[nb], 0, 0, 0);
             }
     }
     template <typename Scores, typename Rest>
@@ -165,8 +225,9 @@ template <typename T, int D> struct PageWaves {
 // into LDS, as rows loaded directly would be, between the products of this one's scores.  A load of a wave is one kilobyte of one page, so its page
 // and scales are the wave's.
 template <typename T, int D> struct PageTiles {
-    typedef FwdShape<T, D, 1> Sh;
-    typedef RowTile<T, D> RT;
+    typedef FwdShape<bf16_t, D, 1> Sh;
+    typedef RowTile<bf16_t, D> RT;
+    static constexpr int WORDS = words_of(sizeof(T));
     static constexpr int RPL = 1024 / D, PPR = D / 16;     // tokens of a load, 16-byte pieces of a token
     static constexpr int N = Sh::KEYS / RPL / 4;           // loads of a wave for a tile of K, and of V
     const CachedArgs &a;
@@ -178,11 +239,13 @@ template <typename T, int D> struct PageTiles {
     uint32_t of_lane;
     unsigned char *next_k, *next_v;
     bool more;
+    OwnRows<T, D> own;
 
     __device__ __forceinline__ explicit PageTiles(const CachedArgs &args) : a(args) {}
-    __device__ __forceinline__ static int piece(int m, int half) { return 2 * m + half; }
-    __device__ __forceinline__ void begin(const CachedArgs &, int si, const Sequence &sq, int hk_, int wave_)
+    __device__ __forceinline__ static int piece(int m, int half) { return piece_of<T>(8 * (2 * (sizeof(T) == 2 ? m : m / 2) + half), m); }
+    __device__ __forceinline__ void begin(const CachedArgs &, int si, const Sequence &sq, int hk_, int wave_, const Frag<T> (&q)[D * sizeof(T) / 32])
     {
+        own.set(q);
         hk = hk_;
         wave = wave_;
         nk = sq.nk;
@@ -228,25 +291,18 @@ template <typename T, int D> struct PageTiles {
         uint4 w = raw[j];
         const float s = scale[j];
         if (at0 + Sh::KEYS > nk && at0 + r >= nk) w = make_uint4(0, 0, 0, 0);
-        if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<bf16x8_t *>(tile + RT::at(r, piece_no)) = widen8(w.x, w.y, s);
-            *reinterpret_cast<bf16x8_t *>(tile + RT::at(r, PPR + piece_no)) = widen8(w.z, w.w, s);
-        } else {
-            *reinterpret_cast<floatx4_t *>(tile + RT::at(r, 2 * piece_no)) = widen4(w.x, s);
-            *reinterpret_cast<floatx4_t *>(tile + RT::at(r, 2 * piece_no + 1)) = widen4(w.y, s);
-            *reinterpret_cast<floatx4_t *>(tile + RT::at(r, 2 * (PPR + piece_no))) = widen4(w.z, s);
-            *reinterpret_cast<floatx4_t *>(tile + RT::at(r, 2 * (PPR + piece_no) + 1)) = widen4(w.w, s);
-        }
+        *reinterpret_cast<bf16x8_t *>(tile + RT::at(r, piece_no)) = widen8(w.x, w.y, s);
+        *reinterpret_cast<bf16x8_t *>(tile + RT::at(r, PPR + piece_no)) = widen8(w.z, w.w, s);
     }
     // as tile_scores(), the next tile's puts between the steps
-    __device__ __forceinline__ void scores(const unsigned char *kt, int r, const Frag<T> (&own)[D * sizeof(T) / 32], floatx16_t (&s)[Sh::KT])
+    __device__ __forceinline__ void scores(const unsigned char *kt, int r, const Frag<T> (&)[D * sizeof(T) / 32], floatx16_t (&s)[Sh::KT])
     {
-        constexpr int NM = D * (int)sizeof(T) / 32;
+        constexpr int NM = D / 16;
         const int half = (threadIdx.x & 63) >> 5;
-        Frag<T> f[kAhead][Sh::KT];
+        Frag<bf16_t> f[kAhead][Sh::KT];
         auto fetch = [&](int m) __attribute__((always_inline)) {
 #pragma unroll
-            for (int t = 0; t < Sh::KT; ++t) f[m % kAhead][t] = row_frag<T, D>(kt, r + 32 * t, m, half);
+            for (int t = 0; t < Sh::KT; ++t) f[m % kAhead][t] = row_frag<bf16_t, D>(kt, r + 32 * t, m, half);
         };
 #pragma unroll
         for (int t = 0; t < Sh::KT; ++t) s[t] = zero16();
@@ -256,13 +312,31 @@ template <typename T, int D> struct PageTiles {
 #pragma unroll
         for (int m = 0; m < NM; ++m) {
 #pragma unroll
-            for (int t = 0; t < Sh::KT; ++t) s[t] = product(f[m % kAhead][t], own[m], s[t]);
+            for (int k = WORDS - 1; k >= 0; --k)
+#pragma unroll
+                for (int t = 0; t < Sh::KT; ++t) s[t] = product(f[m % kAhead][t], own.w[k][m], s[t]);
             if (m + kAhead < NM) fetch(m + kAhead);
             if (m % 2 == 1 && m / 2 < 2 * N && more) put(m / 2);
             pin_order();
         }
     }
-    __device__ __forceinline__ void add(const unsigned char *vt, int r0, const Weights<T> &w, floatx16_t (&acc)[D / 32]) const { weighted_rows<T, D>(vt, r0, w, acc); }
+    // as weighted_rows(), every operand for all words of the weights
+    __device__ __forceinline__ void add(const unsigned char *vt, int r0, const Weights<T> &weights, floatx16_t (&acc)[D / 32]) const
+    {
+        typedef RowSum<bf16_t, D> RS;
+        const WeightWords<T> w(weights);
+        typename RS::Operand f[RS::AHEAD];
+#pragma unroll
+        for (int i = 0; i < RS::AHEAD; ++i) f[i] = RS::fetch(vt, r0, i);
+        pin_order();
+#pragma unroll
+        for (int i = 0; i < RS::STEPS; ++i) {
+#pragma unroll
+            for (int k = WORDS - 1; k >= 0; --k) RS::step(i, f[i % RS::AHEAD], w.w[k], acc);
+            if (i + RS::AHEAD < RS::STEPS) f[i % RS::AHEAD] = RS::fetch(vt, r0, i + RS::AHEAD);
+            pin_order();
+        }
+    }
     template <typename Scores, typename Rest>
     __device__ __forceinline__ void walk(const CachedArgs &, int kbeg, int kend, unsigned char *ka, unsigned char *va, unsigned char *kb, unsigned char *vb, Scores scores,
                                          Rest rest)

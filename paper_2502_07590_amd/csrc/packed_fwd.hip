@@ -28,7 +28,7 @@ template <typename T, int D, int WK> struct RowTiles {
     __device__ __forceinline__ static int piece(int m, int half) { return 2 * m + half; }
     __device__ __forceinline__ void scores(const unsigned char *kt, int r, const Frag<T> (&own)[D * sizeof(T) / 32], floatx16_t (&s)[Sh::KT]) const { tile_scores<T, D, Sh::KT>(kt, r, own, s); }
     __device__ __forceinline__ void add(const unsigned char *vt, int r0, const Weights<T> &w, floatx16_t (&acc)[D / 32]) const { weighted_rows<T, D>(vt, r0, w, acc); }
-    __device__ __forceinline__ void begin(const PackedArgs &a, int, const Sequence &sq, int hk, int wave)
+    __device__ __forceinline__ void begin(const PackedArgs &a, int, const Sequence &sq, int hk, int wave, const Frag<T> (&)[D * sizeof(T) / 32])
     {
         kp = reinterpret_cast<const unsigned char *>(K) + (int64_t)sq.k0 * a.k_row + (int64_t)hk * a.k_head;
         vp = reinterpret_cast<const unsigned char *>(V) + (int64_t)sq.k0 * a.v_row + (int64_t)hk * a.v_head;
@@ -83,7 +83,7 @@ __device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? k
 
 // A: the descriptor, with read_sequence() of its own.  Tiles: brings tiles of keys into LDS,
 //   piece(m, half): which 16 bytes of Q a half of the wave holds for step m of the scores
-//   begin(a, sequence's number, sequence, head of K and V, wave)
+//   begin(a, sequence's number, sequence, head of K and V, wave, own rows)
 //   walk(a, first key, key behind the last, two tiles of K and V each (for NBUF = 1 the second two are not there), scores(K tile, s), rest(key, s, V tile)),
 //   which come back as scores(K tile, row, own rows, s) and add(V tile, first row, weights, sums)
 template <typename T, int D, int WK, typename A, typename Tiles>
@@ -91,7 +91,7 @@ __device__ __forceinline__ void attend(const T *__restrict__ Q, T *__restrict__ 
                                        float *__restrict__ pacc, const A &a, Tiles tiles)
 {
     typedef RowTile<T, D> RT;
-    typedef FwdShape<T, D, WK> Sh;
+    typedef typename Tiles::Sh Sh;
     constexpr int NM = RT::RB / 32, NB = D / 32, KT = Sh::KT;
     // every tile an array of its own: reads of one then need not wait for the loads into another
     __shared__ __align__(1024) unsigned char ka[Sh::TILE], va[Sh::TILE], kb[Sh::NBUF == 2 ? Sh::TILE : 16], vb[Sh::NBUF == 2 ? Sh::TILE : 16];
@@ -121,7 +121,7 @@ __device__ __forceinline__ void attend(const T *__restrict__ Q, T *__restrict__ 
 #pragma unroll
         for (int m = 0; m < NM; ++m) qf[m] = *reinterpret_cast<const Frag<T> *>(qp + Tiles::piece(m, half) * 16);
     }
-    tiles.begin(a, si, sq, hk, wave);
+    tiles.begin(a, si, sq, hk, wave, qf);
 
     const float c = a.scale * kLog2e;
     floatx16_t acc[NB];
@@ -245,8 +245,9 @@ __device__ __forceinline__ void attend(const T *__restrict__ Q, T *__restrict__ 
         } else {
             // the wave's rows by way of LDS, so that they leave as whole lines
             typedef RowTile<T, D> RT;
-            unsigned char *const mine = (wave < 2 ? ka : va) + (wave & 1) * (Sh::TILE / 2);
-            static_assert(Sh::TILE / 2 == 32 * RT::RB, "half a tile is a wave's rows");
+            constexpr bool kHalf = Sh::TILE / 2 == 32 * RT::RB;
+            unsigned char *const mine = kHalf ? (wave < 2 ? ka : va) + (wave & 1) * (Sh::TILE / 2) : wave == 0 ? ka : wave == 1 ? va : wave == 2 ? kb : vb;
+            static_assert(kHalf || (Sh::NBUF == 2 && Sh::TILE == 32 * RT::RB), "half a tile is a wave's rows, or a whole one of keys narrower than they");
             auto place = [&](int r, int p) __attribute__((always_inline)) { return mine + r * RT::RB + ((p ^ (RT::PIECES == 8 ? (r >> 1) & 7 : r & 15)) << 4); };
             auto send = [&](unsigned char *first, int64_t row_b, int64_t head_b) __attribute__((always_inline)) {
 #pragma unroll
@@ -372,7 +373,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2
 }
 
 template <typename T, int D, int WK>
-__global__ __launch_bounds__(256, sizeof(T) == 4 && (D == 128 || WK > 1) ? 1 : 2) void cache_fwd_kernel(const T *__restrict__ Q, T *__restrict__ O, float *__restrict__ lse,
+__global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void cache_fwd_kernel(const T *__restrict__ Q, T *__restrict__ O, float *__restrict__ lse,
                                                                                        float2 *__restrict__ pml, float *__restrict__ pacc, CachedArgs a)
 {
     if constexpr (WK == 1) attend<T, D, WK>(Q, O, nullptr, lse, pml, pacc, a, PageTiles<T, D>(a));
@@ -394,7 +395,7 @@ dsv_status launch_t(const PackedArgs &a, const void *Q, const void *K, const voi
 }
 template <typename T, int D, int WK> dsv_status launch_cached_t(const CachedArgs &a, const void *Q, void *O, float *lse, char *ws, hipStream_t st)
 {
-    const int64_t slots = tile_slots(a.total_q, a.group, FwdShape<T, D, WK>::ROWS, a.n_seq);
+    const int64_t slots = tile_slots(a.total_q, a.group, FwdShape<bf16_t, D, WK>::ROWS, a.n_seq);
     float *const pacc = reinterpret_cast<float *>(ws);
     float2 *const pml = reinterpret_cast<float2 *>(ws + packed_fwd_acc_bytes(a.total_q, a.Hq, D, a.splits));
     cache_fwd_kernel<T, D, WK><<<dim3((unsigned)(slots * a.Hkv), a.splits), 256, 0, st>>>(static_cast<const T *>(Q), static_cast<T *>(O), lse, pml, pacc, a);

@@ -49,6 +49,26 @@ __device__ __forceinline__ void pair_channels(const TurnArgs &a, int i, int &lo,
     }
 }
 
+// The other way round: the pair of channel c, whether c is its second, and its other channel.  c is one of those that are turned.
+__device__ __forceinline__ void pair_of(const TurnArgs &a, int c, int &pair, bool &second, int &other)
+{
+    if (a.layout == DSV_TURN_INTERLEAVED) {
+        pair = c >> 1;
+        second = c & 1;
+        other = c ^ 1;
+        return;
+    }
+    int begin = 0, end = a.total;
+    if (a.layout == DSV_TURN_AXIS_HALVES) {
+        begin = c < 2 * a.end0 ? 0 : c < 2 * a.end1 ? a.end0 : a.end1;
+        end = c < 2 * a.end0 ? a.end0 : c < 2 * a.end1 ? a.end1 : a.total;
+    }
+    const int n = end - begin;
+    second = c - 2 * begin >= n;
+    pair = c - begin - (second ? n : 0);
+    other = second ? c - n : c + n;
+}
+
 // Sixteen channels of a row: two times eight side by side, in eight pairs (2 i, 2 i + 1 of them, or i and 8 + i) or in none.
 struct Sixteen {
     int first, second;  // channels
