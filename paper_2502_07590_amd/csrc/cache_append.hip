@@ -108,7 +108,7 @@ template <typename T> __device__ __forceinline__ void turn_any(const TurnArgs &t
 
 // One tensor's new rows of one page, for heads h0, h0 + step, ...: the next head's loads are under way while one is rounded.
 template <typename T, int D, int N, TurnForm FORM>
-__device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__restrict__ src, int64_t row_s, int64_t head_s, uint8_t *__restrict__ pool, float *__restrict__ scales,
+__device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__restrict__ src, int64_t row_s, int64_t head_s, uint8_t *pool, float *scales,
                                             const CacheArgs &a, int pg, int64_t token0, int begun, int count, int h0, int step, float (&red)[2][4])
 {
     constexpr int PER = D / 16;
@@ -155,7 +155,7 @@ __device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__re
             if (row[j] >= count) continue;
             raw[j].numbers(f[j], g[j]);
             if constexpr (FORM == kEights)
-                if (six[j].pair >= 0) turn_sixteen<false>(interleaved, t[j], f[j], g[j]);
+                if (six[j].pair >= 0) turn_sixteen<false>(interleaved, turns.total - six[j].pair, t[j], f[j], g[j]);
             if constexpr (FORM == kAnyPairs) {
                 if constexpr (!kHeld) any_turns(turns, token0 + row[j], six[j].first, any[0]);
                 turn_any(turns, any[kHeld ? j : 0], src + (token0 + row[j]) * row_s + h * head_s, six[j].first, f[j], g[j]);
@@ -205,8 +205,7 @@ __device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__re
 
 // blockIdx: x a page that some sequence may touch, y the first head (others gridDim.y further), z K or V.  N: sixteens of a page a lane.
 template <typename T, int D, int N, TurnForm FORM>
-__global__ __launch_bounds__(256) void cache_append_kernel(AppendIn in, uint8_t *__restrict__ K8, uint8_t *__restrict__ V8, float *__restrict__ kscale,
-                                                           float *__restrict__ vscale, CacheArgs a)
+__global__ __launch_bounds__(256) void cache_append_kernel(AppendIn in, uint8_t *K8, uint8_t *V8, float *kscale, float *vscale, CacheArgs a)
 {
     __shared__ float red[2][4];
     const int si = __builtin_amdgcn_readfirstlane(find_sequence(a.cu, a.n_seq, a.total, 1, a.page, (int)blockIdx.x, page_gap(a)));

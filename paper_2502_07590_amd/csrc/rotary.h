@@ -15,11 +15,11 @@ struct TurnArgs {
     float gain;
 };
 
-// (cos, sin) of pair i's angle at a token, times the gain; (1, 0) past the last pair.  The product is formed and brought within half a turn in 64 bits: in
+// (cos, sin) of pair i's angle at a token, times the gain.  The product is formed and brought within half a turn in 64 bits: in
 // 32, an angle of 10^6 radians is off by 0.06.
 __device__ __forceinline__ float2 turn_of(const TurnArgs &a, const int (&pos)[3], int i)
 {
-    if (i >= a.total) return make_float2(1.f, 0.f);
+    if (i >= a.total) return make_float2(0.f, 0.f);  // none: not read
     const int p = i < a.end0 ? pos[0] : i < a.end1 ? pos[1] : pos[2];
     double t = (double)p * a.freq[i] * 0.15915494309189535;
     t -= rint(t);
@@ -119,13 +119,14 @@ template <bool BACK> __device__ __forceinline__ void turn(float &x, float &y, fl
     x = a * t.x - b * s;
     y = a * s + b * t.x;
 }
-template <bool BACK> __device__ __forceinline__ void turn_sixteen(bool interleaved, const float2 (&t)[8], float (&f)[8], float (&g)[8])
+// left: how many of the eight are there; the others' channels stay as they are, bit for bit
+template <bool BACK> __device__ __forceinline__ void turn_sixteen(bool interleaved, int left, const float2 (&t)[8], float (&f)[8], float (&g)[8])
 {
     if (interleaved) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            turn<BACK>(f[2 * i], f[2 * i + 1], t[i]);
-            turn<BACK>(g[2 * i], g[2 * i + 1], t[4 + i]);
+            if (i < left) turn<BACK>(f[2 * i], f[2 * i + 1], t[i]);
+            if (4 + i < left) turn<BACK>(g[2 * i], g[2 * i + 1], t[4 + i]);
         }
     } else {
 #pragma unroll

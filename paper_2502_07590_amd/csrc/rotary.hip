@@ -42,7 +42,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const T *X, T *Y, RotaryArg
         float f[8], g[8];
         load8(x + k * a.x_head + s.first, f);
         load8(x + k * a.x_head + s.second, g);
-        if (s.pair >= 0) turn_sixteen<BACK>(a.t.layout == DSV_TURN_INTERLEAVED, t, f, g);
+        if (s.pair >= 0) turn_sixteen<BACK>(a.t.layout == DSV_TURN_INTERLEAVED, a.t.total - s.pair, t, f, g);
         store8(y + k * a.y_head + s.first, f);
         store8(y + k * a.y_head + s.second, g);
     }

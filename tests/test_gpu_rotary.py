@@ -104,6 +104,24 @@ def test_in_place_in_a_fused_projection_and_nothing_beside(pairs, pattern):
     assert (qkv - old).abs().max() < 64 * 2.0 ** -24 * float(old.abs().max())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pattern", LAYOUTS)
+@pytest.mark.parametrize("pairs", [[3], [11], [8], [40, 5]])
+def test_channels_that_are_not_turned_are_copied_bit_for_bit(pairs, pattern, dtype):
+    """Zeros of both signs, infinities and NaN in them, also next to pairs that are turned and in the same 16 bytes."""
+    X, _, pos = inputs(20, 3, 128, len(pairs), dtype)
+    rot = 2 * sum(pairs)
+    odd = torch.tensor([-0.0, 0.0, math.inf, -math.inf, math.nan, 1e-40, 3e38], dtype=X.dtype)
+    X[..., rot:] = odd[torch.arange(128 - rot) % len(odd)]
+    p = dsv.Rotary(20, 3, 128, dtype, pairs, layout=pattern, gain=1.25)
+    freq = ref.freqs(pairs)
+    Y = dsv.rotary_fwd(p, X.to(DEV), pos.to(DEV), freq.to(DEV)).cpu()
+    whole = torch.int16 if dtype == "bf16" else torch.int32
+    assert torch.equal(Y[..., rot:].contiguous().view(whole), X[..., rot:].contiguous().view(whole))
+    value, bound = ref.rotary(X.double(), pos, freq, pairs, pattern, 1.25, dtype=dtype)
+    packed_ref.assert_within("Y", Y[..., :rot], (value[..., :rot], bound[..., :rot]))
+
+
 def test_streams_graphs_and_no_tokens():
     T, H, d = 500, 8, 128
     X, dY, pos = inputs(T, H, d, 3, "bf16")
