@@ -14,6 +14,7 @@ namespace {
 
 constexpr int kLeastExp = -117;  // 2^-9 of it, the least e4m3 value, is a normal fp32 number still
 constexpr int kMostExp = 119;    // 448 of it is finite
+constexpr float kLargest = 0x1p119f;
 
 // The least power of two s with most <= 448 s = 1.75 * 2^8 s, by its bits.
 __device__ __forceinline__ float scale_of(float most)
@@ -27,16 +28,17 @@ __device__ __forceinline__ float scale_of(float most)
 __host__ __device__ __forceinline__ int page_gap(const CacheArgs &a) { return a.max_new == 1 ? 1 : 2; }
 __host__ __forceinline__ int64_t page_slots(const CacheArgs &a) { return a.total / a.page + (int64_t)a.n_seq * page_gap(a); }
 
-// Four values to e4m3, rounded to nearest even; beyond 448 (only past the largest scale) to 448, infinities to NaN as NaN is.
-__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d)
+// Four values to e4m3, rounded to nearest even; infinities become NaN, as NaN is.  CUT: beyond 448 (only past the largest scale) 448, where the conversion
+// itself would make it NaN.
+template <bool CUT = false> __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d)
 {
-    auto fit = [](float x) { return fabsf(x) < __builtin_inff() ? fminf(fmaxf(x, -448.f), 448.f) : __builtin_nanf(""); };
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(fit(a), fit(b), 0, false);
+    auto fit = [](float x) { return CUT && fabsf(x) < __builtin_inff() ? fminf(fmaxf(x, -448.f), 448.f) : x; };
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(fit(a), fit(b), 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fit(c), fit(d), w, true);
 }
-__device__ __forceinline__ uint2 pack8(const float (&f)[8], float by)
+template <bool CUT> __device__ __forceinline__ uint2 pack8(const float (&f)[8], float by)
 {
-    return make_uint2(pack_e4m3(f[0] * by, f[1] * by, f[2] * by, f[3] * by), pack_e4m3(f[4] * by, f[5] * by, f[6] * by, f[7] * by));
+    return make_uint2(pack_e4m3<CUT>(f[0] * by, f[1] * by, f[2] * by, f[3] * by), pack_e4m3<CUT>(f[4] * by, f[5] * by, f[6] * by, f[7] * by));
 }
 __device__ __forceinline__ uint32_t rescale4(uint32_t w, float by)
 {
@@ -161,21 +163,35 @@ __device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__re
                 turn_any(turns, any[kHeld ? j : 0], src + (token0 + row[j]) * row_s + h * head_s, six[j].first, f[j], g[j]);
             }
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {  // numbers alone: one infinity would leave nothing of the page's others
-                most = fabsf(f[j][c]) < __builtin_inff() ? fmaxf(most, fabsf(f[j][c])) : most;
-                most = fabsf(g[j][c]) < __builtin_inff() ? fmaxf(most, fabsf(g[j][c])) : most;
-            }
+            for (int c = 0; c < 8; ++c) most = fmaxf(most, fmaxf(fabsf(f[j][c]), fabsf(g[j][c])));  // of the numbers: fmaxf passes over NaN
         }
         if (h + step < a.Hkv) load(h + step);
         const int64_t at = (int64_t)pg * a.Hkv + h;
         const float held = begun > 0 ? scales[at] : 0.f;
+        auto of_block = [&](float x) __attribute__((always_inline)) {
 #pragma unroll
-        for (int s = 32; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
-        if (blockDim.x > 64) {
-            if ((threadIdx.x & 63) == 0) red[flip][threadIdx.x >> 6] = most;
-            __syncthreads();
-            for (int w = 0; w < (int)blockDim.x / 64; ++w) most = fmaxf(most, red[flip][w]);
-            flip ^= 1;
+            for (int s = 32; s > 0; s >>= 1) x = fmaxf(x, __shfl_xor(x, s));
+            if (blockDim.x > 64) {
+                if ((threadIdx.x & 63) == 0) red[flip][threadIdx.x >> 6] = x;
+                __syncthreads();
+                for (int w = 0; w < (int)blockDim.x / 64; ++w) x = fmaxf(x, red[flip][w]);
+                flip ^= 1;
+            }
+            return x;
+        };
+        most = of_block(most);
+        if (most == __builtin_inff()) {  // one infinity would leave nothing of the page's others: the largest of those (all lanes come here, or none)
+            float rest = 0.f;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                if (row[j] >= count) continue;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    rest = fabsf(f[j][c]) < __builtin_inff() ? fmaxf(rest, fabsf(f[j][c])) : rest;
+                    rest = fabsf(g[j][c]) < __builtin_inff() ? fmaxf(rest, fabsf(g[j][c])) : rest;
+                }
+            }
+            most = of_block(rest);
         }
         const float s = fmaxf(held, scale_of(most)), inv = 1.f / s;  // exact: a power of two
         uint8_t *const to = pool + at * a.page * D;
@@ -187,18 +203,22 @@ __device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__re
                 reinterpret_cast<uint4 *>(to)[i] = w;
             }
         }
+        auto write = [&](auto cut) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            if (row[j] >= count) continue;
-            uint8_t *const y = to + (begun + row[j]) * D;
-            if (!interleaved && FORM == kEights) {
-                *reinterpret_cast<uint2 *>(y + six[j].first) = pack8(f[j], inv);
-                *reinterpret_cast<uint2 *>(y + six[j].second) = pack8(g[j], inv);
-            } else {  // side by side
-                const uint2 lo = pack8(f[j], inv), hi = pack8(g[j], inv);
-                *reinterpret_cast<uint4 *>(y + six[j].first) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            for (int j = 0; j < N; ++j) {
+                if (row[j] >= count) continue;
+                uint8_t *const y = to + (begun + row[j]) * D;
+                const uint2 lo = pack8<decltype(cut)::value>(f[j], inv), hi = pack8<decltype(cut)::value>(g[j], inv);
+                if (!interleaved && FORM == kEights) {
+                    *reinterpret_cast<uint2 *>(y + six[j].first) = lo;
+                    *reinterpret_cast<uint2 *>(y + six[j].second) = hi;
+                } else {  // side by side
+                    *reinterpret_cast<uint4 *>(y + six[j].first) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+                }
             }
-        }
+        };
+        if (s < kLargest) write(std::false_type{});
+        else write(std::true_type{});
         if (threadIdx.x == 0) scales[at] = s;
     }
 }
