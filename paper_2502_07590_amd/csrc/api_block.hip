@@ -148,7 +148,11 @@ Walk walk_of(const dsv_cache &p)
     if (w.few) {
         // Bound by memory.  Twelve caches of up to 16001, four heads, group 4, d = 128, us without the join: pieces of 256 keys 23.6, 384 21.1, 512 19.9, 768
         // 18.9; 64 caches of 2047 .. 19900, two heads, group 7: 640 keys 84, 1280 80, 2560 89; five of up to 1023 in fp32, two heads: 256 10, 512 15.
-        chunk = std::max(tiles * longest / 2048, std::min<int64_t>(512, std::max<int64_t>(256, tiles * longest / 512)));
+        // Short caches go in one piece: a join costs as much as six more steps of a wave, and its launch and workspace on the host besides.  Eight caches of up to 400,
+        // 800 and 1000 keys, four heads, group 4, d = 128, us captured into a graph: 10.3, 10.9, 10.7 in pieces, 9.0, 11.9, 13.1 in one, and by
+        // itself 22 and 17; fp32, four caches of 1000, two heads, d = 64: 9.6 and 12.2, d = 128: 12.7 and 19.8 (500: 12.5 and 13.0).
+        if (longest <= (p.dtype == DSV_F32 && p.d == 128 ? 512 : 1024)) chunk = longest;
+        else chunk = std::max(tiles * longest / 2048, std::min<int64_t>(512, std::max<int64_t>(256, tiles * longest / 512)));
     } else {
         // Two streams of 1560 queries against 21840 and 7800 keys, eight heads on two, d = 128, bf16, us with the join: two pieces 366, five 292, eight 256, twelve 251,
         // sixteen 265.  In pieces for 768, 1024, 1536 and 2048 blocks at most: that call 259, 284, 260, 266; 1045 and 63 queries against 8208 and 192, twelve heads
