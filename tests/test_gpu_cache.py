@@ -1,6 +1,7 @@
 """The 8-bit cache on the GPU: what an append leaves in it, value by value, and attention over it against 64 bits; odd lengths, pages that end inside a tile, pools
 full of NaN where nothing was written, and both together as a sampler runs them."""
 import math
+import random
 
 import pytest
 import torch
@@ -66,6 +67,25 @@ def test_append_pages(d, page, dtype):
 def test_append_turned(pairs, pattern, dtype):
     check_append([40, 3], [5, 0], 2, 64, 32, dtype, pairs=pairs, pattern=pattern)
     check_append([90, 1], [100, 63], 5, 128, 64, dtype, pairs=pairs, pattern=pattern)
+
+
+def test_append_of_many_sequences():
+    """More than one step of the search for a page's sequence, most of them without a token."""
+    g = torch.Generator().manual_seed(9)
+    new = (torch.rand(5000, generator=g) < 0.05).long().tolist()
+    check_append(new, torch.randint(0, 40, (5000,), generator=g).tolist(), 1, 64, 16, "bf16", pairs=[32])
+    check_append([3 * x for x in new[:700]], torch.randint(0, 40, (700,), generator=g).tolist(), 1, 64, 16, "f32")
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_append_of_any_shape(seed):
+    r = random.Random(seed)
+    d, n = r.choice([64, 128]), r.choice([1, 2, 5, 9])
+    page, pairs = r.choice([16, 32, 64, 128, 256]), [r.randint(1, d // 6) for _ in range(r.randint(1, 3))]
+    new = [r.choice([0, 1, r.randint(1, 400)]) for _ in range(n)]
+    new[0] = new[0] or 1
+    check_append(new, [r.choice([0, r.randint(0, 500)]) for _ in range(n)], r.choice([1, 2, 3, 5]), d, page, r.choice(["bf16", "f32"]), pairs=r.choice([None, pairs, [d // 2], [8, 8]]),
+                 pattern=r.choice(["interleaved", "halves", "axis_halves"]), layout=r.choice(["token", "head", "slice"]), grow=r.choice([0.1, 1.0, 30.0]), seed=seed)
 
 
 @pytest.mark.parametrize("layout", ["head", "slice"])
@@ -207,6 +227,37 @@ def test_attend_views(layout):
     a = check_attend([5, 30], [100, 64], 4, 2, 64, 32, "bf16", layout=layout)
     b = check_attend([5, 30], [100, 64], 4, 2, 64, 32, "bf16")
     assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_attend_of_any_shape(seed):
+    r = random.Random(100 + seed)
+    n, Hkv = r.choice([1, 2, 5, 9]), r.choice([1, 2, 3])
+    new = [1] * n if r.random() < 0.4 else [r.choice([0, 1, r.randint(1, 300)]) for _ in range(n)]
+    new[0] = new[0] or 1
+    most = r.choice([100, 1500, 3000])
+    check_attend(new, [r.choice([0, 1, r.randint(1, most)]) for _ in range(n)], Hkv * r.choice([1, 2, 4, 7]), Hkv, r.choice([64, 128]), r.choice([16, 32, 64, 128, 256]),
+                 r.choice(["bf16", "f32"]), r.random() < 0.6, layout=r.choice(["token", "head", "slice"]), behind=r.choice([0, 3]), max_len=r.choice([None, most]), seed=seed)
+
+
+def test_pages_behind_4_gb():
+    """A pool of more than 2^32 bytes: the same tokens into its first pages and into its last, the same bytes there and the same attention over them."""
+    H, d, page, T = 8, 128, 256, 300
+    n_pages = 2 ** 32 // (H * page * d) + 4
+    K, V, Q = (rows(T, h, d, "bf16", i).to(DEV) for i, h in enumerate((H, H, 16)))
+    cu, lens = ints([0, T]), ints([T])
+    K8, V8 = (torch.zeros(n_pages, H, page, d, dtype=torch.uint8, device=DEV) for _ in range(2))
+    ks, vs = (torch.zeros(n_pages, H, device=DEV) for _ in range(2))
+    p = dsv.Cache(1, T, T, 16, H, d, "bf16", n_pages, page, 2, scale=0.1)
+    got = []
+    for first in (0, n_pages - 2):
+        table = ints([[first, first + 1]])
+        dsv.cache_append(p, K, V, cu, lens, table, K8, V8, ks, vs)
+        got.append((*dsv.cache_attn_fwd(p, Q, cu, lens, table, K8, V8, ks, vs), K8[first : first + 2], V8[first : first + 2], ks[first : first + 2], vs[first : first + 2]))
+    torch.cuda.synchronize()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    assert got[0][2].any() and not K8[2 : n_pages - 2 : 997].any()
 
 
 def test_attend_many_streams():

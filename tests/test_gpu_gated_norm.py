@@ -1,5 +1,7 @@
 """Gated norms on the GPU against their formulas in 64 bits: widths around every split of a row over lanes, segments of none to many rows, missing parts,
 views, and runs of them together."""
+import random
+
 import pytest
 import torch
 
@@ -162,6 +164,42 @@ def test_no_rows_and_gradients_that_are_not_wanted():
     only = torch.full((1, 64), 7.0, device=DEV)
     assert dsv.gated_norm_bwd(p, h["X"], cu, stats, h["dZ"], h["Y"], dshift=only)[2:] == (None, None, only)
     assert (only - h["dZ"].float().sum(0)).abs().max() < 1e-4
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_any_shape(seed):
+    r = random.Random(seed)
+    n = r.choice([r.randint(1, 300), 64 * r.randint(1, 40), r.randint(300, 3000)])
+    lens = [r.choice([0, 1, r.randint(1, 80)]) for _ in range(r.choice([1, 2, 7, 90]))]
+    lens[0] = lens[0] or 1
+    gone = r.choice([(), (), ("gate",), ("scale", "shift"), ("dH",), ("Y", "gate")])
+    check(lens, n, r.choice(["bf16", "f32"]), without=gone, kind=r.choice(["layer", "rms"]), post="Y" not in gone and r.random() < 0.5, residual=r.choice([1.0, 0.3]),
+          behind=r.choice([0, 5]), wide=r.choice([0, 0, 16, 5]), seed=seed)
+
+
+@pytest.mark.parametrize("n", [64, 65])
+def test_many_segments(n):
+    g = torch.Generator().manual_seed(3)
+    check(torch.randint(0, 3, (5000,), generator=g).tolist(), n, "bf16")
+
+
+def test_rows_behind_4_gb():
+    """Rows that lie 2^31 elements and more apart."""
+    T, n, apart = 3, 512, 2 ** 31 + 64
+    h = {k: v.to(DEV) for k, v in inputs(T, n, 1, "bf16").items()}
+    far = torch.empty(2 * apart + n, dtype=torch.bfloat16, device=DEV).as_strided((T, n), (apart, 1))
+    cu = packed_ref.cu_of([T]).to(DEV)
+    p = dsv.GatedNorm(T, n, 1, "bf16")
+    args = (cu, h["Y"], h["gate"], h["scale"], h["shift"])
+    Z, H, stats = dsv.gated_norm_fwd(p, h["X"], *args)
+    want = dsv.gated_norm_bwd(p, h["X"], cu, stats, h["dZ"], h["Y"], h["gate"], h["scale"], h["dH"])
+    far.copy_(h["X"])
+    for a, b in zip(dsv.gated_norm_fwd(p, far, *args), (Z, H, stats)):
+        assert torch.equal(a, b)
+    for a, b in zip(dsv.gated_norm_bwd(p, far, cu, stats, h["dZ"], h["Y"], h["gate"], h["scale"], h["dH"]), want):
+        assert torch.equal(a, b)
+    dsv.gated_norm_fwd(p, h["X"], *args, H=far)
+    assert torch.equal(far, H)
 
 
 def test_lengths_that_make_no_sense_stay_inside():

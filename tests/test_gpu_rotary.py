@@ -1,5 +1,6 @@
 """Rotary positions on the GPU against their formula in 64 bits: every layout, whole and partial heads, pairs in eights and not, views, far and negative positions."""
 import math
+import random
 
 import pytest
 import torch
@@ -120,6 +121,28 @@ def test_channels_that_are_not_turned_are_copied_bit_for_bit(pairs, pattern, dty
     assert torch.equal(Y[..., rot:].contiguous().view(whole), X[..., rot:].contiguous().view(whole))
     value, bound = ref.rotary(X.double(), pos, freq, pairs, pattern, 1.25, dtype=dtype)
     packed_ref.assert_within("Y", Y[..., :rot], (value[..., :rot], bound[..., :rot]))
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_any_shape(seed):
+    r = random.Random(seed)
+    d = r.choice([r.randint(2, 200), 64, 128, 16 * r.randint(1, 16)])
+    pairs = [r.randint(0, d // 6) for _ in range(r.randint(1, 3))]
+    pairs[0] = pairs[0] or 1
+    check(r.choice([1, 3, 70, 513]), r.choice([1, 2, 5, 16, 33]), d, pairs, r.choice(LAYOUTS), r.choice(["bf16", "f32"]), r.choice(["token", "head", "slice"]),
+          gain=r.choice([1.0, 1.2]), first=r.choice([0, 10 ** 6]), seed=seed)
+
+
+@pytest.mark.parametrize("pairs", [[64], [5]])
+def test_rows_behind_4_gb(pairs):
+    T, H, d, apart = 2, 3, 128, 2 ** 31 + 64
+    X, _, pos = inputs(T, H, d, 1, "bf16")
+    far = torch.empty(apart + H * d, dtype=torch.bfloat16, device=DEV).as_strided((T, H, d), (apart, d, 1))
+    far.copy_(X)
+    p = dsv.Rotary(T, H, d, "bf16", pairs)
+    want = dsv.rotary_fwd(p, X.to(DEV), pos.to(DEV), ref.freqs(pairs).to(DEV))
+    dsv.rotary_fwd(p, far, pos.to(DEV), ref.freqs(pairs).to(DEV), Y=far)
+    assert torch.equal(far, want)
 
 
 def test_streams_graphs_and_no_tokens():
