@@ -136,29 +136,44 @@ CacheArgs cache_args(const dsv_cache &p, const int32_t *cu, const int32_t *lens,
     a.max_len = std::min(p.max_len, p.page * p.max_pages);
     return a;
 }
-// As the packed forward's, but for the pieces: lengths of caches, which the kernels alone know, are anything up to the longest, so there are pieces enough
-// that the blocks of a few long ones fill the chip (blocks of a piece that a cache does not reach end at once).
+// The packed forward's tiles, in pieces of their own: lengths of caches, which the kernels alone know, are anything up to the longest (blocks of a piece that
+// a cache does not reach end at once).
 Walk walk_of(const dsv_cache &p)
 {
     const int64_t g = p.Hq / p.Hkv, longest = std::min(p.max_len, p.page * p.max_pages), own = p.total * g, max_own = (int64_t)std::min(p.max_new, p.total) * g;
     Walk w = plan_forward(p.dtype, p.d, p.causal != 0, own, max_own, p.Hkv, p.n_seq, p.n_seq * longest, longest);
-    const int64_t rows = w.few ? 32 : 128;
-    const int64_t tiles = std::min<int64_t>((int64_t)p.n_seq * ((max_own + rows - 1) / rows), own / rows + p.n_seq) * p.Hkv;
-    int64_t chunk;
+    const int64_t rows = w.few ? 32 : 128, most = (max_own + rows - 1) / rows;
+    const int64_t tiles = std::min<int64_t>((int64_t)p.n_seq * most, own / rows + p.n_seq) * p.Hkv;
+    int64_t chunk = longest;
     if (w.few) {
         // Bound by memory.  Twelve caches of up to 16001, four heads, group 4, d = 128, us without the join: pieces of 256 keys 23.6, 384 21.1, 512 19.9, 768
         // 18.9; 64 caches of 2047 .. 19900, two heads, group 7: 640 keys 84, 1280 80, 2560 89; five of up to 1023 in fp32, two heads: 256 10, 512 15.
         // Short caches go in one piece: a join costs as much as six more steps of a wave, and its launch and workspace on the host besides.  Eight caches of up to 400,
         // 800 and 1000 keys, four heads, group 4, d = 128, us captured into a graph: 10.3, 10.9, 10.7 in pieces, 9.0, 11.9, 13.1 in one, and by
         // itself 22 and 17; fp32, four caches of 1000, two heads, d = 64: 9.6 and 12.2, d = 128: 12.7 and 19.8 (500: 12.5 and 13.0).
-        if (longest <= (p.dtype == DSV_F32 && p.d == 128 ? 512 : 1024)) chunk = longest;
-        else chunk = std::max(tiles * longest / 2048, std::min<int64_t>(512, std::max<int64_t>(256, tiles * longest / 512)));
-    } else {
-        // Two streams of 1560 queries against 21840 and 7800 keys, eight heads on two, d = 128, bf16, us with the join: two pieces 366, five 292, eight 256, twelve 251,
-        // sixteen 265.  In pieces for 768, 1024, 1536 and 2048 blocks at most: that call 259, 284, 260, 266; 1045 and 63 queries against 8208 and 192, twelve heads
-        // on three: 103, 96, 104, 111; eight streams of 2 .. 915 against 32 .. 17860, d = 64: 44, 39, 34, 34.
-        if (tiles >= 1024) return w;
-        chunk = std::max<int64_t>((longest * tiles + 1535) / 1536, 512);
+        if (longest > (p.dtype == DSV_F32 && p.d == 128 ? 512 : 1024))
+            chunk = std::max(tiles * longest / 2048, std::min<int64_t>(512, std::max<int64_t>(256, tiles * longest / 512)));
+    } else if (longest > 0) {
+        // Rounds of blocks, the sequence of most queries taken to have the longest cache and the others half of it; a tenth of a round more costs none.  Times in
+        // keys a block walks (37 ns), 200 to begin and to end.  us, by the rule and by others: 1045 and 63 queries
+        // against 8208 and 192 keys, twelve heads on three, d = 128, bf16: five pieces 86, four 92, eight 98, seventeen 106; 129 queries on 14912, fp32:
+        // seventeen 51, thirty 70; 1560 queries each on 21840 and 7800, eight heads on two: three 265, eight 257, five 295.
+        const int per_cu = p.dtype == DSV_F32 ? (p.d == 128 ? 1 : 2) : (p.d == 128 ? 2 : 3);
+        const double at_once = 256.0 * per_cu, of_longest = (double)(most * p.Hkv), others = (double)tiles - of_longest;
+        const double join = (double)p.total * p.Hq * p.d * 8.0 / 4e12 / 37e-9;  // a piece
+        double best = 0;
+        int64_t before = 0;
+        for (int64_t s = 1; s <= 64; ++s) {
+            const int64_t c = std::max<int64_t>(256, ((longest + s - 1) / s + 127) / 128 * 128);
+            if (c == before) continue;
+            before = c;
+            const double pieces = (double)((longest + c - 1) / c), blocks = of_longest * pieces + others * std::ceil(pieces / 2);
+            const double t = std::max(1.0, std::floor(blocks / at_once + 0.9)) * ((double)c + 200.0) + (pieces > 1 ? join * pieces + 128.0 : 0.0);
+            if (s == 1 || t < 0.965 * best) {
+                best = t;
+                chunk = c;
+            }
+        }
     }
     chunk = (std::max(chunk, (longest + 63) / 64) + 127) / 128 * 128;
     w.chunk = chunk < longest ? (int)chunk : 0;
