@@ -837,19 +837,24 @@ def _row(c, name: str, t, shape, dtype, device):
     return t.data_ptr()
 
 
+def _made(like, *shape, dtype=None):
+    """(tensor, pointer) of a new contiguous tensor, which needs no check: rows like those of `like`, or of another shape and type."""
+    t = torch.empty(shape, dtype=dtype, device=like.device) if shape else torch.empty_like(like, memory_format=torch.contiguous_format)
+    return t, t.data_ptr()
+
+
 def gated_norm_fwd(p: GatedNorm, X, cu, Y=None, gate=None, scale=None, shift=None, Z=None, H=None, stats=None, stream=None):
     """(Z, H, stats) of h = residual X + gate Y, z = norm(h) (1 + scale) + shift.  X, Y [tokens, n], gate, scale, shift [n_seg, n] or None, any strides
     between rows; cu int32 [n_seg + 1] on the device.  Without Y there is no H (None).  H may be X.  stats (float [tokens, 4]): for the backward."""
     lib = load_library()
     with _On(X, stream) as on:
         dev, td, c, shape, mod = X.device, p.torch_dtype, _CGatedNorm.from_buffer_copy(p._c), p.shape, p.mod_shape
-        Z = torch.empty_like(X) if Z is None else Z
-        H = torch.empty_like(X) if H is None and Y is not None else H
-        stats = torch.empty((p.tokens, 4), dtype=torch.float32, device=dev) if stats is None else stats
-        _check(lib.dsv_gated_norm_fwd(c, _row(c, "x", X, shape, td, dev), _row(c, "y", Y, shape, td, dev), _flat("cu", cu, (p.n_seg + 1,), torch.int32, dev),
-                                      _row(c, "gate", gate, mod, td, dev), _row(c, "scale", scale, mod, td, dev), _row(c, "shift", shift, mod, td, dev),
-                                      _row(c, "z", Z, shape, td, dev), _row(c, "h", H, shape, td, dev), _flat("stats", stats, (p.tokens, 4), torch.float32, dev),
-                                      on.ptr), "dsv_gated_norm_fwd")
+        x, y = _row(c, "x", X, shape, td, dev), _row(c, "y", Y, shape, td, dev)
+        Z, z = _made(X) if Z is None else (Z, _row(c, "z", Z, shape, td, dev))
+        H, h = _made(X) if H is None and Y is not None else (H, _row(c, "h", H, shape, td, dev))
+        stats, st = _made(X, p.tokens, 4, dtype=torch.float32) if stats is None else (stats, _flat("stats", stats, (p.tokens, 4), torch.float32, dev))
+        _check(lib.dsv_gated_norm_fwd(c, x, y, _flat("cu", cu, (p.n_seg + 1,), torch.int32, dev), _row(c, "gate", gate, mod, td, dev),
+                                      _row(c, "scale", scale, mod, td, dev), _row(c, "shift", shift, mod, td, dev), z, h, st, on.ptr), "dsv_gated_norm_fwd")
     return Z, H, stats
 
 
@@ -864,16 +869,18 @@ def gated_norm_bwd(p: GatedNorm, X, cu, stats, dZ, Y=None, gate=None, scale=None
     lib = load_library()
     with _On(X, stream) as on:
         dev, td, c, shape, mod, f32 = X.device, p.torch_dtype, _CGatedNorm.from_buffer_copy(p._c), p.shape, p.mod_shape, torch.float32
-        dX = torch.empty_like(X) if dX is None else dX
-        dY = torch.empty_like(X) if dY is None and Y is not None else dY
-        dgate = torch.empty(mod, dtype=f32, device=dev) if dgate is None and gate is not None else dgate
-        if scale is not None:
-            dscale = torch.empty(mod, dtype=f32, device=dev) if dscale is None else dscale
-            dshift = torch.empty(mod, dtype=f32, device=dev) if dshift is None else dshift
-        args = (_row(c, "x", X, shape, td, dev), _row(c, "y", Y, shape, td, dev), _flat("cu", cu, (p.n_seg + 1,), torch.int32, dev),
-                _row(c, "gate", gate, mod, td, dev), _row(c, "scale", scale, mod, td, dev), _flat("stats", stats, (p.tokens, 4), f32, dev),
-                _row(c, "dz", dZ, shape, td, dev), _row(c, "dh", dH, shape, td, dev), _row(c, "dx", dX, shape, td, dev), _row(c, "dy", dY, shape, td, dev),
-                _row(c, "dgate", dgate, mod, f32, dev), _row(c, "dscale", dscale, mod, f32, dev), _row(c, "dshift", dshift, mod, f32, dev))
+        x, y = _row(c, "x", X, shape, td, dev), _row(c, "y", Y, shape, td, dev)
+        dX, dx = _made(X) if dX is None else (dX, _row(c, "dx", dX, shape, td, dev))
+        dY, dy = _made(X) if dY is None and Y is not None else (dY, _row(c, "dy", dY, shape, td, dev))
+        if gate is not None and scale is not None and dgate is None and dscale is None and dshift is None:  # the usual call: one tensor for the three
+            sums, dg = _made(X, 3, *mod, dtype=f32)
+            (dgate, dscale, dshift), ds, dt = sums.unbind(), dg + 4 * mod[0] * mod[1], dg + 8 * mod[0] * mod[1]
+        else:
+            dgate, dg = _made(X, *mod, dtype=f32) if dgate is None and gate is not None else (dgate, _row(c, "dgate", dgate, mod, f32, dev))
+            dscale, ds = _made(X, *mod, dtype=f32) if dscale is None and scale is not None else (dscale, _row(c, "dscale", dscale, mod, f32, dev))
+            dshift, dt = _made(X, *mod, dtype=f32) if dshift is None and scale is not None else (dshift, _row(c, "dshift", dshift, mod, f32, dev))
+        args = (x, y, _flat("cu", cu, (p.n_seg + 1,), torch.int32, dev), _row(c, "gate", gate, mod, td, dev), _row(c, "scale", scale, mod, td, dev),
+                _flat("stats", stats, (p.tokens, 4), f32, dev), _row(c, "dz", dZ, shape, td, dev), _row(c, "dh", dH, shape, td, dev), dx, dy, dg, ds, dt)
         wanted = dgate is not None or dscale is not None or dshift is not None
         ws, nbytes, held = _scratch(lib.dsv_gated_norm_bwd_workspace(c) if wanted else 0, dev, workspace)
         _check(lib.dsv_gated_norm_bwd(c, *args, ws, nbytes, on.ptr), "dsv_gated_norm_bwd")
@@ -941,10 +948,12 @@ def cache_attn_fwd(p: Cache, Q, cu, lens, table, K8, V8, kscale, vscale, O=None,
     lib = load_library()
     with _On(Q, stream) as on:
         dev, td, c = Q.device, p.torch_dtype, _CCache.from_buffer_copy(p._c)
+        q = _rows(c, "q", Q, p.q_shape, td, dev)
         O = torch.empty_like(Q) if O is None else O
-        lse = torch.empty((p.Hq, p.total), dtype=torch.float32, device=dev) if lse is None else lse
+        o = _rows(c, "o", O, p.q_shape, td, dev)
+        lse, l = _made(Q, p.Hq, p.total, dtype=torch.float32) if lse is None else (lse, _flat("lse", lse, (p.Hq, p.total), torch.float32, dev))
         index, pools = _cache_args(p, cu, lens, table, K8, V8, kscale, vscale, dev)
-        args = (_rows(c, "q", Q, p.q_shape, td, dev), *index, *pools, _rows(c, "o", O, p.q_shape, td, dev), _flat("lse", lse, (p.Hq, p.total), torch.float32, dev))
+        args = (q, *index, *pools, o, l)
         ws, nbytes, held = _scratch(lib.dsv_cache_attn_fwd_workspace(c), dev, workspace)
         _check(lib.dsv_cache_attn_fwd(c, *args, ws, nbytes, on.ptr), "dsv_cache_attn_fwd")
     return O, lse
