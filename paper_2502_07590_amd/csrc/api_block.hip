@@ -238,7 +238,7 @@ dsv_status dsv_gated_norm_fwd(const dsv_gated_norm *p, const void *X, const void
 size_t dsv_gated_norm_bwd_workspace(const dsv_gated_norm *p)
 {
     if (check_gated(p, true) != DSV_OK) return 0;
-    return gated_bwd_bytes(p->tokens, p->n, p->dtype);
+    return gated_bwd_bytes(p->tokens, p->n, p->n_seg, p->dtype);
 }
 
 dsv_status dsv_gated_norm_bwd(const dsv_gated_norm *p, const void *X, const void *Y, const int32_t *cu, const void *gate, const void *scale, const float *stats,
@@ -251,7 +251,7 @@ dsv_status dsv_gated_norm_bwd(const dsv_gated_norm *p, const void *X, const void
     if (p->tokens > 0 && !Y && (gate || dY || dgate || p->post)) return DSV_EINVAL;
     if (p->tokens > 0 && (!X || !stats || !dZ || !dX || (Y && !dY))) return DSV_EINVAL;
     if (dH && !in_place_or_apart(dX, p->dx, dH, p->dh)) return DSV_EINVAL;
-    st = check_workspace(workspace, ws_bytes, dgate || dscale || dshift ? gated_bwd_bytes(p->tokens, p->n, p->dtype) : 0);
+    st = check_workspace(workspace, ws_bytes, dgate || dscale || dshift ? gated_bwd_bytes(p->tokens, p->n, p->n_seg, p->dtype) : 0);
     if (st != DSV_OK) return st;
     const bool wide = wide_rows(p->n, p->dtype, {{X, p->x}, {Y, p->y}, {gate, p->gate}, {scale, p->scale}, {dZ, p->dz}, {dH, p->dh}, {dX, p->dx}, {dY, p->dy}});
     return launch_gated_bwd(gated_args(*p, cu), p->dtype, wide, {X, Y, gate, scale, nullptr}, reinterpret_cast<const float4 *>(stats), dZ, dH, dX, dY, dgate, dscale,

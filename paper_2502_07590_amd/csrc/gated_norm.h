@@ -18,7 +18,7 @@ struct GatedNormIn {
     const void *X, *Y, *gate, *scale, *shift;
 };
 dsv_status launch_gated_fwd(GatedNormArgs a, int dtype, bool wide, const GatedNormIn &in, void *Z, void *H, float4 *stats, hipStream_t st);
-size_t gated_bwd_bytes(int64_t tokens, int n, int dtype);  // of the sums of segments that have several blocks
+size_t gated_bwd_bytes(int64_t tokens, int n, int n_seg, int dtype);  // of the sums of segments that have several blocks
 dsv_status launch_gated_bwd(GatedNormArgs a, int dtype, bool wide, const GatedNormIn &in, const float4 *stats, const void *dZ, const void *dH, void *dX, void *dY,
                             float *dgate, float *dscale, float *dshift, float *part, hipStream_t st);
 

@@ -8,7 +8,7 @@
 //
 // Bound by memory: a row's elements are read once into registers, LPR lanes to a row, the next row's on their way while one is worked on.
 // The backward forms h from x and y once more: as many bytes as reading it, and none of the 8 bits that its rounding leaves.  32768 rows of 2048, bf16:
-// 102 to 107 us forward (5.2 TB/s; a copy of 1 GiB: 5.1), 177 to 181 and 7 for the sums backward (4.5); 20280 of 1536, fp32, post: 91 (5.5) and 159 (4.7).
+// 102 to 107 us forward (5.2 TB/s; a copy of 1 GiB: 5.1), 172 and 7 for the sums backward (4.7); 20280 of 1536, fp32, post: 90 (5.5) and 158 (4.7).
 #include <algorithm>
 
 #include "gated_norm.h"
@@ -158,15 +158,15 @@ __device__ __forceinline__ int64_t part_row(const GatedNormArgs &a, int first) {
 // What is not there -- a modulation, Y, dH, elements past the row's end -- is held as zeros (a gate that is not there as ones), so that no element asks.
 // Past the end that leaves numbers in no sum but dg, of columns that are not written.
 template <typename T, int CH, int LPR, int NP>
-__global__ __launch_bounds__(256, NP * CH <= 8 ? 3 : NP * CH <= 16 ? 2 : 1) void gated_bwd_kernel(const T *__restrict__ X, const T *__restrict__ Y, const T *__restrict__ gate,
+__global__ __launch_bounds__(LPR < 256 ? 256 : LPR, LPR == 512 ? 2 : NP * CH <= 8 ? 3 : NP * CH <= 16 ? 2 : 1) void gated_bwd_kernel(const T *__restrict__ X, const T *__restrict__ Y, const T *__restrict__ gate,
                                                                                    const T *__restrict__ scale, const float4 *__restrict__ stats,
                                                                                    const T *__restrict__ dZ, const T *dH, T *dX, T *__restrict__ dY, float *dgate,
                                                                                    float *dscale, float *dshift, float *__restrict__ part, GatedNormArgs a)
 {
     typedef Lane<T, CH, LPR, NP> L;
-    constexpr int RPB = 256 / LPR;
-    constexpr bool kAhead = NP * CH <= 16;  // the next row's loads under way: its registers would be others' with more elements
-    __shared__ float2 red[2][4];
+    constexpr int RPB = LPR < 256 ? 256 / LPR : 1;
+    constexpr bool kAhead = NP * CH <= (CH == 8 ? 16 : 8);  // the next row's loads under way: its registers would be others' with more elements
+    __shared__ float2 red[2][LPR < 256 ? 4 : LPR / 64];
     const Span s = block_rows(a);
     if (s.count <= 0) return;
     const L l(a.n);
@@ -331,7 +331,8 @@ __global__ __launch_bounds__(256) void gated_sum_kernel(const float *__restrict_
 }
 
 // Lanes to a row and pieces to a lane: few elements a lane, a row to a block where a wave would hold more than two pieces.  (A wave to rows of 2048, four
-// pieces a lane: the backward's registers leave one wave a SIMD, 32768 rows in bf16 346 us.)
+// pieces a lane: the backward's registers leave one wave a SIMD, 32768 rows in bf16 346 us.)  Past two pieces a lane of 256, 512 lanes, for the same
+// reason; us, 256 and 512: 20000 rows of 4480 in bf16 352, 224; 1500 of 8192 100, 46; in fp32 of 2560 362, 252; 1500 of 8192 104, 75.
 NormShape bwd_shape(int n, int ch)
 {
     const int pieces = (n + ch - 1) / ch;
@@ -345,9 +346,9 @@ NormShape bwd_shape(int n, int ch)
     for (int lpr = 8; lpr <= 64; lpr *= 2)
         if (pieces <= lpr) return {lpr, 1};
     if (pieces <= 128) return {64, 2};
-    int np = 1;
-    while (pieces > 256 * np) np *= 2;
-    return {256, np};
+    for (int np : {1, 2})
+        if (np * ch <= 16 && pieces <= 256 * np) return {256, np};
+    return {512, pieces <= 1024 ? 2 : 4};
 }
 // f(integral constants LPR, NP) for the shape of a row
 template <int CH, typename F> dsv_status with_bwd_shape(const NormShape &s, F f)
@@ -357,8 +358,8 @@ template <int CH, typename F> dsv_status with_bwd_shape(const NormShape &s, F f)
     if constexpr (CH == 1) {
         DSV_SHAPE(64, 1) DSV_SHAPE(64, 4) DSV_SHAPE(64, 8) DSV_SHAPE(256, 4) DSV_SHAPE(256, 8) DSV_SHAPE(256, 16) DSV_SHAPE(256, 32)
     } else {
-        DSV_SHAPE(8, 1) DSV_SHAPE(16, 1) DSV_SHAPE(32, 1) DSV_SHAPE(64, 1) DSV_SHAPE(64, 2) DSV_SHAPE(256, 1) DSV_SHAPE(256, 2) DSV_SHAPE(256, 4)
-        if constexpr (CH == 4) { DSV_SHAPE(256, 8) }
+        DSV_SHAPE(8, 1) DSV_SHAPE(16, 1) DSV_SHAPE(32, 1) DSV_SHAPE(64, 1) DSV_SHAPE(64, 2) DSV_SHAPE(256, 1) DSV_SHAPE(256, 2) DSV_SHAPE(512, 2)
+        if constexpr (CH == 4) { DSV_SHAPE(512, 4) }
     }
 #undef DSV_SHAPE
     return DSV_EUNSUPPORTED;
@@ -366,17 +367,21 @@ template <int CH, typename F> dsv_status with_bwd_shape(const NormShape &s, F f)
 
 int rows_a_block(int64_t tokens, int lpr, int blocks)
 {
-    const int rpb = 256 / lpr;
+    const int rpb = std::max(1, 256 / lpr);
     return (int)std::max<int64_t>(1, (tokens + (int64_t)blocks * rpb - 1) / ((int64_t)blocks * rpb)) * rpb;
 }
 // Forward: a block goes on to further rows with the modulation in its registers and the next row under way, or there are more blocks.  us, with 2048, 8192
 // and 32768 blocks: 17000 rows of 2048 in bf16 49, 54, 54; 64000 of 512 47, 52, 61; 64000 of 2048 210, 185, 192; 17000 of 5120 144, 144, 162;
 // in fp32 17000 of 512 24, 23, 23; 17000 of 2048 127, 108, 107; 64000 of 2048 449, 420, 370; 17000 of 8192 576, 513, 389.
 int fwd_blocks(int64_t tokens, int n, bool bf16) { return !bf16 ? 32768 : tokens * n >= (3ll << 24) ? 8192 : 2048; }
-// Backward: three blocks of up to 8 elements a lane run on a CU at once, and each leaves 3 n floats to sum.  32768 rows of 2048 in bf16, 20280 of 1536 in
-// fp32 with post, us: 512 blocks 200, 184; 768 183, 159; 1024 (four a CU, at 128 registers) 257, 372.
-constexpr int kBwdBlocks = 768;
-int bwd_rows(int64_t tokens, int lpr) { return rows_a_block(tokens, lpr, kBwdBlocks); }
+// Backward: two blocks of 256 a CU, or one of 512, and no more of them than that by the segments' last ones: a CU that takes a third sets the time.  Each
+// leaves 3 n floats to sum.  us, 512 blocks and 768 (three a CU fit up to 8 elements a lane): 32768 rows of 2048 in four segments, bf16, forward and
+// backward 276, 282 (512 without regard to the segments: 300); backward alone 1500 rows of 2048 24, 29; 20000 111, 119; in fp32 208, 213.
+int bwd_rows(int64_t tokens, int n_seg, const NormShape &s)
+{
+    const int blocks = s.lpr == 512 ? 256 : 512;
+    return rows_a_block(tokens, s.lpr, blocks - std::min(n_seg, blocks / 4));
+}
 int chunk_of(int dtype, bool wide) { return !wide ? 1 : dtype == DSV_BF16 ? 8 : 4; }
 
 template <typename T, int CH>
@@ -397,10 +402,10 @@ dsv_status bwd_t(GatedNormArgs a, const GatedNormIn &in, const float4 *stats, co
                  float *dshift, float *part, hipStream_t st)
 {
     const NormShape s = bwd_shape(a.n, CH);
-    a.rows = bwd_rows(a.tokens, s.lpr);
+    a.rows = bwd_rows(a.tokens, a.n_seg, s);
     return with_bwd_shape<CH>(s, [&](auto lpr, auto np) {
         if (a.tokens > 0) {
-            gated_bwd_kernel<T, CH, decltype(lpr)::value, decltype(np)::value><<<(unsigned)tile_slots(a.tokens, 1, a.rows, a.n_seg), 256, 0, st>>>(
+            gated_bwd_kernel<T, CH, decltype(lpr)::value, decltype(np)::value><<<(unsigned)tile_slots(a.tokens, 1, a.rows, a.n_seg), std::max(256, s.lpr), 0, st>>>(
                 static_cast<const T *>(in.X), static_cast<const T *>(in.Y), static_cast<const T *>(in.gate), static_cast<const T *>(in.scale), stats,
                 static_cast<const T *>(dZ), static_cast<const T *>(dH), static_cast<T *>(dX), static_cast<T *>(dY), dgate, dscale, dshift, part, a);
             DSV_LAUNCH_CHECK();
@@ -422,11 +427,11 @@ dsv_status launch_gated_fwd(GatedNormArgs a, int dtype, bool wide, const GatedNo
 }
 
 // the pointers do not enter: as many rows as either alignment leaves
-size_t gated_bwd_bytes(int64_t tokens, int n, int dtype)
+size_t gated_bwd_bytes(int64_t tokens, int n, int n_seg, int dtype)
 {
     size_t most = 0;
     for (bool wide : {false, true}) {
-        const int rows = bwd_rows(tokens, bwd_shape(n, chunk_of(dtype, wide)).lpr);
+        const int rows = bwd_rows(tokens, n_seg, bwd_shape(n, chunk_of(dtype, wide)));
         // one segment of more than `rows` at least; the last one's begins at row 2 floor(first / rows) and has ceil(len / rows)
         most = std::max(most, tokens > rows ? (size_t)(2 * (tokens / rows) + 2) * 3 * n * 4 : (size_t)0);
     }

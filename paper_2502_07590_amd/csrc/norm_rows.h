@@ -43,7 +43,7 @@ __device__ __forceinline__ void put(float *p, const float (&f)[4]) { *reinterpre
 __device__ __forceinline__ void put(bf16_t *p, const float (&f)[1]) { *p = (bf16_t)(pack2(f[0], 0.f) & 0xFFFFu); }
 __device__ __forceinline__ void put(float *p, const float (&f)[1]) { *p = f[0]; }
 
-// Sums of two values over the LPR lanes of a row.  256: the whole block, through LDS.
+// Sums of two values over the LPR lanes of a row.  256 and more: the whole block, through LDS.
 template <int LPR> __device__ __forceinline__ float2 row_sums(float a, float b, float2 *red)
 {
     constexpr int W = LPR < 64 ? LPR : 64;
@@ -52,12 +52,20 @@ template <int LPR> __device__ __forceinline__ float2 row_sums(float a, float b, 
         a += __shfl_xor(a, s);
         b += __shfl_xor(b, s);
     }
-    if constexpr (LPR == 256) {
+    if constexpr (LPR >= 256) {
+        constexpr int N = LPR / 64;
         const int wave = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0) red[wave] = make_float2(a, b);
         __syncthreads();
-        a = (red[0].x + red[1].x) + (red[2].x + red[3].x);
-        b = (red[0].y + red[1].y) + (red[2].y + red[3].y);
+        float2 v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = red[i];
+#pragma unroll
+        for (int s = 1; s < N; s *= 2)
+#pragma unroll
+            for (int i = 0; i < N; i += 2 * s) v[i] = make_float2(v[i].x + v[i + s].x, v[i].y + v[i + s].y);
+        a = v[0].x;
+        b = v[0].y;
     }
     return make_float2(a, b);
 }

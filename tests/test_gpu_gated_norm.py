@@ -86,6 +86,14 @@ def test_segments_of_several_blocks(lens, n, dtype):
     check(lens, n, dtype, post=n < 600)
 
 
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("dtype,n", [("bf16", 5888), ("bf16", 8192), ("f32", 2560), ("f32", 4480)])
+def test_wide_rows_of_several_blocks(dtype, n, kind):
+    """512 lanes to a row: segments of many blocks, of one, of none; more segments than blocks are held back for."""
+    check([600, 0, 3, 500], n, dtype, kind=kind, post=kind == "rms", behind=2)
+    check([1] * 90 + [400], n, dtype, kind=kind, post=kind == "layer")
+
+
 @pytest.mark.parametrize("n", [64, 1001])
 @pytest.mark.parametrize("without", [(k,) for k in PARTS if k != "Y"] + [("gate", "scale", "shift", "dH"), ("Y", "gate"), ("Y", "gate", "scale", "shift", "dH")])
 @pytest.mark.parametrize("kind", ["layer", "rms"])
