@@ -80,47 +80,67 @@ template <> struct Raw<float> {
 
 enum TurnForm { kStraight, kEights, kAnyPairs };
 
-// Sixteen channels from c0 on whose pairs lie anywhere: what each is multiplied by, and its other channel.
-__device__ __forceinline__ void any_turns(const TurnArgs &t, int64_t token, int c0, float2 (&by)[16])
+// Sixteen channels from c0 on whose pairs lie anywhere: pairs and other channels (bytes: D is at most 128), the same for all rows and heads.
+struct AnySixteen {
+    uint32_t pair[4], other[4], turned, second;  // the last two: a bit a channel
+    __device__ __forceinline__ AnySixteen(const TurnArgs &t, int c0) : pair{}, other{}, turned(0), second(0)
+    {
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+            if (c0 + c >= 2 * t.total) continue;
+            int p, o;
+            bool sec;
+            pair_of(t, c0 + c, p, sec, o);
+            pair[c / 4] |= (uint32_t)p << 8 * (c % 4);
+            other[c / 4] |= (uint32_t)o << 8 * (c % 4);
+            turned |= 1u << c;
+            second |= (sec ? 1u : 0u) << c;
+        }
+    }
+    static __device__ __forceinline__ int byte(const uint32_t (&w)[4], int c) { return (int)(w[c / 4] >> 8 * (c % 4) & 0xFFu); }
+};
+// what each channel, and its other one, is multiplied by
+__device__ __forceinline__ void any_turns(const TurnArgs &t, const AnySixteen &s, int64_t token, float2 (&by)[16])
 {
     int pos[3];
     read_position(t, token, pos);
 #pragma unroll
     for (int c = 0; c < 16; ++c) {
         by[c] = make_float2(1.f, 0.f);
-        if (c0 + c >= 2 * t.total) continue;
-        int pair, other;
-        bool second;
-        pair_of(t, c0 + c, pair, second, other);
-        by[c] = turn_of(t, pos, pair);
-        if (!second) by[c].y = -by[c].y;
+        if (!(s.turned >> c & 1)) continue;
+        by[c] = turn_of(t, pos, AnySixteen::byte(s.pair, c));
+        if (!(s.second >> c & 1)) by[c].y = -by[c].y;
     }
 }
-template <typename T> __device__ __forceinline__ void turn_any(const TurnArgs &t, const float2 (&by)[16], const T *x, int c0, float (&f)[8], float (&g)[8])
+template <typename T> __device__ __forceinline__ void turn_any(const AnySixteen &s, const float2 (&by)[16], const T *x, float (&f)[8], float (&g)[8])
 {
+    T o[16];
+#pragma unroll
+    for (int c = 0; c < 16; ++c) o[c] = x[AnySixteen::byte(s.other, c)];  // of a channel that is not turned: the row's first, unused
 #pragma unroll
     for (int c = 0; c < 16; ++c) {
-        if (c0 + c >= 2 * t.total) continue;
-        int pair, other;
-        bool second;
-        pair_of(t, c0 + c, pair, second, other);
         float &v = c < 8 ? f[c & 7] : g[c & 7];
-        v = v * by[c].x + to_f32(x[other]) * by[c].y;
+        v = s.turned >> c & 1 ? v * by[c].x + to_f32(o[c]) * by[c].y : v;
     }
+}
+
+template <TurnForm FORM> __device__ __forceinline__ auto channels(const TurnArgs &t, int c0)
+{
+    if constexpr (FORM == kAnyPairs) return AnySixteen(t, c0);
+    else return 0;
 }
 
 // One tensor's new rows of one page, for heads h0, h0 + step, ...: the next head's loads are under way while one is rounded.
 template <typename T, int D, int N, TurnForm FORM>
 __device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__restrict__ src, int64_t row_s, int64_t head_s, uint8_t *pool, float *scales,
-                                            const CacheArgs &a, int pg, int64_t token0, int begun, int count, int h0, int step, float (&red)[2][4])
+                                            const CacheArgs &a, int pg, int64_t token0, int begun, int count, int h0, int step, float (&red)[2][16])
 {
     constexpr int PER = D / 16;
     const bool interleaved = turns.layout == DSV_TURN_INTERLEAVED;
     Sixteen six[N];
     int row[N];
     float2 t[FORM == kEights ? N : 1][8];
-    constexpr bool kHeld = FORM == kAnyPairs && N <= 2;  // the turns of all heads; more would take all registers
-    float2 any[kHeld ? N : 1][16];
+    float2 any[FORM == kAnyPairs ? N : 1][16];  // the turns of all heads
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         const int job = (int)threadIdx.x + j * (int)blockDim.x;
@@ -128,6 +148,7 @@ __device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__re
         six[j] = Sixteen{16 * (job % PER), 16 * (job % PER) + 8, -1};
         if constexpr (FORM == kEights) six[j] = sixteen_of(turns, job % PER);
     }
+    const std::conditional_t<FORM == kAnyPairs, AnySixteen, int> chans = channels<FORM>(turns, 16 * ((int)threadIdx.x % PER));  // of all its jobs
     Raw<T> raw[N];
     auto load = [&](int h) __attribute__((always_inline)) {
 #pragma unroll
@@ -145,10 +166,10 @@ __device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__re
                 for (int i = 0; i < 8; ++i) t[j][i] = turn_of(turns, pos, six[j].pair + i);
             }
     }
-    if constexpr (kHeld) {
+    if constexpr (FORM == kAnyPairs) {
 #pragma unroll
         for (int j = 0; j < N; ++j)
-            if (row[j] < count) any_turns(turns, token0 + row[j], six[j].first, any[j]);
+            if (row[j] < count) any_turns(turns, chans, token0 + row[j], any[j]);
     }
     int flip = 0;
     for (int h = h0; h < a.Hkv; h += step) {
@@ -159,10 +180,7 @@ __device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__re
             raw[j].numbers(f[j], g[j]);
             if constexpr (FORM == kEights)
                 if (six[j].pair >= 0) turn_sixteen<false>(interleaved, turns.total - six[j].pair, t[j], f[j], g[j]);
-            if constexpr (FORM == kAnyPairs) {
-                if constexpr (!kHeld) any_turns(turns, token0 + row[j], six[j].first, any[0]);
-                turn_any(turns, any[kHeld ? j : 0], src + (token0 + row[j]) * row_s + h * head_s, six[j].first, f[j], g[j]);
-            }
+            if constexpr (FORM == kAnyPairs) turn_any(chans, any[j], src + (token0 + row[j]) * row_s + h * head_s, f[j], g[j]);
 #pragma unroll
             for (int c = 0; c < 8; ++c) most = fmaxf(most, fmaxf(fabsf(f[j][c]), fabsf(g[j][c])));  // of the numbers: fmaxf passes over NaN
         }
@@ -224,11 +242,11 @@ __device__ __forceinline__ void append_page(const TurnArgs &turns, const T *__re
     }
 }
 
-// blockIdx: x a page that some sequence may touch, y the first head (others gridDim.y further), z K or V.  N: sixteens of a page a lane.
-template <typename T, int D, int N, TurnForm FORM>
-__global__ __launch_bounds__(256) void cache_append_kernel(AppendIn in, uint8_t *K8, uint8_t *V8, float *kscale, float *vscale, CacheArgs a)
+// blockIdx: x a page that some sequence may touch, y the first head (others gridDim.y further), z K or V.  N: sixteens of a page a lane.  MOST: lanes, at most.
+template <typename T, int D, int N, int MOST, TurnForm FORM>
+__global__ __launch_bounds__(MOST) void cache_append_kernel(AppendIn in, uint8_t *K8, uint8_t *V8, float *kscale, float *vscale, CacheArgs a)
 {
-    __shared__ float red[2][4];
+    __shared__ float red[2][16];
     const int si = __builtin_amdgcn_readfirstlane(find_sequence(a.cu, a.n_seq, a.total, 1, a.page, (int)blockIdx.x, page_gap(a)));
     const Sequence sq = read_cached(a, si);
     const int start = sq.nk - sq.nq, place = (int)blockIdx.x - first_slot(a.cu[si], a.total, 1, a.page, si * page_gap(a));
@@ -246,18 +264,18 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendIn in, uint8_t 
         append_page<T, D, N, kStraight>(in.turn, static_cast<const T *>(in.V), in.v_row, in.v_head, V8, vscale, a, pg, token0, begun, count, blockIdx.y, gridDim.y, red);
 }
 
-// Heads to a block, one after another with the sines that they share: as many as leave 2048 blocks.  32568 tokens of 16 heads, d = 128, bf16, us: in 1024
+// Heads to a block, one after another with the sines that they share: as many as leave 2048 blocks of 256 lanes, or as many lanes.  32568 tokens of 16 heads, d = 128, bf16, us: in 1024
 // blocks (of both tensors together) 115, 3084 96, 4112 101, 7200 106, 15420 142.
 constexpr int64_t kBlocks = 2048;
-template <typename T, int D, int N>
+template <typename T, int D, int N, int MOST>
 dsv_status launch_n(const CacheArgs &a, const AppendIn &in, int threads, uint8_t *K8, uint8_t *V8, float *kscale, float *vscale, hipStream_t st)
 {
     const int64_t slots = page_slots(a);
-    const int64_t heads = std::min<int64_t>(a.Hkv, std::max<int64_t>(1, kBlocks / slots));
+    const int64_t heads = std::min<int64_t>(a.Hkv, std::max<int64_t>(1, kBlocks * 256 / MOST / slots));
     const dim3 grid((unsigned)slots, (unsigned)heads, 2);
-    if (in.turn.total == 0) cache_append_kernel<T, D, N, kStraight><<<grid, threads, 0, st>>>(in, K8, V8, kscale, vscale, a);
-    else if (in.eights) cache_append_kernel<T, D, N, kEights><<<grid, threads, 0, st>>>(in, K8, V8, kscale, vscale, a);
-    else cache_append_kernel<T, D, N, kAnyPairs><<<grid, threads, 0, st>>>(in, K8, V8, kscale, vscale, a);
+    if (in.turn.total == 0) cache_append_kernel<T, D, N, MOST, kStraight><<<grid, threads, 0, st>>>(in, K8, V8, kscale, vscale, a);
+    else if (in.eights) cache_append_kernel<T, D, N, MOST, kEights><<<grid, threads, 0, st>>>(in, K8, V8, kscale, vscale, a);
+    else cache_append_kernel<T, D, N, MOST, kAnyPairs><<<grid, threads, 0, st>>>(in, K8, V8, kscale, vscale, a);
     DSV_LAUNCH_CHECK();
     return DSV_OK;
 }
@@ -266,14 +284,15 @@ dsv_status launch_d(const CacheArgs &a, const AppendIn &in, uint8_t *K8, uint8_t
 {
     int rows = 1;  // new ones of a page, at most
     while (rows < std::min(a.page, a.max_new)) rows *= 2;
-    const int jobs = rows * (D / 16), threads = std::min(256, std::max(64, jobs));
-    switch ((jobs + threads - 1) / threads) {
-        case 1: return launch_n<T, D, 1>(a, in, threads, K8, V8, kscale, vscale, st);
-        case 2: return launch_n<T, D, 2>(a, in, threads, K8, V8, kscale, vscale, st);
-        case 4: return launch_n<T, D, 4>(a, in, threads, K8, V8, kscale, vscale, st);
-        case 8: return launch_n<T, D, 8>(a, in, threads, K8, V8, kscale, vscale, st);
-        default: return DSV_EUNSUPPORTED;
-    }
+    // A lane holds two sixteens at most.  Pages of 256, 20900 tokens of 16 heads, bf16, us: in 1024 lanes 74, in 256 of eight sixteens each 151; pairs that lie
+    // anywhere 229, 592.
+    const int jobs = rows * (D / 16);
+    if (jobs <= 256) return launch_n<T, D, 1, 256>(a, in, std::max(64, jobs), K8, V8, kscale, vscale, st);
+    if (jobs <= 512) return launch_n<T, D, 2, 256>(a, in, 256, K8, V8, kscale, vscale, st);
+    if (jobs <= 1024) return launch_n<T, D, 2, 512>(a, in, 512, K8, V8, kscale, vscale, st);
+    if constexpr (D == 128)
+        if (jobs <= 2048) return launch_n<T, D, 2, 1024>(a, in, 1024, K8, V8, kscale, vscale, st);
+    return DSV_EUNSUPPORTED;
 }
 }  // namespace
 

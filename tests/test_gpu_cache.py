@@ -69,6 +69,13 @@ def test_append_turned(pairs, pattern, dtype):
     check_append([90, 1], [100, 63], 5, 128, 64, dtype, pairs=pairs, pattern=pattern)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pairs,pattern", [([64], "halves"), ([57], "axis_halves"), ([29, 3, 7], "axis_halves"), ([61], "interleaved"), ([9], "halves")])
+@pytest.mark.parametrize("page", [128, 256])
+def test_append_turned_to_large_pages(page, pairs, pattern, dtype):
+    check_append([700, 1, 255], [100, 255, 3], 3, 128, page, dtype, pairs=pairs, pattern=pattern)
+
+
 def test_append_of_many_sequences():
     """More than one step of the search for a page's sequence, most of them without a token."""
     g = torch.Generator().manual_seed(9)
