@@ -73,7 +73,8 @@ dsv_status check_gated(const dsv_gated_norm *p, bool grad)
     if (p->tokens < 0 || p->n < 1 || p->n_seg < 1 || p->flags) return DSV_EINVAL;
     if (p->kind != DSV_NORM_LAYER && p->kind != DSV_NORM_RMS) return DSV_EINVAL;
     if ((p->post != 0 && p->post != 1) || !std::isfinite(p->eps) || !(p->eps >= 0.f) || !std::isfinite(p->residual)) return DSV_EINVAL;
-    if (!supported_dtype(p->dtype) || p->n > kMaxNormWidth || (int64_t)p->n_seg * ((p->n + 31) / 32) >= 1 << 24) return DSV_EUNSUPPORTED;
+    if (!supported_dtype(p->dtype) || p->n > kMaxNormWidth) return DSV_EUNSUPPORTED;
+    if ((int64_t)p->n_seg * ((p->n + 31) / 32) >= (1 << 24) - (1 << 16)) return DSV_EUNSUPPORTED;  // blocks of a launch: as many, or one a segment and 32768
     for (int64_t s : {p->x, p->y, p->gate, p->scale, grad ? p->dz : p->h, grad ? p->dh : p->z, grad ? p->dx : p->shift, grad ? p->dy : 0, grad ? p->dgate : 0,
                       grad ? p->dscale : 0, grad ? p->dshift : 0})
         if (!ok_stride(s)) return DSV_EINVAL;

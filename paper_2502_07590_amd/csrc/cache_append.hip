@@ -272,6 +272,7 @@ dsv_status launch_n(const CacheArgs &a, const AppendIn &in, int threads, uint8_t
 {
     const int64_t slots = page_slots(a);
     const int64_t heads = std::min<int64_t>(a.Hkv, std::max<int64_t>(1, kBlocks * 256 / MOST / slots));
+    if (slots * threads >= (int64_t)1 << 32) return DSV_EUNSUPPORTED;  // lanes of a grid
     const dim3 grid((unsigned)slots, (unsigned)heads, 2);
     if (in.turn.total == 0) cache_append_kernel<T, D, N, MOST, kStraight><<<grid, threads, 0, st>>>(in, K8, V8, kscale, vscale, a);
     else if (in.eights) cache_append_kernel<T, D, N, MOST, kEights><<<grid, threads, 0, st>>>(in, K8, V8, kscale, vscale, a);

@@ -249,6 +249,13 @@ def test_cache_descriptors_that_are_refused(dsv, change, status):
     assert append(dsv, p) == status and attend(dsv, p) == status and dsv.cache_attn_fwd_workspace(p) == 0
 
 
+def test_launches_of_more_lanes_than_a_grid_holds_are_refused(dsv):
+    """2^32 of them: pages that many sequences may touch, and blocks of many short segments."""
+    assert append(dsv, dsv.Cache(**{**CACHE, **dict(Hq=1, Hkv=1, d=128, page=16, max_pages=1 << 20, n_seq=1 << 23, total=1 << 28, max_new=64)})) == -2
+    assert append(dsv, dsv.Cache(**{**CACHE, **dict(Hq=1, Hkv=1, d=128, page=256, max_pages=1 << 20, n_seq=1 << 22, total=1 << 28, max_new=200)})) == -2
+    assert gated_fwd(dsv, dsv.GatedNorm(**{**GATED, **dict(tokens=1 << 24, n=32, n_seg=(1 << 24) - 1)})) == -2
+
+
 def test_cache_pointers_strides_and_workspaces_that_are_refused(dsv):
     p = dsv.Cache(**CACHE)
     turn = dsv.Rotary(300, 2, 128, "bf16", 64)
