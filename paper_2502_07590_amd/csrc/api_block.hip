@@ -155,10 +155,13 @@ Walk walk_of(const dsv_cache &p)
         if (longest > (p.dtype == DSV_F32 && p.d == 128 ? 512 : 1024))
             chunk = std::max(tiles * longest / 2048, std::min<int64_t>(512, std::max<int64_t>(256, tiles * longest / 512)));
     } else if (longest > 0) {
-        // Rounds of blocks, the sequence of most queries taken to have the longest cache and the others half of it; a tenth of a round more costs none.  Times in
-        // keys a block walks (37 ns), 200 to begin and to end.  us, by the rule and by others: 1045 and 63 queries
+        // Rounds of blocks, the sequence of most queries taken to have the longest cache and the others an eighth of it; a tenth of a round more costs none.
+        // Times in keys a block walks (37 ns), 200 to begin and to end.  us, by the rule and by others: 1045 and 63 queries
         // against 8208 and 192 keys, twelve heads on three, d = 128, bf16: five pieces 86, four 92, eight 98, seventeen 106; 129 queries on 14912, fp32:
-        // seventeen 51, thirty 70; 1560 queries each on 21840 and 7800, eight heads on two: three 265, eight 257, five 295.
+        // seventeen 51, thirty 70; 1560 queries each on 21840 and 7800, eight heads on two: four 263, three 265, eight 257, five 295.
+        // An eighth or half: 3 to 221 queries on eight caches of 108 to 9368, 16 heads on four, bf16 52, 71; 300 on each of 30000, 4000 and 200 135, 189; 1560 on each
+        // of two of 20280 647, 653, with eight heads on two 365, 401; but 200 on each of eight of 9000, twelve heads, d = 64 111, 101, and 300 on each of 30000,
+        // 4000 and 200, eight heads on two, fp32 284, 228.
         const int per_cu = p.dtype == DSV_F32 ? (p.d == 128 ? 1 : 2) : (p.d == 128 ? 2 : 3);
         const double at_once = 256.0 * per_cu, of_longest = (double)(most * p.Hkv), others = (double)tiles - of_longest;
         const double join = (double)p.total * p.Hq * p.d * 8.0 / 4e12 / 37e-9;  // a piece
@@ -168,9 +171,9 @@ Walk walk_of(const dsv_cache &p)
             const int64_t c = std::max<int64_t>(256, ((longest + s - 1) / s + 127) / 128 * 128);
             if (c == before) continue;
             before = c;
-            const double pieces = (double)((longest + c - 1) / c), blocks = of_longest * pieces + others * std::ceil(pieces / 2);
+            const double pieces = (double)((longest + c - 1) / c), blocks = of_longest * pieces + others * std::ceil(pieces / 8);
             const double t = std::max(1.0, std::floor(blocks / at_once + 0.9)) * ((double)c + 200.0) + (pieces > 1 ? join * pieces + 128.0 : 0.0);
-            if (s == 1 || t < 0.965 * best) {
+            if (s == 1 || t < 0.98 * best) {
                 best = t;
                 chunk = c;
             }
