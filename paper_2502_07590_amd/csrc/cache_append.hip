@@ -5,7 +5,8 @@
 //
 // Bound by memory for whole clips (two or four bytes in, one out), by latency for single tokens: a block takes one touched page of a sequence, of one or
 // several heads, and holds the new values in registers between the maximum and the rounding.  32568 tokens of 16 heads, d = 128, bf16: 98 us, 4.1 TB/s
-// (a copy of 1 GiB: 5.1); with each head's loads begun only when the one before was written, and the form of turning read at run time, 141.  Twelve single tokens: 5.5 us.
+// (a copy of 1 GiB: 5.1); with each head's loads begun only when the one before was written, and the form of turning
+// read at run time, 141.  Twelve single tokens: 5.5 us.
 #include <algorithm>
 
 #include "cache.h"
@@ -264,8 +265,8 @@ __global__ __launch_bounds__(MOST) void cache_append_kernel(AppendIn in, uint8_t
         append_page<T, D, N, kStraight>(in.turn, static_cast<const T *>(in.V), in.v_row, in.v_head, V8, vscale, a, pg, token0, begun, count, blockIdx.y, gridDim.y, red);
 }
 
-// Heads to a block, one after another with the sines that they share: as many as leave 2048 blocks of 256 lanes, or as many lanes.  32568 tokens of 16 heads, d = 128, bf16, us: in 1024
-// blocks (of both tensors together) 115, 3084 96, 4112 101, 7200 106, 15420 142.
+// Heads to a block, one after another with the sines that they share: as many as leave 2048 blocks of 256 lanes, or as many
+// lanes.  32568 tokens of 16 heads, d = 128, bf16, us: in 1024 blocks (of both tensors together) 115, 3084 96, 4112 101, 7200 106, 15420 142.
 constexpr int64_t kBlocks = 2048;
 template <typename T, int D, int N, int MOST>
 dsv_status launch_n(const CacheArgs &a, const AppendIn &in, int threads, uint8_t *K8, uint8_t *V8, float *kscale, float *vscale, hipStream_t st)

@@ -224,9 +224,9 @@ template <typename T, int D> struct PageWaves {
 
 // For blocks of 128 rows: the waves bring the bytes of the tile after next into registers while one is worked on, and widen and lay those of the next
 // into LDS, as rows loaded directly would be, between the products of this one's scores.  A load of a wave is one kilobyte of one page, so its page
-// and scales are the wave's.  Two streams of 1560 queries on 21840 and 7800 keys, eight heads on two, d = 128, bf16: 262 us a call.  Of a kernel
-// of 287 us (eight pieces, traced) the widening with its writes took 25, the loads 20, both together 67.  Bytes two tiles ahead: 265 against 257; eight waves to 256 rows, each with half of the widening: 242 to
-// 287 by how their rounds fall, against 256.
+// and scales are the wave's.  Two streams of 1560 queries on 21840 and 7800 keys, eight heads on two, d = 128, bf16: 263 us a call.  Of a kernel
+// of 287 us (eight pieces, traced) the widening with its writes took 25, the loads 20, both together 67.  Bytes two tiles ahead: 265
+// against 257; eight waves to 256 rows, each with half of the widening: 242 to 287 by how their rounds fall, against 256.
 template <typename T, int D> struct PageTiles {
     typedef FwdShape<bf16_t, D, 1> Sh;
     typedef RowTile<bf16_t, D> RT;

@@ -158,10 +158,9 @@ __device__ __forceinline__ int64_t part_row(const GatedNormArgs &a, int first) {
 // What is not there -- a modulation, Y, dH, elements past the row's end -- is held as zeros (a gate that is not there as ones), so that no element asks.
 // Past the end that leaves numbers in no sum but dg, of columns that are not written.
 template <typename T, int CH, int LPR, int NP>
-__global__ __launch_bounds__(LPR < 256 ? 256 : LPR, LPR == 512 ? 2 : NP * CH <= 8 ? 3 : NP * CH <= 16 ? 2 : 1) void gated_bwd_kernel(const T *__restrict__ X, const T *__restrict__ Y, const T *__restrict__ gate,
-                                                                                   const T *__restrict__ scale, const float4 *__restrict__ stats,
-                                                                                   const T *__restrict__ dZ, const T *dH, T *dX, T *__restrict__ dY, float *dgate,
-                                                                                   float *dscale, float *dshift, float *__restrict__ part, GatedNormArgs a)
+__global__ __launch_bounds__(LPR < 256 ? 256 : LPR, LPR == 512 ? 2 : NP * CH <= 8 ? 3 : NP * CH <= 16 ? 2 : 1) void gated_bwd_kernel(
+    const T *__restrict__ X, const T *__restrict__ Y, const T *__restrict__ gate, const T *__restrict__ scale, const float4 *__restrict__ stats,
+    const T *__restrict__ dZ, const T *dH, T *dX, T *__restrict__ dY, float *dgate, float *dscale, float *dshift, float *__restrict__ part, GatedNormArgs a)
 {
     typedef Lane<T, CH, LPR, NP> L;
     constexpr int RPB = LPR < 256 ? 256 / LPR : 1;

@@ -2,8 +2,8 @@
 //
 //   pair i of coordinate p:  t = p freq_i;  lo' = gain (lo cos t - hi sin t), hi' = gain (lo sin t + hi cos t);  back: t -> -t (the transpose)
 //
-// Bound by memory: 16-byte pieces in and out; the sines are formed once for all heads that a lane walks.  32768 tokens, 32 heads of 128 inside rows of 48, bf16: 115 us, 4.7 TB/s, where a copy of 1 GiB has 5.1; 1024 tokens, four heads of 64, fp32:
-// 4.8 us.
+// Bound by memory: 16-byte pieces in and out; the sines are formed once for all heads that a lane walks.  32768 tokens, 32 heads of 128
+// inside rows of 48, bf16: 115 us, 4.7 TB/s, where a copy of 1 GiB has 5.1; 1024 tokens, four heads of 64, fp32: 4.8 us.
 #include <algorithm>
 
 #include "rotary.h"
