@@ -110,6 +110,7 @@ bool wide_rows(int n, int dtype, std::initializer_list<Row> rows)
 }
 
 // ---- cache
+int32_t longest_cache(const dsv_cache &p) { return (int32_t)std::min<int64_t>(p.max_len, (int64_t)p.page * p.max_pages); }
 dsv_status check_cache(const dsv_cache *p)
 {
     if (!p || p->n_seq < 1 || p->total < 0 || p->max_new < 0 || p->max_len < 0 || p->flags) return DSV_EINVAL;
@@ -118,6 +119,7 @@ dsv_status check_cache(const dsv_cache *p)
     if (!(p->scale >= 1e-30f && p->scale <= 1e30f)) return DSV_EINVAL;
     if (!supported_dtype(p->dtype) || !supported_d(p->d)) return DSV_EUNSUPPORTED;
     if (p->page < 16 || p->page > 256 || (p->page & (p->page - 1)) || (int64_t)p->page * p->max_pages >= 1ll << 31) return DSV_EUNSUPPORTED;
+    if (longest_cache(*p) > 1 << 30) return DSV_EUNSUPPORTED;  // the kernels count keys in 32 bits, a piece or four tiles ahead
     if ((int64_t)p->total * p->Hq >= 1ll << 31 || (int64_t)p->total * p->Hq * (p->Hq / p->Hkv) >= 1ll << 32) return DSV_EUNSUPPORTED;
     if ((int64_t)p->total * p->Hq / 32 + (int64_t)p->n_seq * p->Hkv >= 1 << 24) return DSV_EUNSUPPORTED;
     return DSV_OK;
@@ -134,14 +136,14 @@ CacheArgs cache_args(const dsv_cache &p, const int32_t *cu, const int32_t *lens,
     a.n_seq = p.n_seq, a.total = p.total, a.max_new = std::min(p.max_new, p.total);
     a.Hkv = p.Hkv, a.n_pages = p.n_pages, a.page = p.page, a.max_pages = p.max_pages;
     while ((1 << a.page_log2) < p.page) ++a.page_log2;
-    a.max_len = std::min(p.max_len, p.page * p.max_pages);
+    a.max_len = longest_cache(p);
     return a;
 }
 // The packed forward's tiles, in pieces of their own: lengths of caches, which the kernels alone know, are anything up to the longest (blocks of a piece that
 // a cache does not reach end at once).
 Walk walk_of(const dsv_cache &p)
 {
-    const int64_t g = p.Hq / p.Hkv, longest = std::min(p.max_len, p.page * p.max_pages), own = p.total * g, max_own = (int64_t)std::min(p.max_new, p.total) * g;
+    const int64_t g = p.Hq / p.Hkv, longest = longest_cache(p), own = p.total * g, max_own = (int64_t)std::min(p.max_new, p.total) * g;
     Walk w = plan_forward(p.dtype, p.d, p.causal != 0, own, max_own, p.Hkv, p.n_seq, p.n_seq * longest, longest);
     const int64_t rows = w.few ? 32 : 128, most = (max_own + rows - 1) / rows;
     const int64_t tiles = std::min<int64_t>((int64_t)p.n_seq * most, own / rows + p.n_seq) * p.Hkv;

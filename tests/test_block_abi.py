@@ -256,6 +256,23 @@ def test_launches_of_more_lanes_than_a_grid_holds_are_refused(dsv):
     assert gated_fwd(dsv, dsv.GatedNorm(**{**GATED, **dict(tokens=1 << 24, n=32, n_seg=(1 << 24) - 1)})) == -2
 
 
+@pytest.mark.parametrize("change", [dict(page=256, max_pages=(1 << 22) + 1), dict(page=256, max_pages=(1 << 23) - 1), dict(page=16, max_pages=(1 << 27) - 1, max_len=(1 << 30) + 1)])
+def test_caches_of_more_than_2_to_the_30_tokens_are_refused(dsv, change):
+    """The kernels count keys in 32 bits, a piece of them, or a few tiles, ahead: from 2^31 - 512 tokens on (in pieces from 2^30) that passes 2^31, and a
+    negative key has a page before the table."""
+    p = dsv.Cache(**{**CACHE, **change})
+    assert append(dsv, p) == -2 and attend(dsv, p) == -2 and dsv.cache_attn_fwd_workspace(p) == 0
+
+
+@pytest.mark.parametrize("change", [dict(page=256, max_pages=1 << 22), dict(page=256, max_pages=(1 << 23) - 1, max_len=1 << 30), dict(page=16, max_pages=(1 << 27) - 1, max_len=5000)])
+def test_tables_of_more_are_not_where_max_len_says_less(dsv, change):
+    p = dsv.Cache(**{**CACHE, **change})
+    assert dsv.cache_attn_fwd_workspace(p) > 0                                               # in pieces
+    assert attend(dsv, p, ws=None, ws_bytes=0) == -3
+    none = dsv.Cache(**{**CACHE, **change, "total": 0})
+    assert append(dsv, none) == 0 and attend(dsv, none) == 0
+
+
 def test_cache_pointers_strides_and_workspaces_that_are_refused(dsv):
     p = dsv.Cache(**CACHE)
     turn = dsv.Rotary(300, 2, 128, "bf16", 64)
