@@ -509,7 +509,8 @@ DSV_API dsv_status dsv_gated_norm_bwd(const dsv_gated_norm *p, const void *X, co
  *     rows that see it NaN; a V that is not also reaches rows that causal order hides it from, up to 190 tokens away.  Finite values at or above 2^127 are cut to 448 * 2^119.
  *   - max_new, max_len: no sequence has more new tokens, or more in all (INT32_MAX: no bound but the table's).
  *   - Roundings of the attention are those of dsv_packed_attn_fwd: widening the cache is exact.  (fp32 queries and weights are multiplied as three bf16
- *     words, 24 bits; queries below 3.38e38.)  The same results from run to run, bit for bit.
+ *     words, 24 bits; queries below 3.38e38.  The weights of bf16 calls of few queries, which run in blocks of 32 rows, as two words, 16 bits.)  The
+ *     same results from run to run, bit for bit.
  *   - Limits: Hkv divides Hq; total * Hq * (Hq / Hkv) < 2^32; total * Hq / 32 + n_seq * Hkv < 2^24; page * max_pages < 2^31, and the
  *     lesser of that and max_len <= 2^30.  Workspace of the attention: for partial results of pieces of long caches, as sized from max_len. */
 typedef struct dsv_cache {

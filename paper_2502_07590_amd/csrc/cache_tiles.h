@@ -3,6 +3,10 @@
 //
 // Values of 8 bits are bf16 ones, whatever the queries' type; fp32 queries and weights go into the products as three bf16 words, 24 bits, whose
 // products with them are exact in the 32-bit sums: three bf16 products where eight of fp32 would take five times as long.
+//
+// The weights of a bf16 call: two words, 16 bits, in blocks of 32 rows, which are bound by memory (caches as below, d = 128, captured, us, two words and one: 64 of
+// 2047 .. 19948 86 and 86, twelve of 1 .. 16001 24.7 and 23.9, 24 of 6000 .. 8300 with four queries each 89.1 and 88.0; eight of 900 14.2 and 13.5); one in
+// blocks of 128, which are bound by the products (2 x 1560 queries on 21840 and 7800 332 and 263; 4 x 4096 on 32768, 32 heads on eight 12514 and 9764).
 #pragma once
 
 #include "cache.h"
@@ -61,19 +65,21 @@ template <int D> struct OwnRows<float, D> {
         }
     }
 };
-template <typename T> struct WeightWords;
-template <> struct WeightWords<bf16_t> {
-    Weights<bf16_t> w[1];
-    __device__ __forceinline__ explicit WeightWords(const Weights<bf16_t> &x) { w[0] = x; }
-};
-template <> struct WeightWords<float> {
-    Weights<bf16_t> w[3];
+// Weights as N bf16 words.
+template <int N> struct WeightWords {
+    Weights<bf16_t> w[N];
+    __device__ __forceinline__ explicit WeightWords(const Weights<bf16_t> &x)
+    {
+        static_assert(N == 1, "rounded already");
+        w[0] = x;
+    }
     __device__ __forceinline__ explicit WeightWords(const Weights<float> &x)
     {
         floatx16_t r = x.v;
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
+        for (int k = 0; k < N; ++k) {
             w[k].set(r);
+            if (k + 1 == N) break;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const uint4 h = __builtin_bit_cast(uint4, w[k].v[s]);
@@ -100,9 +106,11 @@ typedef __attribute__((address_space(3))) s32x2_t lds_s32x2_t;
 // Bound by memory: 64 caches of 2047 .. 19948, two heads, group 7, d = 128: 80 us, 4.4 TB/s (tiles that the four waves laid into LDS together: 126).
 template <typename T, int D> struct PageWaves {
     typedef FwdShape<bf16_t, D, 4> Sh;
+    typedef Weights<float> W;
     static constexpr int NK = D / 32;                  // 16-byte pieces of a key to a lane: the pieces 2 j + half, two steps of the products each
     static constexpr int PPR = D / 16, RPL = 64 / PPR; // pieces of a key, keys of a load of V
     static constexpr int WORDS = words_of(sizeof(T));
+    static constexpr int WEIGHT_WORDS = sizeof(T) == 2 ? 2 : 3;  // the second costs up to 0.8 us; a bf16 weight's rounding would be as large as O's
     struct Step {
         uint4 k[NK], v[NK];
         float ks, vs[2];
@@ -170,11 +178,11 @@ template <typename T, int D> struct PageWaves {
             }
         }
     }
-    __device__ __forceinline__ void add(const Step &st, int, const Weights<T> &weights, floatx16_t (&acc)[D / 32]) const
+    __device__ __forceinline__ void add(const Step &st, int, const W &weights, floatx16_t (&acc)[D / 32]) const
     {
         const int lane = threadIdx.x & 63, e = (lane >> 1) & 7, half = lane >> 5;
         const int r = (e < 4 ? e : 4 + e) + 4 * half, p = (lane >> 4) & 1, sub = (lane & 1) * 8;
-        const WeightWords<T> w(weights);
+        const WeightWords<WEIGHT_WORDS> w(weights);
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
@@ -182,7 +190,7 @@ template <typename T, int D> struct PageWaves {
                 const s32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_s32x2_t *)(vt + at(16 * g + r, 2 * nb + p) + sub));
                 const bf16x8_t v = widen8((uint32_t)x[0], (uint32_t)x[1], st.vs[g]);
 #pragma unroll
-                for (int k = WORDS - 1; k >= 0; --k) acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w.w[k].v[g], acc[nb], 0, 0, 0);
+                for (int k = WEIGHT_WORDS - 1; k >= 0; --k) acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w.w[k].v[g], acc[nb], 0, 0, 0);
             }
     }
     template <typename Scores, typename Rest>
@@ -230,6 +238,7 @@ template <typename T, int D> struct PageWaves {
 template <typename T, int D> struct PageTiles {
     typedef FwdShape<bf16_t, D, 1> Sh;
     typedef RowTile<bf16_t, D> RT;
+    typedef Weights<T> W;
     static constexpr int WORDS = words_of(sizeof(T));
     static constexpr int RPL = 1024 / D, PPR = D / 16;     // tokens of a load, 16-byte pieces of a token
     static constexpr int N = Sh::KEYS / RPL / 4;           // loads of a wave for a tile of K, and of V
@@ -324,10 +333,10 @@ template <typename T, int D> struct PageTiles {
         }
     }
     // as weighted_rows(), every operand for all words of the weights
-    __device__ __forceinline__ void add(const unsigned char *vt, int r0, const Weights<T> &weights, floatx16_t (&acc)[D / 32]) const
+    __device__ __forceinline__ void add(const unsigned char *vt, int r0, const W &weights, floatx16_t (&acc)[D / 32]) const
     {
         typedef RowSum<bf16_t, D> RS;
-        const WeightWords<T> w(weights);
+        const WeightWords<WORDS> w(weights);
         typename RS::Operand f[RS::AHEAD];
 #pragma unroll
         for (int i = 0; i < RS::AHEAD; ++i) f[i] = RS::fetch(vt, r0, i);

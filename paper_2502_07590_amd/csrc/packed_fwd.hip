@@ -21,6 +21,7 @@ namespace {
 // Tiles loaded directly into LDS from rows of the caller's tensors.
 template <typename T, int D, int WK> struct RowTiles {
     typedef FwdShape<T, D, WK> Sh;
+    typedef Weights<T> W;
     const T *K, *V;
     const unsigned char *kp, *vp;
     int nk;
@@ -82,6 +83,7 @@ template <typename T, int D, int WK> struct RowTiles {
 __device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? kNegInf : (m + __builtin_amdgcn_logf(l)) * kLn2; }
 
 // A: the descriptor, with read_sequence() of its own.  Tiles: brings tiles of keys into LDS,
+//   W: the weights, as add() takes them: Weights<bf16_t>, rounded, or Weights<float>
 //   piece(m, half): which 16 bytes of Q a half of the wave holds for step m of the scores
 //   begin(a, sequence's number, sequence, head of K and V, wave, own rows)
 //   walk(a, first key, key behind the last, two tiles of K and V each (for NBUF = 1 the second two are not there), scores(K tile, s), rest(key, s, V tile)),
@@ -93,6 +95,7 @@ __device__ __forceinline__ void attend(const T *__restrict__ Q, T *__restrict__ 
     typedef RowTile<T, D> RT;
     typedef typename Tiles::Sh Sh;
     constexpr int NM = RT::RB / 32, NB = D / 32, KT = Sh::KT;
+    constexpr bool kRounded = std::is_same<typename Tiles::W, Weights<bf16_t>>::value;  // the weights, to one bf16 word
     // every tile an array of its own: reads of one then need not wait for the loads into another
     __shared__ __align__(1024) unsigned char ka[Sh::TILE], va[Sh::TILE], kb[Sh::NBUF == 2 ? Sh::TILE : 16], vb[Sh::NBUF == 2 ? Sh::TILE : 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -166,9 +169,9 @@ __device__ __forceinline__ void attend(const T *__restrict__ Q, T *__restrict__ 
                 s[t][i] = fast_exp2(fmaf(s[t][i], c, -mref));
                 lt += s[t][i];
             }
-            Weights<T> w;
+            typename Tiles::W w;
             w.set(s[t]);
-            if constexpr (sizeof(T) == 2) lrt = w.sum(lrt);
+            if constexpr (kRounded) lrt = w.sum(lrt);
             tiles.add(vt, sub + 32 * t, w, acc);
         }
         l += lt;
@@ -176,10 +179,10 @@ __device__ __forceinline__ void attend(const T *__restrict__ Q, T *__restrict__ 
     };
     if (kbeg < kend) tiles.walk(a, kbeg, kend, ka, va, kb, vb, scores, rest);
     l = halves_sum(l);
-    // Weights go into the product as one bf16 word: a second one, as the sparse forward has it, would make three products of two, in a kernel bound by
-    // their power.  O is the average by the weights that were summed, lse the logarithm of the unrounded ones': rounding then moves weight between the keys and
+    // Rounded weights go into the product as one bf16 word: a second one, as the sparse forward has it, would make three products of two, in kernels bound by
+    // their power.  O is then the average by the weights that were summed, lse the logarithm of the unrounded ones': rounding then moves weight between the keys and
     // adds none (bf16, against 64 bits: O 2.4e-3 off when divided by l, 1.9e-3 by lr, 1.7e-3 the rounding of O alone)
-    const float whole = sizeof(T) == 2 ? halves_sum(lr) : l, fair = whole == 0.f ? 0.f : l / whole;
+    const float whole = kRounded ? halves_sum(lr) : l, fair = whole == 0.f ? 0.f : l / whole;
     if constexpr (WK > 1) {  // the waves' sums over their keys, joined in LDS: wave w then holds channels 32 w / 4 .. of every row
         __shared__ float sm[128], sl[128];
         auto area = [&](int w) __attribute__((always_inline)) {  // 32 rows of D sums
