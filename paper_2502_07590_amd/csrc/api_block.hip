@@ -144,7 +144,8 @@ CacheArgs cache_args(const dsv_cache &p, const int32_t *cu, const int32_t *lens,
 Walk walk_of(const dsv_cache &p)
 {
     const int64_t g = p.Hq / p.Hkv, longest = longest_cache(p), own = p.total * g, max_own = (int64_t)std::min(p.max_new, p.total) * g;
-    Walk w = plan_forward(p.dtype, p.d, p.causal != 0, own, max_own, p.Hkv, p.n_seq, p.n_seq * longest, longest);
+    Walk w{};
+    w.few = few_rows(own, p.Hkv, p.n_seq, longest);
     const int64_t rows = w.few ? 32 : 128, most = (max_own + rows - 1) / rows;
     const int64_t tiles = std::min<int64_t>((int64_t)p.n_seq * most, own / rows + p.n_seq) * p.Hkv;
     int64_t chunk = longest;
@@ -157,24 +158,34 @@ Walk walk_of(const dsv_cache &p)
         if (longest > (p.dtype == DSV_F32 && p.d == 128 ? 512 : 1024))
             chunk = std::max(tiles * longest / 2048, std::min<int64_t>(512, std::max<int64_t>(256, tiles * longest / 512)));
     } else if (longest > 0) {
-        // Rounds of blocks, the sequence of most queries taken to have the longest cache and the others an eighth of it; a tenth of a round more costs none.
-        // Times in keys a block walks (37 ns), 200 to begin and to end.  us, by the rule and by others: 1045 and 63 queries
-        // against 8208 and 192 keys, twelve heads on three, d = 128, bf16: five pieces 86, four 92, eight 98, seventeen 106; 129 queries on 14912, fp32:
-        // seventeen 51, thirty 70; 1560 queries each on 21840 and 7800, eight heads on two: four 263, three 265, eight 257, five 295.
-        // An eighth or half: 3 to 221 queries on eight caches of 108 to 9368, 16 heads on four, bf16 52, 71; 300 on each of 30000, 4000 and 200 135, 189; 1560 on each
-        // of two of 20280 647, 653, with eight heads on two 365, 401; but 200 on each of eight of 9000, twelve heads, d = 64 111, 101, and 300 on each of 30000,
-        // 4000 and 200, eight heads on two, fp32 284, 228.
-        const int per_cu = p.dtype == DSV_F32 ? (p.d == 128 ? 1 : 2) : (p.d == 128 ? 2 : 3);
-        const double at_once = 256.0 * per_cu, of_longest = (double)(most * p.Hkv), others = (double)tiles - of_longest;
-        const double join = (double)p.total * p.Hq * p.d * 8.0 / 4e12 / 37e-9;  // a piece
+        // Time in keys that a block walks: those of a piece and 100 to begin and to end, times the rounds of all blocks, each counted by the keys it has; and
+        // the join.  Rounds lie between the whole ones and as many as the blocks fill, with 0.6 for those that end late.  The sequence of most queries is taken
+        // to have the longest cache; of the others nothing is known, so nine parts of the time with an eighth of it for each stand beside one with all of it.
+        // us by the rule, in one piece and at best of 1 to 64, bf16, d = 128 unless said: 32 x 256 queries on 8000, 32 heads on eight: 1149 (one piece); 4 x 4096 on
+        // 32768: 9310 (one), two pieces 9220; 8 x 1560 on 21840, 16 heads on 16: 2659 (five), 2777, 2591, on four: 2456 (four), 2701; 2 x 1560 on
+        // 20280, 16 on four: 638 (four), 669, 602, eight on two: 331 (nine), 479, 309; in fp32 774 (nine), 845, 725; 2 x 1560 on 21840 and 7800, eight on
+        // two: 251 (nine), 508, 244; 300 on each of 30000, 4000 and 200, 16 on four: 129 (ten), 713; eight on two, fp32: 225 (twenty), 1217; 3 to 221
+        // on eight of 108 to 9368, 16 on four: 77 (eleven), 230, 65; 8 x 200 on 9000, twelve on three, d = 64: 85 (nine), 158; 1045 and 63 on 8208 and
+        // 192, twelve on three: 85 (five), 200; 129 on 14912, 16 on four, fp32: 72 (twelve), 604.  78 calls, most of them drawn: 4.7 % from the best in the mean, 22 at most;
+        // a rule that charged every block the longest, whatever its keys, 8.9 and 33.  70 others: 0.98 of that rule's time in the mean, 0.57 to 1.23.
+        const bool bf16 = p.dtype == DSV_BF16;
+        const int per_cu = !bf16 ? (p.d == 128 ? 1 : 2) : (p.d == 128 ? 2 : 3);
+        const double key = 1e-9 * (bf16 ? (p.d == 128 ? 37 : 32) : (p.d == 128 ? 41 : 44));  // seconds, a block among others
+        const double at_once = 256.0 * per_cu, of_longest = (double)(most * p.Hkv), others = std::max(0.0, (double)tiles - of_longest), ends = 100;
+        const double join = (double)p.total * p.Hq * p.d * 8.0 / 5.7e12 / key;  // a piece, written and read
         double best = 0;
         int64_t before = 0;
         for (int64_t s = 1; s <= 64; ++s) {
             const int64_t c = std::max<int64_t>(256, ((longest + s - 1) / s + 127) / 128 * 128);
             if (c == before) continue;
             before = c;
-            const double pieces = (double)((longest + c - 1) / c), blocks = of_longest * pieces + others * std::ceil(pieces / 8);
-            const double t = std::max(1.0, std::floor(blocks / at_once + 0.9)) * ((double)c + 200.0) + (pieces > 1 ? join * pieces + 128.0 : 0.0);
+            const int64_t pieces = (longest + c - 1) / c;
+            const double walk = (double)std::min(c, longest) + ends;
+            auto rounds = [&](double part) {  // the others' caches: so much of the longest
+                const double keys = part * (double)longest, x = (of_longest * (double)pieces + others * (keys + ends * std::ceil(keys / (double)c)) / walk) / at_once;
+                return std::max(1.0, 0.5 * (std::ceil(x) + x + 0.6));
+            };
+            const double t = (0.9 * rounds(0.125) + 0.1 * rounds(1.0)) * walk + (pieces > 1 ? join * (double)pieces + 128.0 : 0.0);
             if (s == 1 || t < 0.98 * best) {
                 best = t;
                 chunk = c;
@@ -186,9 +197,8 @@ Walk walk_of(const dsv_cache &p)
     w.splits = w.chunk ? (int)((longest + chunk - 1) / chunk) : 1;
     return w;
 }
-size_t cache_fwd_bytes(const dsv_cache &p)
+size_t cache_fwd_bytes(const dsv_cache &p, const Walk &w)
 {
-    const Walk w = walk_of(p);
     return w.splits > 1 ? packed_fwd_acc_bytes(p.total, p.Hq, p.d, w.splits) + align_up((size_t)p.total * p.Hq * w.splits * 8, 256) : 0;
 }
 }  // namespace
@@ -284,7 +294,7 @@ dsv_status dsv_cache_append(const dsv_cache *p, const dsv_rotary *turn, const vo
 size_t dsv_cache_attn_fwd_workspace(const dsv_cache *p)
 {
     if (check_cache(p) != DSV_OK) return 0;
-    return cache_fwd_bytes(*p);
+    return cache_fwd_bytes(*p, walk_of(*p));
 }
 
 dsv_status dsv_cache_attn_fwd(const dsv_cache *p, const void *Q, const int32_t *cu, const int32_t *lens, const int32_t *table, const void *K8, const void *V8,
@@ -295,10 +305,10 @@ dsv_status dsv_cache_attn_fwd(const dsv_cache *p, const void *Q, const int32_t *
     if (!ok_cache(cu, lens, table, K8, V8, kscale, vscale) || !on_elements({lse}, 4)) return DSV_EINVAL;
     if (!ok_strides(p->q, esize(p->dtype)) || !ok_strides(p->o, esize(p->dtype)) || !rows_apart(p->o, p->total, p->Hq, p->d)) return DSV_EINVAL;
     if (p->total > 0 && (!ok_ptrs({Q, O}) || !lse)) return DSV_EINVAL;
-    st = check_workspace(workspace, ws_bytes, cache_fwd_bytes(*p));
+    const Walk w = walk_of(*p);
+    st = check_workspace(workspace, ws_bytes, cache_fwd_bytes(*p, w));
     if (st != DSV_OK) return st;
     if (p->total == 0) return DSV_OK;
-    const Walk w = walk_of(*p);
     const int64_t es = (int64_t)esize(p->dtype);
     CachedArgs a{};
     a.cu_q = cu;

@@ -80,14 +80,11 @@ struct StepCost {
 };
 Walk plan_walk(const StepCost &cost, int d, bool causal, int64_t own, int64_t max_own, int64_t heads, int64_t n_seq, int64_t other, int64_t max_other)
 {
-    constexpr int64_t kUnit = 128, kMinChunk = 256, kMaxSplits = 64, kCus = 256;
+    constexpr int64_t kUnit = 128, kMaxSplits = 64;
     Walk w{};
     w.splits = 1;
     const int64_t pieces = std::max<int64_t>(1, max_other / kMinChunk);
-    // Small tiles where the mean sequence would leave large ones half empty, or those would not fill the chip even in the shortest pieces.  By the
-    // mean, so a long sequence among many short ones goes to small tiles with them: 8192 tokens beside 255 sequences of one, eight heads, d = 128,
-    // bf16, take 513 us forward and 1908 backward, and 141 and 277 MB of workspace; apart, 301 + 23 and 965 + 91 us, and none and 0.5 MB.
-    w.few = own / n_seq <= 64 || (own / 128 + 1) * heads * pieces < kCus;
+    w.few = few_rows(own, heads, n_seq, max_other);
     int64_t chunk = max_other;
     const double rest = (double)(n_seq - 1), longest = (double)std::max<int64_t>(max_other, 1);
     const double rest_own = (double)std::max<int64_t>(own - max_own, 0), rest_other = n_seq > 1 ? (double)std::max<int64_t>(other - max_other, 0) / rest : 0.0;
@@ -156,33 +153,18 @@ Walk plan_walk(const StepCost &cost, int d, bool causal, int64_t own, int64_t ma
     return w;
 }
 enum Step { kFwd, kDq, kDkdv };
-StepCost step_cost(int dtype, int d, Step step)
+Walk walk_of(const dsv_packed &p, Step step)
 {
-    const bool bf16 = dtype == DSV_BF16;
+    const bool bf16 = p.dtype == DSV_BF16;
+    const int64_t g = p.Hq / p.Hkv;
     // operations a pair and channel, and rates: as measured at 32768 tokens.  (fp32 dK and dV: those of blocks of 128 keys, where launch_dkdv runs blocks
     // of 32, one a CU: four times as many as counted, and so more pieces than they need.)
     StepCost c{};
     c.bf16 = bf16;
-    c.per_cu = step == kDkdv ? (d == 64 ? 2 : 1) : bf16 ? (d == 64 ? 3 : 2) : (d == 64 ? 2 : 1);
+    c.per_cu = step == kDkdv ? (p.d == 64 ? 2 : 1) : bf16 ? (p.d == 64 ? 3 : 2) : (p.d == 64 ? 2 : 1);
     c.flops = step == kFwd ? 4 : 8;
     c.rate = bf16 ? 1.1e15 : 1e14;
     c.results = step == kDkdv ? 2 : 1;
-    return c;
-}
-}  // namespace
-
-Walk plan_forward(int dtype, int d, bool causal, int64_t own, int64_t max_own, int64_t heads, int64_t n_seq, int64_t other, int64_t max_other)
-{
-    return plan_walk(step_cost(dtype, d, kFwd), d, causal, own, max_own, heads, n_seq, other, max_other);
-}
-
-namespace {
-Walk walk_of(const dsv_packed &p, Step step)
-{
-    const int64_t g = p.Hq / p.Hkv;
-    if (step == kFwd)
-        return plan_forward(p.dtype, p.d, p.causal != 0, (int64_t)p.total_q * g, std::min(p.max_q, p.total_q) * g, p.Hkv, p.n_seq, p.total_k, std::min(p.max_k, p.total_k));
-    const StepCost c = step_cost(p.dtype, p.d, step);
     if (step == kDkdv)
         return plan_walk(c, p.d, p.causal != 0, p.total_k, std::min(p.max_k, p.total_k), p.Hkv, p.n_seq, (int64_t)p.total_q * g, std::min(p.max_q, p.total_q) * g);
     return plan_walk(c, p.d, p.causal != 0, (int64_t)p.total_q * g, std::min(p.max_q, p.total_q) * g, p.Hkv, p.n_seq, p.total_k, std::min(p.max_k, p.total_k));

@@ -73,3 +73,24 @@ def test_workspaces_hold_every_piece(plan):
         assert keys % 128 == 0 and (pieces - 1) * keys < longest <= pieces * keys and longest + keys < 2 ** 31, c
         assert rows * pieces * (d + 2) * 4 <= ws <= rows * pieces * (d + 2) * 4 + 512, c
     assert split > 200
+
+
+def equal(n, new, length, Hq, Hkv, d=128, dtype="bf16"):
+    return described([new] * n, [length] * n, Hq, Hkv, d, 64, dtype, max_len=length)
+
+
+def test_calls_that_fill_the_chip_are_not_cut_into_pieces(plan):
+    """Batches of one size whose blocks of 128 rows fill the chip four times over: pieces would save nothing, and leave hundreds of MB to write and to join."""
+    for c in (equal(32, 256, 8000, 32, 8), equal(4, 4096, 32768, 32, 8), equal(12, 3400, 5000, 32, 8), equal(4, 2000, 1500, 12, 12, dtype="f32"), equal(32, 1142, 1684, 12, 4, dtype="f32"),
+              equal(16, 1560, 4000, 16, 16, d=64)):
+        assert plan([c]) == [(0, 1, 0, 0)], c
+    # three times over: the last round is worth a few
+    assert all(pieces <= 5 for _, pieces, *_ in plan([equal(8, 1560, 21840, 16, 16), equal(8, 1560, 21840, 16, 4)]))
+
+
+def test_long_caches_that_leave_the_chip_empty_are_cut(plan):
+    """One long cache among short ones, and a few long ones: blocks for all CUs."""
+    calls = [described([300] * 3, [30000, 4000, 200], 16, 4, 128, 64, "bf16", max_len=30000), described([1560] * 2, [21840, 7800], 8, 2, 128, 64, "bf16", max_len=21840),
+             described([129], [14912], 16, 4, 128, 64, "f32", max_len=14912), described([1045, 63], [8208, 192], 12, 3, 128, 64, "bf16", max_len=8208)]
+    for (few, pieces, *_), (at_least, at_most) in zip(plan(calls), ((8, 24), (4, 12), (10, 12), (4, 6))):
+        assert not few and at_least <= pieces <= at_most
