@@ -448,7 +448,7 @@ DSV_API dsv_status dsv_rotary_freqs(int32_t pairs, double base, int32_t scaling,
  *     dgate = sum dh u,  dscale = sum dZ xh,  dshift = sum dZ  over the rows of a segment
  *
  *   - X, Y, H, Z, dZ, dH, dX, dY: [tokens, n], each with its stride from row to row, of any alignment (rows that begin on 16 bytes and fill
- *     whole ones are read 16 bytes at a time).  gate, scale, shift: [n_seg, n] in `dtype`, each with its stride (chunks of one projection's
+ *     whole ones are read 16 bytes at a time); strides of tensors that are NULL are not looked at.  gate, scale, shift: [n_seg, n] in `dtype`, each with its stride (chunks of one projection's
  *     output), or NULL (1, 0, 0).  Y NULL: h = residual * x, and H, gate, dY, dgate are NULL too; dH NULL: zero.
  *     tokens = 0: nothing is written but zeros to dgate, dscale, dshift, and the tensors of rows may be NULL.
  *   - cu: DEVICE int32 [n_seg + 1], ascending from 0, read by the kernels only, as for packed attention: segment s has rows cu[s] .. cu[s+1] - 1,

@@ -67,7 +67,7 @@ dsv_status run_rotary(const dsv_rotary *p, bool back, const void *X, const int32
 }
 
 // ---- gated norm
-dsv_status check_gated(const dsv_gated_norm *p, bool grad)
+dsv_status check_gated(const dsv_gated_norm *p)
 {
     if (!p) return DSV_EINVAL;
     if (p->tokens < 0 || p->n < 1 || p->n_seg < 1 || p->flags) return DSV_EINVAL;
@@ -75,14 +75,24 @@ dsv_status check_gated(const dsv_gated_norm *p, bool grad)
     if ((p->post != 0 && p->post != 1) || !std::isfinite(p->eps) || !(p->eps >= 0.f) || !std::isfinite(p->residual)) return DSV_EINVAL;
     if (!supported_dtype(p->dtype) || p->n > kMaxNormWidth) return DSV_EUNSUPPORTED;
     if ((int64_t)p->n_seg * ((p->n + 31) / 32) >= (1 << 24) - (1 << 16)) return DSV_EUNSUPPORTED;  // blocks of a launch: as many, or one a segment and 32768
-    for (int64_t s : {p->x, p->y, p->gate, p->scale, grad ? p->dz : p->h, grad ? p->dh : p->z, grad ? p->dx : p->shift, grad ? p->dy : 0, grad ? p->dgate : 0,
-                      grad ? p->dscale : 0, grad ? p->dshift : 0})
-        if (!ok_stride(s)) return DSV_EINVAL;
-    for (int64_t s : {grad ? p->dx : p->z, grad ? p->dy : p->h})  // outputs: rows apart
-        if (p->tokens > 1 && s < p->n) return DSV_EINVAL;
-    for (int64_t s : {p->dgate, p->dscale, p->dshift})
-        if (grad && p->n_seg > 1 && s < p->n) return DSV_EINVAL;
     return DSV_OK;
+}
+struct Row {
+    const void *p;
+    int64_t stride;
+};
+// Strides of the tensors that are there.  Outputs: `rows` of n elements apart.
+bool ok_inputs(std::initializer_list<Row> in)
+{
+    for (const Row &r : in)
+        if (r.p && !ok_stride(r.stride)) return false;
+    return true;
+}
+bool ok_outputs(int rows, int n, std::initializer_list<Row> out)
+{
+    for (const Row &r : out)
+        if (r.p && (!ok_stride(r.stride) || (rows > 1 && r.stride < n))) return false;
+    return true;
 }
 GatedNormArgs gated_args(const dsv_gated_norm &p, const int32_t *cu)
 {
@@ -95,10 +105,6 @@ GatedNormArgs gated_args(const dsv_gated_norm &p, const int32_t *cu)
     a.dz = p.dz, a.dh = p.dh, a.dx = p.dx, a.dy = p.dy, a.dgate = p.dgate, a.dscale = p.dscale, a.dshift = p.dshift;
     return a;
 }
-struct Row {
-    const void *p;
-    int64_t stride;
-};
 // whether every tensor's rows begin on 16 bytes and fill whole ones
 bool wide_rows(int n, int dtype, std::initializer_list<Row> rows)
 {
@@ -240,8 +246,9 @@ dsv_status dsv_rotary_freqs(int32_t pairs, double base, int32_t scaling, double 
 dsv_status dsv_gated_norm_fwd(const dsv_gated_norm *p, const void *X, const void *Y, const int32_t *cu, const void *gate, const void *scale, const void *shift,
                               void *Z, void *H, float *stats, void *hip_stream)
 {
-    const dsv_status st = check_gated(p, false);
+    const dsv_status st = check_gated(p);
     if (st != DSV_OK) return st;
+    if (!ok_inputs({{X, p->x}, {Y, p->y}, {gate, p->gate}, {scale, p->scale}, {shift, p->shift}}) || !ok_outputs(p->tokens, p->n, {{Z, p->z}, {H, p->h}})) return DSV_EINVAL;
     if (!cu || !on_elements({cu}, 4) || !aligned16(stats) || !on_elements({X, Y, gate, scale, shift, Z, H}, esize(p->dtype))) return DSV_EINVAL;
     if (p->tokens > 0 && !Y && (H || gate || p->post)) return DSV_EINVAL;
     if (p->tokens > 0 && (!X || !Z || !stats || (Y && !H))) return DSV_EINVAL;
@@ -253,7 +260,7 @@ dsv_status dsv_gated_norm_fwd(const dsv_gated_norm *p, const void *X, const void
 
 size_t dsv_gated_norm_bwd_workspace(const dsv_gated_norm *p)
 {
-    if (check_gated(p, true) != DSV_OK) return 0;
+    if (check_gated(p) != DSV_OK) return 0;
     return gated_bwd_bytes(p->tokens, p->n, p->n_seg, p->dtype);
 }
 
@@ -261,8 +268,10 @@ dsv_status dsv_gated_norm_bwd(const dsv_gated_norm *p, const void *X, const void
                               const void *dZ, const void *dH, void *dX, void *dY, float *dgate, float *dscale, float *dshift, void *workspace, size_t ws_bytes,
                               void *hip_stream)
 {
-    dsv_status st = check_gated(p, true);
+    dsv_status st = check_gated(p);
     if (st != DSV_OK) return st;
+    if (!ok_inputs({{X, p->x}, {Y, p->y}, {gate, p->gate}, {scale, p->scale}, {dZ, p->dz}, {dH, p->dh}})) return DSV_EINVAL;
+    if (!ok_outputs(p->tokens, p->n, {{dX, p->dx}, {dY, p->dy}}) || !ok_outputs(p->n_seg, p->n, {{dgate, p->dgate}, {dscale, p->dscale}, {dshift, p->dshift}})) return DSV_EINVAL;
     if (!cu || !on_elements({cu, dgate, dscale, dshift}, 4) || !aligned16(stats) || !on_elements({X, Y, gate, scale, dZ, dH, dX, dY}, esize(p->dtype))) return DSV_EINVAL;
     if (p->tokens > 0 && !Y && (gate || dY || dgate || p->post)) return DSV_EINVAL;
     if (p->tokens > 0 && (!X || !stats || !dZ || !dX || (Y && !dY))) return DSV_EINVAL;

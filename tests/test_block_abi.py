@@ -192,6 +192,34 @@ def test_gated_pointers_and_strides_that_are_refused(dsv):
         dsv.GatedNorm(**{**GATED, "kind": "batch"})
 
 
+def test_strides_of_gated_tensors_that_are_not_there_are_not_looked_at(dsv):
+    """A descriptor whose fields for NULL tensors were left at zero, or hold anything.  The calls end at a check behind that of the strides: a workspace that is
+    too small."""
+    forward, backward = ("x", "y", "z", "h", "gate", "scale", "shift"), ("x", "y", "gate", "scale", "dz", "dh", "dx", "dy", "dgate", "dscale", "dshift")
+    big = {**GATED, "tokens": 100000}
+    for left in (0, -5, 1 << 50):
+        def descriptor(there, **more):
+            p = dsv.GatedNorm(**{**big, **more})
+            for name in forward + backward:
+                if name not in there:
+                    setattr(p._c, name, left)
+            return p
+
+        # no block output: its stream, gate and gradients are not there
+        p = descriptor(("x", "z", "scale", "shift", "dz", "dh", "dx", "dscale", "dshift"))
+        need = dsv.gated_norm_bwd_workspace(p)
+        assert need == dsv.gated_norm_bwd_workspace(dsv.GatedNorm(**big)) > 0
+        assert gated_bwd(dsv, p, [ONE, None, ONE, None, ONE, ONE, ONE, ONE, ONE, None, None, ONE, ONE], ws_bytes=need - 1) == -3
+        # no modulation wanted but one, and nothing that comes back to h
+        p = descriptor(("x", "y", "dz", "dx", "dy", "dshift"))
+        assert gated_bwd(dsv, p, [ONE, ONE, ONE, None, None, ONE, ONE, None, ONE, ONE, None, None, ONE], ws_bytes=need - 1) == -3
+        assert gated_bwd(dsv, p, [ONE, ONE, ONE, None, None, ONE, ONE, None, ONE, ONE, ONE, None, ONE], ws_bytes=need - 1) == -1
+        # no rows at all
+        p = descriptor((), tokens=0)
+        assert gated_fwd(dsv, p, [None, None, ONE] + [None] * 6) == 0
+        assert gated_bwd(dsv, p, [None, None, ONE] + [None] * 10, ws=None, ws_bytes=0) == 0
+
+
 @pytest.mark.parametrize("kind", ["layer", "rms"])
 @pytest.mark.parametrize("post", [False, True])
 def test_the_gated_reference(kind, post):
