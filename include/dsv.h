@@ -454,7 +454,8 @@ DSV_API dsv_status dsv_rotary_freqs(int32_t pairs, double base, int32_t scaling,
  *   - cu: DEVICE int32 [n_seg + 1], ascending from 0, read by the kernels only, as for packed attention: segment s has rows cu[s] .. cu[s+1] - 1,
  *     which may be none.  Rows of no segment are left as they are in every output.  Other entries: undefined results, no access outside.
  *   - stats: float [tokens, 4], on 16 bytes: mean and 1 / deviation of h, and of y (0 without post); the forward writes them for the backward.
- *   - The backward forms h from X and Y (the unrounded one that the forward normed), so H need not be kept for it.
+ *   - The backward forms h from X and Y (the unrounded one that the forward normed), so H need not be kept for it, and X has to be: the X and Y
+ *     that the forward read.  A forward with H in X's place leaves no X for a backward: for samplers, or with a copy of X kept.
  *   - dgate, dscale, dshift: float [n_seg, n], each with its stride, each NULL where it is not wanted; zeros for a segment of no rows.
  *   - H may be X, and dX may be dH, with the same stride (in place); no output may overlap an input otherwise, nor another output.
  *   - n <= 8192; n_seg * ceil(n / 32) < 2^24 (larger: DSV_EUNSUPPORTED); eps >= 0, residual finite.
@@ -506,7 +507,8 @@ DSV_API dsv_status dsv_gated_norm_bwd(const dsv_gated_norm *p, const void *X, co
  *   - Entries of cu, lens or table out of their range give undefined results but no access outside the tensors.  Table entries of pages that
  *     lens does not reach are not used.
  *   - Finite inputs are assumed; a value that is not becomes NaN in the cache and leaves the page's scale alone.  A K that is not finite makes the
- *     rows that see it NaN; a V that is not also reaches rows that causal order hides it from, up to 190 tokens away.  Finite values at or above 2^127 are cut to 448 * 2^119.
+ *     rows that see it NaN; a V that is not also reaches rows that causal order hides it from, up to 190 tokens away.  Finite values above
+ *     448 * 2^119 are cut to it; a K that its turn (its length, times the gain) takes past the largest float is not finite.
  *   - max_new, max_len: no sequence has more new tokens, or more in all (INT32_MAX: no bound but the table's).
  *   - Roundings of the attention are those of dsv_packed_attn_fwd: widening the cache is exact.  (fp32 queries and weights are multiplied as three bf16
  *     words, 24 bits; queries below 3.38e38.  The weights of bf16 calls of few queries, which run in blocks of 32 rows, as two words, 16 bits.)  The

@@ -845,7 +845,8 @@ def _made(like, *shape, dtype=None):
 
 def gated_norm_fwd(p: GatedNorm, X, cu, Y=None, gate=None, scale=None, shift=None, Z=None, H=None, stats=None, stream=None):
     """(Z, H, stats) of h = residual X + gate Y, z = norm(h) (1 + scale) + shift.  X, Y [tokens, n], gate, scale, shift [n_seg, n] or None, any strides
-    between rows; cu int32 [n_seg + 1] on the device.  Without Y there is no H (None).  H may be X.  stats (float [tokens, 4]): for the backward."""
+    between rows; cu int32 [n_seg + 1] on the device.  Without Y there is no H (None).  H may be X where no backward follows, or a copy of X is kept
+    for it.  stats (float [tokens, 4]): for the backward."""
     lib = load_library()
     with _On(X, stream) as on:
         dev, td, c, shape, mod = X.device, p.torch_dtype, _CGatedNorm.from_buffer_copy(p._c), p.shape, p.mod_shape
@@ -864,8 +865,8 @@ def gated_norm_bwd_workspace(p: GatedNorm) -> int:
 
 def gated_norm_bwd(p: GatedNorm, X, cu, stats, dZ, Y=None, gate=None, scale=None, dH=None, dX=None, dY=None, dgate=None, dscale=None, dshift=None,
                    workspace=None, stream=None):
-    """(dX, dY, dgate, dscale, dshift) of gated_norm_fwd; dY None without Y.  dgate, dscale, dshift float [n_seg, n]: made where gate, and where scale, was
-    given, and filled where they were passed; else None.  dX may be dH."""
+    """(dX, dY, dgate, dscale, dshift) of gated_norm_fwd, from the X and Y that it read (not an X that its H was written over); dY None without Y.
+    dgate, dscale, dshift float [n_seg, n]: made where gate, and where scale, was given, and filled where they were passed; else None.  dX may be dH."""
     lib = load_library()
     with _On(X, stream) as on:
         dev, td, c, shape, mod, f32 = X.device, p.torch_dtype, _CGatedNorm.from_buffer_copy(p._c), p.shape, p.mod_shape, torch.float32
