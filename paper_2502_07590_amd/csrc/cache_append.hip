@@ -5,7 +5,7 @@
 //
 // Bound by memory for whole clips (two or four bytes in, one out), by latency for single tokens: a block takes one touched page of a sequence, of one or
 // several heads, and holds the new values in registers between the maximum and the rounding.  32568 tokens of 16 heads, d = 128, bf16: 98 us, 4.1 TB/s
-// (a copy of 1 GiB: 5.1); with each head's loads begun only when the one before was written, and the form of turning
+// (a copy of 1 GiB: 5.1), in fp32 136, 4.9; with each head's loads begun only when the one before was written, and the form of turning
 // read at run time, 141.  Twelve single tokens: 5.5 us.
 #include <algorithm>
 
@@ -286,8 +286,9 @@ dsv_status launch_d(const CacheArgs &a, const AppendIn &in, uint8_t *K8, uint8_t
 {
     int rows = 1;  // new ones of a page, at most
     while (rows < std::min(a.page, a.max_new)) rows *= 2;
-    // A lane holds two sixteens at most.  Pages of 256, 20900 tokens of 16 heads, bf16, us: in 1024 lanes 74, in 256 of eight sixteens each 151; pairs that lie
-    // anywhere 229, 592.
+    // A lane holds two sixteens at most.  Pages of 256, 20900 tokens of 16 heads, bf16, us a call: in 1024 lanes 74, in 256 of eight sixteens each 151; pairs that
+    // lie anywhere 229, 592 (captured, in 1024 lanes: 60, 204).  1024 lanes leave 128 registers each: of pairs that lie anywhere 155 are spilled (fp32
+    // 176; of pairs in eights 12 in fp32).
     const int jobs = rows * (D / 16);
     if (jobs <= 256) return launch_n<T, D, 1, 256>(a, in, std::max(64, jobs), K8, V8, kscale, vscale, st);
     if (jobs <= 512) return launch_n<T, D, 2, 256>(a, in, 256, K8, V8, kscale, vscale, st);

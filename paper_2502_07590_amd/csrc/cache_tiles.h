@@ -103,7 +103,7 @@ typedef __attribute__((address_space(3))) s32x2_t lds_s32x2_t;
 
 // For blocks of 32 rows whose four waves share the keys: every wave reads 32 keys of its own, K straight into the products' registers, V by way of
 // LDS of its own, turned there; no wave waits for another.  The next 32 keys' bytes, and the pages of those after them, are on their way meanwhile.
-// Bound by memory: 64 caches of 2047 .. 19948, two heads, group 7, d = 128: 80 us, 4.4 TB/s (tiles that the four waves laid into LDS together: 126).
+// Bound by memory: 64 caches of 2047 .. 19948, two heads, group 7, d = 128: 81 us, 4.3 TB/s (tiles that the four waves laid into LDS together: 126).
 template <typename T, int D> struct PageWaves {
     typedef FwdShape<bf16_t, D, 4> Sh;
     typedef Weights<float> W;
@@ -232,7 +232,7 @@ template <typename T, int D> struct PageWaves {
 
 // For blocks of 128 rows: the waves bring the bytes of the tile after next into registers while one is worked on, and widen and lay those of the next
 // into LDS, as rows loaded directly would be, between the products of this one's scores.  A load of a wave is one kilobyte of one page, so its page
-// and scales are the wave's.  Two streams of 1560 queries on 21840 and 7800 keys, eight heads on two, d = 128, bf16: 263 us a call.  Of a kernel
+// and scales are the wave's.  Two streams of 1560 queries on 21840 and 7800 keys, eight heads on two, d = 128, bf16: 263 us a call (nine pieces).  Of a kernel
 // of 287 us (eight pieces, traced) the widening with its writes took 25, the loads 20, both together 67.  Bytes two tiles ahead: 265
 // against 257; eight waves to 256 rows, each with half of the widening: 242 to 287 by how their rounds fall, against 256.
 template <typename T, int D> struct PageTiles {

@@ -332,6 +332,7 @@ __global__ __launch_bounds__(256) void gated_sum_kernel(const float *__restrict_
 // Lanes to a row and pieces to a lane: few elements a lane, a row to a block where a wave would hold more than two pieces.  (A wave to rows of 2048, four
 // pieces a lane: the backward's registers leave one wave a SIMD, 32768 rows in bf16 346 us.)  Past two pieces a lane of 256, 512 lanes, for the same
 // reason; us, 256 and 512: 20000 rows of 4480 in bf16 352, 224; 1500 of 8192 100, 46; in fp32 of 2560 362, 252; 1500 of 8192 104, 75.
+// (Spilled: 19 and 21 registers of bf16 rows past 2048 in pieces of one element, 4 of fp32 rows past 4096.)
 NormShape bwd_shape(int n, int ch)
 {
     const int pieces = (n + ch - 1) / ch;
